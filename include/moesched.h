@@ -433,6 +433,53 @@ int moesched_path_run(const moesched_path_t* h_path, int B, int N, const int32_t
                       const moesched_model_t* h_model, int overlap, void* stream);
 
 /*
+ * Demand matrices from the router's choices (paper Sec. 2.1: an expert-parallel layer sends every token to the ranks that host
+ * its chosen experts). Rank i of all-to-all b has S choices, d_experts[b][i][s] = expert of choice s, or -1 for none
+ * (a dropped token, padding). The E experts sit in blocks, P = E / N on a rank, so expert e belongs to rank e / P.
+ *   d_counts[b][i][e] = choices of rank i for expert e
+ *   d_demand[b][i][j] = sum of d_counts over the experts of rank j: the input of the decompositions
+ *   d_slot[b][i][s]   = place of choice s among rank i's choices sorted by expert, equal experts in the order of s: its
+ *                       row in the send buffer, where the rows of a pair (i, j) lie together; -1 for choices that are not sent
+ * A choice outside -1 .. E-1 is treated as not sent, and its source is marked BAD_INPUT.
+ *
+ *   d_experts  in   [B][N][S] int32, S >= 0;  B * N <= 2^31-1
+ *   E          in   a multiple of N, at most MOESCHED_MAX_EXPERTS
+ *   d_demand   out  [B][N][N] int32;  d_counts  out  [B][N][E] int32;  d_slot  out  [B][N][S] int32
+ *   d_status   out  [B][N] int32: OK or BAD_INPUT, one for every source
+ */
+#define MOESCHED_MAX_EXPERTS 1024
+int moesched_route_demand(int B, int N, int S, int E, const int32_t* d_experts, int32_t* d_demand, int32_t* d_counts,
+                          int32_t* d_slot, int32_t* d_status, void* stream);
+
+/*
+ * Where the tokens of a schedule go: the replay of moesched_schedule_eval, with the place of every transfer. For matching
+ * k < count[b] and source i, j = perm[b][k][i], with `used` = what earlier matchings have carried of the pair (i, j):
+ *   d_start[b][k][i]  = min(D_ij, used)               first token of the pair's that matching k carries
+ *   d_length[b][k][i] = min(D_ij - start, dur_k)      tokens that it carries
+ *   d_row[b][k][i]    = tokens that rank j has received in the matchings before k: row of its receive buffer where
+ *                       the transfer lands (arrivals lie in the order of the matchings)
+ * All three are 0 for k >= count[b]. d_rows[b][j] = tokens that rank j receives in all. With d_counts, the choices by
+ * expert of moesched_route_demand, a pair's tokens lie by expert, and
+ *   d_offsets[b][j][k * P + e] = first row of rank j's receive buffer that matching k fills for an expert e' >= e of rank j's P,
+ * the last of the K * P + 1 entries being d_rows[b][j]: the d_offsets that the expert entry points below take, for all matchings
+ * (groups = K * P) or for those of one (groups = P, from entry k * P on).
+ *
+ *   d_demand, k_stride, d_perm, d_dur, d_count   in   as in moesched_schedule_eval
+ *   experts_per_rank  in   P >= 1, N * P <= MOESCHED_MAX_EXPERTS;  ignored without d_counts
+ *   d_counts   in   [B][N][N * P] int32, the sums over each rank's P experts being d_demand; NULL: no offsets are made
+ *   d_start, d_length, d_row   out  [B][k_stride][N] int32
+ *   d_rows     out  [B][N] int32
+ *   d_offsets  out  [B][N][k_stride * P + 1] int32; NULL if and only if d_counts is
+ *   d_status   out  [B] int32 OK, or BAD_INPUT: a negative entry or duration, a row that is no permutation, a count out of
+ *                   range, counts that do not add up to the demand of a pair that is served, or over 2^31-1 rows; all outputs of
+ *                   that matrix are then 0
+ */
+int moesched_schedule_slots(int B, int N, const int32_t* d_demand, int k_stride, const uint8_t* d_perm, const int32_t* d_dur,
+                            const int32_t* d_count, int experts_per_rank, const int32_t* d_counts, int32_t* d_start,
+                            int32_t* d_length, int32_t* d_row, int32_t* d_rows, int32_t* d_offsets, int32_t* d_status,
+                            void* stream);
+
+/*
  * Measurement aid (no counterpart in the paper): enqueue a kernel of `blocks` CTAs of 256
  * threads, each thread running 8 independent chains of add / min / xor for `iters`
  * iterations, and return the number of integer lane-operations it executes

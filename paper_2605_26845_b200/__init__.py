@@ -55,6 +55,7 @@ _SIGNATURES = {
     "moesched_sinkhorn_scale": "iipidipppppp", "moesched_sinkhorn_durations": "iipppipp",
     "moesched_schedule_order": "iipippp" + "p" * 8, "moesched_schedule_permute": "iiipppppp",
     "moesched_best_budget": "iipppqppp", "moesched_bvn_real_decompose": "iipdipppppppp",
+    "moesched_route_demand": "iiii" + "p" * 6, "moesched_schedule_slots": "iipipppi" + "p" * 8,
     "moesched_path_run": "piippip", "moesched_last_cuda_error": "",
 }
 
@@ -429,6 +430,59 @@ def best_budget(count, prefix_overlap_ns, prefix_unserved_tokens, ns_per_unserve
     _call("moesched_best_budget", po.device, B, K, _ptr(count), _ptr(po), _ptr(pu), int(ns_per_unserved_token),
           _ptr(best_k), _ptr(best_cost))
     return {"best_k": best_k, "best_cost": best_cost}
+
+
+MAX_EXPERTS = 1024
+
+
+def route_demand(experts, num_experts, out=None) -> dict:
+    """Demand matrices from the router's choices: experts [B, N, S] int32 (expert of every choice of every rank, -1 for none).
+    The num_experts experts sit in equal blocks on the N ranks. Returns 'demand' [B, N, N], 'counts' [B, N, num_experts], 'slot'
+    [B, N, S] (row of every choice in its rank's send buffer, which lies by expert; -1 for none) and 'status' [B, N], all
+    int32; `out` may hand back the dict of an earlier call of the same shape for reuse."""
+    experts = _dev(experts, torch.int32, "experts")
+    if experts.dim() != 3:
+        raise MoeschedError("experts must have shape [B, N, S]")
+    B, N, S = experts.shape
+    E, dev = int(num_experts), experts.device
+    shapes = dict(demand=(B, N, N), counts=(B, N, E), slot=(B, N, S), status=(B, N))
+    if out is None:
+        out = {k: torch.empty(v, dtype=torch.int32, device=dev) for k, v in shapes.items()}
+    elif any(_dev(out[k], torch.int32, f"out['{k}']").shape != v or out[k].device != dev for k, v in shapes.items()):
+        raise MoeschedError("out has the wrong shape or device")
+    _call("moesched_route_demand", dev, B, N, S, E, _ptr(experts), _ptr(out["demand"]), _ptr(out["counts"]), _ptr(out["slot"]),
+          _ptr(out["status"]))
+    return out
+
+
+def schedule_slots(demand, perm, dur, count, counts=None) -> dict:
+    """Place of every transfer of a schedule: 'start' (first token of the pair's), 'length' (tokens) and 'row' (first row in
+    the receiver's buffer), [B, k_stride, N] int32 by matching and source; 'rows' [B, N] (tokens that a rank receives);
+    'status' [B]. With counts (route_demand's) also 'offsets' [B, N, k_stride * P + 1], P = experts per rank: the rows
+    of every matching and expert in a rank's receive buffer, as expert_ffn and expert_matvec4 take them."""
+    demand = _check_demand(demand)
+    perm = _dev(perm, torch.uint8, "perm")
+    dur = _dev(dur, torch.int32, "dur")
+    count = _dev(count, torch.int32, "count")
+    B, N, _ = demand.shape
+    if perm.dim() != 3 or perm.shape[0] != B or perm.shape[2] != N or dur.shape != perm.shape[:2] or count.shape != (B,):
+        raise MoeschedError("perm must be [B, k_stride, N], dur [B, k_stride] and count [B]")
+    K, P, dev = int(perm.shape[1]), 0, demand.device
+    if counts is not None:
+        counts = _dev(counts, torch.int32, "counts")
+        if counts.dim() != 3 or counts.shape[:2] != (B, N) or counts.shape[2] % N != 0:
+            raise MoeschedError("counts must be [B, N, N * experts per rank]")
+        P = counts.shape[2] // N
+    if any(t is not None and t.device != dev for t in (perm, dur, count, counts)):
+        raise MoeschedError("all tensors must be on one device")
+    start, length, row = torch.empty((3, B, K, N), dtype=torch.int32, device=dev).unbind(0)
+    res = dict(start=start, length=length, row=row, rows=torch.empty((B, N), dtype=torch.int32, device=dev),
+               status=torch.empty(B, dtype=torch.int32, device=dev))
+    if counts is not None:
+        res["offsets"] = torch.empty((B, N, K * P + 1), dtype=torch.int32, device=dev)
+    _call("moesched_schedule_slots", dev, B, N, _ptr(demand), K, _ptr(perm), _ptr(dur), _ptr(count), P, _ptr(counts), _ptr(start),
+          _ptr(length), _ptr(row), _ptr(res["rows"]), _ptr(res.get("offsets")), _ptr(res["status"]))
+    return res
 
 
 class Path:

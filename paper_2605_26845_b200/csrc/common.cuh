@@ -250,6 +250,13 @@ cudaError_t run_bvn_real(int B, int N, const double* matrix, double tol, int k_m
                          int32_t* count, double* sum_lambda, double* max_left, double* scratch, int32_t* status,
                          cudaStream_t stream);
 
+// router's choices to demand (route_kernel.cu), places of a schedule's transfers (slots_kernel.cu)
+cudaError_t run_route(int B, int N, int S, int E, const int32_t* experts, int32_t* demand, int32_t* counts, int32_t* slot,
+                      int32_t* status, cudaStream_t stream);
+cudaError_t run_slots(int B, int N, const int32_t* demand, int K, const uint8_t* perm, const int32_t* dur, const int32_t* count,
+                      int P, const int32_t* counts, int32_t* start, int32_t* length, int32_t* row, int32_t* rows,
+                      int32_t* offsets, int32_t* status, cudaStream_t stream);
+
 // All of an SM's memory that can be shared memory is, while the kernel runs there. (A preference: failing is harmless.)
 template <typename Kernel>
 void prefer_shared_memory(Kernel kern) {
