@@ -480,6 +480,72 @@ int moesched_schedule_slots(int B, int N, const int32_t* d_demand, int k_stride,
                             void* stream);
 
 /*
+ * The expert batch itself: what expert_fixed_ns and expert_ps_per_token of the model stand for (paper Sec. 2.1 and Fig. 1: the
+ * time of an expert's feed-forward block against the tokens that it gets).
+ *
+ * Rows (tokens) lie by group: group g = rows d_offsets[g] .. d_offsets[g + 1] - 1 of the [R] rows, and belongs to expert g % E.
+ * `groups` is a multiple of E: E for one batch, K * E for what K matchings brought (moesched_schedule_slots writes such offsets).
+ * Groups may be empty. Rows before the first and behind the last group are neither used nor written. Tensors are densely
+ * packed, row major, 16-byte aligned, all of one type, MOESCHED_BF16 or MOESCHED_FP16; products are summed in 32 bits.
+ * Values beyond the type's range become infinities.
+ */
+#define MOESCHED_BF16 0
+#define MOESCHED_FP16 1
+#define MOESCHED_ACT_SILU 0 /* a / (1 + exp(-a)) */
+#define MOESCHED_ACT_GELU 1 /* a F(a), F the normal distribution (not its tanh approximation) */
+
+/*
+ * Gated feed-forward block: for a row x of expert e
+ *   a = Wg_e x,  u = Wu_e x,  h = act(a) * u,  y = Wd_e h.
+ * a and u are summed and h is computed in 32 bits; h is rounded to the type once, for the second product, and y once.
+ *
+ *   d_x        in   [R][D];  D, I multiples of 8, 8 .. 65536
+ *   d_w_gate, d_w_up  in  [E][I][D];  d_w_down  in  [E][D][I];  E <= MOESCHED_MAX_EXPERTS
+ *   d_offsets  in   [groups + 1] int32
+ *   d_y        out  [R][D]
+ *   d_gate, d_up  out  [R][I] a and u, rounded to the type, for the backward pass; both may be NULL
+ *   d_scratch  tmp  moesched_expert_scratch_bytes(R, I, groups, 0) bytes, 256-byte aligned; calls that overlap need their own
+ *   d_status   out  [1] int32: OK, or BAD_INPUT where the offsets are not in order or not within 0 .. R: the outputs then
+ *                   hold nothing of use
+ */
+size_t moesched_expert_scratch_bytes(int R, int I, int groups, int backward);
+int moesched_expert_ffn(int R, int D, int I, int E, int groups, int dtype, int act, const void* d_x, const void* d_w_gate,
+                        const void* d_w_up, const void* d_w_down, const int32_t* d_offsets, void* d_y, void* d_gate,
+                        void* d_up, void* d_scratch, int32_t* d_status, void* stream);
+
+/*
+ * Its backward pass: from dY, the inputs, and a and u as moesched_expert_ffn wrote them
+ *   dh = dY Wd,  da = dh u act'(a),  du = dh act(a),  h = act(a) u,
+ *   dX = da Wg + du Wu;  dWg_e = sum da^T x,  dWu_e = sum du^T x,  dWd_e = sum dy^T h  over the rows of expert e (0 without rows).
+ * da, du and h are rounded to the type once, as the operands of the products that follow; sums are in 32 bits.
+ *
+ *   d_dy      in   [R][D];  d_gate, d_up  in  [R][I];  the others as above
+ *   d_dx      out  [R][D], rows outside the groups left as they were
+ *   d_dw_gate, d_dw_up  out  [E][I][D];  d_dw_down  out  [E][D][I]: written, not added to
+ *   d_scratch tmp  moesched_expert_scratch_bytes(R, I, groups, 1) bytes, 256-byte aligned
+ */
+int moesched_expert_ffn_backward(int R, int D, int I, int E, int groups, int dtype, int act, const void* d_dy, const void* d_x,
+                                 const void* d_w_gate, const void* d_w_up, const void* d_w_down, const int32_t* d_offsets,
+                                 const void* d_gate, const void* d_up, void* d_dx, void* d_dw_gate, void* d_dw_up,
+                                 void* d_dw_down, void* d_scratch, int32_t* d_status, void* stream);
+
+/*
+ * Products of few rows with weights in 4 bits: an expert's batch while decoding. For a row x of expert e
+ *   y_n = sum_k W[e][n][k] x_k,  W[e][n][k] = (q - 8) * scale[e][n][k / group],
+ * or, with a second matrix, act(W x) * (W_up x). The q of k = 2m is the low half of byte m. The sum over a group is made in 32
+ * bits before it is scaled. The weights are read once for every eight rows of an expert.
+ *
+ *   d_x      in   [R][K];  K a multiple of group, group 32, 64 or 128
+ *   d_w      in   [E][N][K / 2] bytes;  d_scale  in  [E][N][K / group], in the type of d_x;  N >= 1
+ *   d_w_up, d_scale_up  in  the same for the second matrix; both NULL: the plain product, and `act` is not looked at
+ *   d_y      out  [R][N]
+ *   d_status out  [1] int32, as above
+ */
+int moesched_expert_matvec4(int R, int K, int N, int E, int groups, int group, int dtype, int act, const void* d_x,
+                            const uint8_t* d_w, const void* d_scale, const uint8_t* d_w_up, const void* d_scale_up,
+                            const int32_t* d_offsets, void* d_y, int32_t* d_status, void* stream);
+
+/*
  * Measurement aid (no counterpart in the paper): enqueue a kernel of `blocks` CTAs of 256
  * threads, each thread running 8 independent chains of add / min / xor for `iters`
  * iterations, and return the number of integer lane-operations it executes

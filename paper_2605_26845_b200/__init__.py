@@ -56,6 +56,8 @@ _SIGNATURES = {
     "moesched_schedule_order": "iipippp" + "p" * 8, "moesched_schedule_permute": "iiipppppp",
     "moesched_best_budget": "iipppqppp", "moesched_bvn_real_decompose": "iipdipppppppp",
     "moesched_route_demand": "iiii" + "p" * 6, "moesched_schedule_slots": "iipipppi" + "p" * 8,
+    "moesched_expert_ffn": "i" * 7 + "p" * 11, "moesched_expert_ffn_backward": "i" * 7 + "p" * 15,
+    "moesched_expert_matvec4": "i" * 8 + "p" * 9,
     "moesched_path_run": "piippip", "moesched_last_cuda_error": "",
 }
 
@@ -73,6 +75,7 @@ def _open(path):
         fn.restype, fn.argtypes = ctypes.c_int, [_ARGTYPES[c] for c in signature]
     lib.moesched_bvn_scratch_bytes.restype = ctypes.c_size_t
     lib.moesched_order_scratch_bytes.restype = ctypes.c_size_t
+    lib.moesched_expert_scratch_bytes.restype = ctypes.c_size_t
     lib.moesched_probe_int_ops.restype = ctypes.c_longlong
     lib.moesched_debug_index_faults.restype = ctypes.c_longlong
     return lib
@@ -483,6 +486,144 @@ def schedule_slots(demand, perm, dur, count, counts=None) -> dict:
     _call("moesched_schedule_slots", dev, B, N, _ptr(demand), K, _ptr(perm), _ptr(dur), _ptr(count), P, _ptr(counts), _ptr(start),
           _ptr(length), _ptr(row), _ptr(res["rows"]), _ptr(res.get("offsets")), _ptr(res["status"]))
     return res
+
+
+_ACTS = {"silu": 0, "gelu": 1}
+_TYPES = {torch.bfloat16: 0, torch.float16: 1}
+
+
+def _act(act):
+    if act not in _ACTS:
+        raise MoeschedError(f"act must be one of {sorted(_ACTS)}")
+    return _ACTS[act]
+
+
+def _expert_rows(x, offsets, num_experts):
+    """Element type of x [R, width] and number of groups of offsets; both checked."""
+    if not isinstance(x, torch.Tensor) or x.dtype not in _TYPES:
+        raise MoeschedError("x must be bfloat16 or float16")
+    x = _dev(x, x.dtype, "x")
+    offsets = _dev(offsets, torch.int32, "offsets")
+    groups = offsets.numel() - 1
+    if x.dim() != 2 or offsets.dim() != 1 or num_experts < 1 or groups < 1 or groups % num_experts != 0:
+        raise MoeschedError("x must be [R, width] and offsets [groups + 1], groups a multiple of the number of experts")
+    return _TYPES[x.dtype], groups
+
+
+def _like(t, like, shape, what):
+    """`t`, or a new tensor, of the type and device of `like` and the given shape."""
+    if t is None:
+        return torch.empty(shape, dtype=like.dtype, device=like.device)
+    _dev(t, like.dtype, what)
+    if t.shape != tuple(shape) or t.device != like.device:
+        raise MoeschedError(f"{what} must have shape {tuple(shape)}, on the device of x")
+    return t
+
+
+def _expert_weights(x, w_gate, w_up, w_down):
+    if not isinstance(w_gate, torch.Tensor) or w_gate.dim() != 3 or x.dim() != 2:
+        raise MoeschedError("x must be [R, D], w_gate and w_up [E, I, D] and w_down [E, D, I]")
+    E, I, D = w_gate.shape
+    for t, shape, what in ((w_gate, (E, I, D), "w_gate"), (w_up, (E, I, D), "w_up"), (w_down, (E, D, I), "w_down")):
+        if t is None:
+            raise MoeschedError(f"{what} is missing")
+        _like(t, x, shape, what)
+    if x.shape[1] != D:
+        raise MoeschedError("x must be [R, D] with the D of the weights")
+    return E, I, D
+
+
+def _status_of(status, device):
+    if status is None:
+        return torch.empty(1, dtype=torch.int32, device=device)
+    _dev(status, torch.int32, "status")
+    if status.numel() != 1 or status.device != device:
+        raise MoeschedError("status must hold one int32, on the device of x")
+    return status
+
+
+def _expert_scratch(scratch, x, I, groups, backward):
+    """256-byte aligned working memory: the caller's (uint8), or new."""
+    need = int(load_library().moesched_expert_scratch_bytes(x.shape[0], I, groups, backward))
+    if scratch is None:
+        return torch.empty(max(1, need), dtype=torch.uint8, device=x.device)
+    _dev(scratch, torch.uint8, "scratch")
+    if scratch.numel() < need or scratch.device != x.device:
+        raise MoeschedError("scratch is smaller than expert_scratch_bytes, or on another device")
+    return scratch
+
+
+def expert_scratch_bytes(rows, width, groups, backward=False) -> int:
+    """Working memory of expert_ffn (or its backward pass) for that many rows, a hidden width of `width` and `groups` groups."""
+    return int(load_library().moesched_expert_scratch_bytes(int(rows), int(width), int(groups), int(backward)))
+
+
+def expert_ffn(x, w_gate, w_up, w_down, offsets, act="silu", save=False, out=None, scratch=None, status=None):
+    """Gated feed-forward block of the experts, y = (act(x Wg^T) * (x Wu^T)) Wd^T, on rows grouped by expert: group g of
+    x [R, D] is rows offsets[g] .. offsets[g+1]-1 and belongs to expert g % E. w_gate, w_up [E, I, D], w_down [E, D, I], bfloat16
+    or float16; offsets [groups + 1] int32, groups a multiple of E (schedule_slots' offsets of a rank, or the part of them for one matching).
+    Returns y [R, D]; rows outside the groups are left as they were (undefined in a tensor made here). With save=True
+    returns (y, saved) for expert_ffn_backward. `status` [1] int32 takes the outcome (ST_BAD_INPUT: offsets out of order);
+    `scratch` is working memory of expert_scratch_bytes(R, I, groups)."""
+    E, I, D = _expert_weights(x, w_gate, w_up, w_down)
+    dtype, groups = _expert_rows(x, offsets, E)
+    if offsets.device != x.device:
+        raise MoeschedError("all tensors must be on one device")
+    R, dev = x.shape[0], x.device
+    out = _like(out, x, (R, D), "out")
+    saved = {k: torch.empty((R, I), dtype=x.dtype, device=dev) for k in ("gate", "up")} if save else {}
+    scratch = _expert_scratch(scratch, x, I, groups, 0)
+    _call("moesched_expert_ffn", dev, R, D, I, E, groups, dtype, _act(act), _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(w_down),
+          _ptr(offsets), _ptr(out), _ptr(saved.get("gate")), _ptr(saved.get("up")), _ptr(scratch), _ptr(_status_of(status, dev)))
+    return (out, saved) if save else out
+
+
+def expert_ffn_backward(dy, x, w_gate, w_up, w_down, offsets, saved, act="silu", out=None, scratch=None, status=None) -> dict:
+    """Gradients of expert_ffn: 'dx' [R, D], 'dw_gate', 'dw_up' [E, I, D] and 'dw_down' [E, D, I] (0 for an expert without rows)
+    from dy [R, D], the inputs of the forward call and what it saved. `out` may hand back the dict of an earlier
+    call for reuse; `scratch` is working memory of expert_scratch_bytes(R, I, groups, True)."""
+    E, I, D = _expert_weights(x, w_gate, w_up, w_down)
+    dtype, groups = _expert_rows(x, offsets, E)
+    R, dev = x.shape[0], x.device
+    if offsets.device != dev:
+        raise MoeschedError("all tensors must be on one device")
+    for t, shape, what in ((dy, (R, D), "dy"), (saved["gate"], (R, I), "saved['gate']"), (saved["up"], (R, I), "saved['up']")):
+        if t is None:
+            raise MoeschedError(f"{what} is missing")
+        _like(t, x, shape, what)
+    shapes = dict(dx=(R, D), dw_gate=(E, I, D), dw_up=(E, I, D), dw_down=(E, D, I))
+    grads = {k: _like(None if out is None else out[k], x, v, k) for k, v in shapes.items()}
+    scratch = _expert_scratch(scratch, x, I, groups, 1)
+    _call("moesched_expert_ffn_backward", dev, R, D, I, E, groups, dtype, _act(act), _ptr(dy), _ptr(x), _ptr(w_gate), _ptr(w_up),
+          _ptr(w_down), _ptr(offsets), _ptr(saved["gate"]), _ptr(saved["up"]), *(_ptr(grads[k]) for k in shapes), _ptr(scratch),
+          _ptr(_status_of(status, dev)))
+    return grads
+
+
+def expert_matvec4(x, weight, scale, offsets, weight_up=None, scale_up=None, act="silu", out=None, status=None):
+    """Products of a few rows with their experts' 4-bit weights: y[r, n] = sum_k (q - 8) scale[e, n, k // group] x[r, k], the q of
+    k = 2m in the low half of byte m of weight [E, N, K / 2] uint8, scale [E, N, K / group] in the type of x (bfloat16
+    or float16), group 32, 64 or 128. With weight_up and scale_up, act(x W^T) * (x W_up^T). Rows lie by group as in expert_ffn."""
+    if not isinstance(weight, torch.Tensor) or not isinstance(scale, torch.Tensor) or weight.dim() != 3 or scale.dim() != 3:
+        raise MoeschedError("weight must be [E, N, K / 2] and scale [E, N, K / group]")
+    E, N = weight.shape[:2]
+    K = 2 * weight.shape[2]
+    dtype, groups = _expert_rows(x, offsets, E)
+    if K == 0 or x.shape[1] != K or scale.shape[2] == 0 or K % scale.shape[2] != 0:
+        raise MoeschedError("x must be [R, K], weight [E, N, K / 2] and scale [E, N, K / group]")
+    if (weight_up is None) != (scale_up is None):
+        raise MoeschedError("weight_up and scale_up go together")
+    for w, s, what in ((weight, scale, ""), (weight_up, scale_up, "_up")):
+        if w is not None:
+            if _dev(w, torch.uint8, "weight" + what).shape != weight.shape or w.device != x.device:
+                raise MoeschedError("weight_up must be like weight, on the device of x")
+            _like(s, x, (E, N, scale.shape[2]), "scale" + what)
+    if offsets.device != x.device:
+        raise MoeschedError("all tensors must be on one device")
+    out = _like(out, x, (x.shape[0], N), "out")
+    _call("moesched_expert_matvec4", x.device, x.shape[0], K, N, E, groups, K // scale.shape[2], dtype, _act(act), _ptr(x), _ptr(weight),
+          _ptr(scale), _ptr(weight_up), _ptr(scale_up), _ptr(offsets), _ptr(out), _ptr(_status_of(status, x.device)))
+    return out
 
 
 class Path:

@@ -55,6 +55,7 @@ void register_fault_reader(FaultReader reader) { fault_readers().push_back(reade
 #endif
 
 static bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3) == 0; }
+static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 static bool aligned8(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 7) == 0; }
 
 // The argument checks of the entry points that moesched_path_run is made of.
@@ -72,6 +73,12 @@ static bool bvn_pointers_ok(const void* demand, const void* perm, const void* co
 static bool eval_pointers_ok(const void* demand, const void* perm, const void* dur, const void* count, const void* status) {
   return demand && perm && dur && count && status && aligned4(demand) && aligned4(dur) && aligned4(count) && aligned4(status);
 }
+
+static bool expert_sizes_ok(int R, int E, int groups, int dtype, int act) {
+  return R >= 0 && E >= 1 && E <= MOESCHED_MAX_EXPERTS && groups >= E && groups % E == 0 && groups <= (1 << 24) &&
+         (dtype == MOESCHED_BF16 || dtype == MOESCHED_FP16) && (act == MOESCHED_ACT_SILU || act == MOESCHED_ACT_GELU);
+}
+static bool ffn_width_ok(int v) { return v >= 8 && v <= 65536 && v % 8 == 0; }
 
 }  // namespace moesched
 
@@ -366,6 +373,60 @@ int moesched_schedule_slots(int B, int N, const int32_t* d_demand, int k_stride,
     return MOESCHED_EINVAL;
   cudaError_t e = run_slots(B, N, d_demand, k_stride, d_perm, d_dur, d_count, experts_per_rank, d_counts, d_start, d_length, d_row,
                             d_rows, d_offsets, d_status, static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? MOESCHED_OK : fail_cuda(e);
+}
+
+size_t moesched_expert_scratch_bytes(int R, int I, int groups, int backward) {
+  if (R < 0 || !ffn_width_ok(I) || groups < 1 || groups > (1 << 24)) return 0;
+  return expert_scratch(R, I, groups, backward != 0).bytes;
+}
+
+int moesched_expert_ffn(int R, int D, int I, int E, int groups, int dtype, int act, const void* d_x, const void* d_w_gate,
+                        const void* d_w_up, const void* d_w_down, const int32_t* d_offsets, void* d_y, void* d_gate,
+                        void* d_up, void* d_scratch, int32_t* d_status, void* stream) {
+  if (!expert_sizes_ok(R, E, groups, dtype, act) || !ffn_width_ok(D) || !ffn_width_ok(I)) return MOESCHED_EINVAL;
+  if ((d_gate == nullptr) != (d_up == nullptr) || !d_offsets || !aligned4(d_offsets) || !d_status || !aligned4(d_status))
+    return MOESCHED_EINVAL;
+  const void* pointers[] = {d_x, d_w_gate, d_w_up, d_w_down, d_y, d_scratch};
+  for (const void* p : pointers)
+    if ((R > 0 && p == nullptr) || !aligned16(p)) return MOESCHED_EINVAL;
+  if (!aligned16(d_gate) || !aligned16(d_up) || (reinterpret_cast<uintptr_t>(d_scratch) & 255) != 0) return MOESCHED_EINVAL;
+  cudaError_t e = run_expert_ffn(R, D, I, E, groups, dtype, act, d_x, d_w_gate, d_w_up, d_w_down, d_offsets, d_y, d_gate, d_up,
+                                 d_scratch, d_status, static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? MOESCHED_OK : fail_cuda(e);
+}
+
+int moesched_expert_ffn_backward(int R, int D, int I, int E, int groups, int dtype, int act, const void* d_dy, const void* d_x,
+                                 const void* d_w_gate, const void* d_w_up, const void* d_w_down, const int32_t* d_offsets,
+                                 const void* d_gate, const void* d_up, void* d_dx, void* d_dw_gate, void* d_dw_up,
+                                 void* d_dw_down, void* d_scratch, int32_t* d_status, void* stream) {
+  if (!expert_sizes_ok(R, E, groups, dtype, act) || !ffn_width_ok(D) || !ffn_width_ok(I)) return MOESCHED_EINVAL;
+  if (!d_offsets || !aligned4(d_offsets) || !d_status || !aligned4(d_status) || !d_dw_gate || !d_dw_up || !d_dw_down ||
+      !d_scratch || (reinterpret_cast<uintptr_t>(d_scratch) & 255) != 0)
+    return MOESCHED_EINVAL;
+  const void* pointers[] = {d_dy, d_x, d_w_gate, d_w_up, d_w_down, d_gate, d_up, d_dx, d_dw_gate, d_dw_up, d_dw_down};
+  for (const void* p : pointers)
+    if ((R > 0 && p == nullptr) || !aligned16(p)) return MOESCHED_EINVAL;
+  cudaError_t e = run_expert_backward(R, D, I, E, groups, dtype, act, d_dy, d_x, d_w_gate, d_w_up, d_w_down, d_offsets, d_gate, d_up,
+                                      d_dx, d_dw_gate, d_dw_up, d_dw_down, d_scratch, d_status, static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? MOESCHED_OK : fail_cuda(e);
+}
+
+int moesched_expert_matvec4(int R, int K, int N, int E, int groups, int group, int dtype, int act, const void* d_x,
+                            const uint8_t* d_w, const void* d_scale, const uint8_t* d_w_up, const void* d_scale_up,
+                            const int32_t* d_offsets, void* d_y, int32_t* d_status, void* stream) {
+  if (d_w_up == nullptr) act = MOESCHED_ACT_SILU;   // (not looked at)
+  if (!expert_sizes_ok(R, E, groups, dtype, act) || K < 1 || N < 1 || (group != 32 && group != 64 && group != 128) ||
+      K % group != 0 || K > (1 << 24) || N > (1 << 24))
+    return MOESCHED_EINVAL;
+  if ((d_w_up == nullptr) != (d_scale_up == nullptr) || !d_offsets || !aligned4(d_offsets) || !d_status || !aligned4(d_status))
+    return MOESCHED_EINVAL;
+  const void* pointers[] = {d_x, d_w, d_scale, d_y};
+  for (const void* p : pointers)
+    if ((R > 0 && p == nullptr) || !aligned16(p)) return MOESCHED_EINVAL;
+  if (!aligned16(d_w_up) || !aligned16(d_scale_up)) return MOESCHED_EINVAL;
+  cudaError_t e = run_few(R, K, N, E, groups, group, dtype, act, d_x, d_w, d_scale, d_w_up, d_scale_up, d_offsets, d_y, nullptr,
+                          nullptr, d_status, static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? MOESCHED_OK : fail_cuda(e);
 }
 
