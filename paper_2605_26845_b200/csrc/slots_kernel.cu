@@ -13,10 +13,13 @@ namespace moesched {
 
 constexpr int SLOT_CHUNK = 32;         // matchings per step: one per lane
 constexpr int SLOT_FUSED_N = 128;      // up to here the pairs of a whole matrix fit one CTA's shared memory
+constexpr int SLOT_MAX_PARTS = 8;      // CTAs that share the matchings of one matrix
 constexpr int SLOT_BLOCK = 64;         // sources per CTA above
 
 struct SlotArgs {
   int N, K, P, CS;                     // CS: CTAs of a cluster, each with a stretch of the matchings
+  unsigned per_n, per_sources;         // 2^22 / N and 2^22 / (sources of a CTA), rounded up (see slot_row)
+  bool words, quads;                   // four destinations, four choices by expert at a time
   const int32_t* demand;
   const uint8_t* perm;
   const int32_t* dur;
@@ -29,14 +32,21 @@ struct SlotArgs {
 __host__ __device__ inline int slot_int_stride(int N) { return N | 1; }
 __host__ __device__ inline int slot_byte_stride(int N) { return 4 * (((N + 3) / 4) | 1); }
 
+// q / n for q < 32 n, n <= 256, with m = ceil(2^22 / n): the quotient is off by less than q / 2^22 < 1 / n
+__host__ __device__ inline unsigned slot_reciprocal(int n) { return ((1u << 22) + n - 1) / n; }
+__device__ __forceinline__ int slot_row(int q, unsigned m) { return (int)((unsigned)q * m >> 22); }
+// offsets of a receiver that a warp collects before it stores them side by side (ints; more go out as they come)
+constexpr int SLOT_STAGED_P = 8;
+__host__ __device__ inline int slot_staged(int P) { return P <= SLOT_STAGED_P ? SLOT_CHUNK * P : 0; }
+
 struct SlotSmem {
-  size_t pairs, received, start, len, begins, perm, source, dur, bad, bytes;
+  size_t pairs, received, start, len, begins, perm, source, dur, bad, seen, staged, bytes;
 };
 // `sources` in this CTA (with their pairs if it walks them), and `receivers` (all of them, or none)
-__host__ __device__ inline SlotSmem slot_smem(int N, int sources, bool pairs, int receivers) {
+__host__ __device__ inline SlotSmem slot_smem(int N, int sources, bool pairs, int receivers, int warps, int staged) {
   SlotSmem m;
   size_t at = 0;
-  m.pairs = at, at += pairs ? align16((size_t)sources * N * sizeof(int2)) : 0;
+  m.pairs = at, at += pairs ? align16((size_t)sources * slot_int_stride(N) * sizeof(int2)) : 0;
   m.received = at, at += align16((size_t)receivers * sizeof(long long));
   m.start = at, at += align16((size_t)SLOT_CHUNK * slot_int_stride(sources) * 4);
   m.len = at, at += align16((size_t)SLOT_CHUNK * slot_int_stride(sources) * 4);
@@ -44,7 +54,9 @@ __host__ __device__ inline SlotSmem slot_smem(int N, int sources, bool pairs, in
   m.perm = at, at += align16((size_t)SLOT_CHUNK * slot_byte_stride(N));
   m.source = at, at += align16((size_t)SLOT_CHUNK * slot_int_stride(receivers) * 2);
   m.dur = at, at += SLOT_CHUNK * 4;
-  m.bad = at, at += 4;
+  m.bad = at, at += 16;
+  m.seen = at, at += pairs ? align16((size_t)warps * slot_byte_stride(N)) : 0;
+  m.staged = at, at += (size_t)warps * staged * 4;
   m.bytes = at;
   return m;
 }
@@ -60,8 +72,8 @@ __global__ void __launch_bounds__(1024) slots_kernel(const SlotArgs a) {
   const size_t b = blockIdx.x / a.CS;
   const int i0 = SOURCES && !RECEIVERS ? blockIdx.y * SLOT_BLOCK : 0;
   const int sources = SOURCES && !RECEIVERS ? min(SLOT_BLOCK, N - i0) : N;
-  const SlotSmem at = slot_smem(N, SOURCES && !RECEIVERS ? SLOT_BLOCK : N, SOURCES, RECEIVERS ? N : 0);
-  const int IS = slot_int_stride(SOURCES && !RECEIVERS ? SLOT_BLOCK : N), BS = slot_byte_stride(N);
+  const SlotSmem at = slot_smem(N, SOURCES && !RECEIVERS ? SLOT_BLOCK : N, SOURCES, RECEIVERS ? N : 0, blockDim.x >> 5, 0);
+  const int IS = slot_int_stride(SOURCES && !RECEIVERS ? SLOT_BLOCK : N), BS = slot_byte_stride(N), PS = slot_int_stride(N);
   int2* pairs = reinterpret_cast<int2*>(smem + at.pairs);          // x used, y demand
   long long* received = reinterpret_cast<long long*>(smem + at.received);
   int* c_start = reinterpret_cast<int*>(smem + at.start);
@@ -80,25 +92,38 @@ __global__ void __launch_bounds__(1024) slots_kernel(const SlotArgs a) {
   const int count = bad ? 0 : count_in;
   if (threadIdx.x == 0) *bad_flag = 0;
   if constexpr (SOURCES) {
-    for (int q = threadIdx.x; q < sources * N; q += threads) {
-      const int d = D[(size_t)i0 * N + q];
-      bad |= d < 0;
-      pairs[q] = make_int2(0, max(d, 0));
+    for (int i = warp; i < sources; i += warps) {
+      for (int j = lane; j < PS; j += 32) {
+        const int d = j < N ? D[(size_t)(i0 + i) * N + j] : 0;
+        bad |= d < 0;
+        pairs[i * PS + j] = make_int2(0, max(d, 0));
+      }
     }
   }
   if constexpr (RECEIVERS) {
     for (int j = threadIdx.x; j < N; j += threads) received[j] = 0;
   }
+  uint8_t* seen = smem + at.seen + warp * BS;                      // by receiver: a lane that has named it
+  int* staged = reinterpret_cast<int*>(smem + at.staged) + warp * slot_staged(P);
   const int chunks = (a.K + SLOT_CHUNK - 1) / SLOT_CHUNK;
   const int c_begin = (int)((long long)chunks * part / a.CS), c_end = (int)((long long)chunks * (part + 1) / a.CS);
 
   auto load_chunk = [&](int k0) {
     const int used_k = min(SLOT_CHUNK, count - k0);                // matchings of the chunk that count (may be negative)
-    for (int q = threadIdx.x; q < SLOT_CHUNK * N; q += threads) {
-      const int kk = q / N, i = q - kk * N;
-      if (kk < used_k) c_perm[kk * BS + i] = perm[(size_t)k0 * N + q];
-      if constexpr (RECEIVERS) c_source[kk * IS + i] = -1, c_begins[kk * IS + i] = 0;
+    if (a.words) {
+      const unsigned* from = reinterpret_cast<const unsigned*>(perm + (size_t)k0 * N);
+      for (int q = threadIdx.x; 4 * q < used_k * N; q += threads) {
+        const int kk = slot_row(4 * q, a.per_n), i = 4 * q - kk * N;
+        *reinterpret_cast<unsigned*>(c_perm + kk * BS + i) = from[q];
+      }
+    } else {
+      for (int q = threadIdx.x; q < used_k * N; q += threads) {
+        const int kk = slot_row(q, a.per_n), i = q - kk * N;
+        c_perm[kk * BS + i] = perm[(size_t)k0 * N + q];
+      }
     }
+    if constexpr (RECEIVERS)
+      for (int q = threadIdx.x; q < SLOT_CHUNK * IS / 2; q += threads) reinterpret_cast<unsigned*>(c_source)[q] = FULL;   // -1, -1
     if (threadIdx.x < SLOT_CHUNK) {
       const int d = (int)threadIdx.x < used_k ? dur[k0 + threadIdx.x] : 0;
       bad |= d < 0;
@@ -114,20 +139,25 @@ __global__ void __launch_bounds__(1024) slots_kernel(const SlotArgs a) {
       bad |= live && dest >= N;
       dest = ok ? dest : 0;
       const int d = ok ? c_dur[lane] : 0;
-      const unsigned peers = __match_any_sync(FULL, ok ? dest : -1 - lane);
+      // Do two lanes name one receiver? Each leaves its number there and looks whether it is still there. (Only then a
+      // vote on equal destinations, which takes some 300 cycles for 32 different ones.)
+      if (ok) seen[dest] = (uint8_t)lane;
+      __syncwarp();
+      unsigned peers = 1u << lane;
       long long before = 0;                                        // carried by earlier matchings of the chunk
-      if (__any_sync(FULL, (peers & (peers - 1)) != 0)) {
+      if (__any_sync(FULL, ok && *static_cast<volatile uint8_t*>(seen + dest) != lane)) {
+        peers = __match_any_sync(FULL, ok ? dest : -1 - lane);
 #pragma unroll 4
         for (int s = 0; s < 31; ++s) {
           const int v = __shfl_sync(FULL, d, s);
           if (s < lane && ((peers >> s) & 1u)) before += v;
         }
       }
-      const int2 p = ok ? pairs[MS_AT(i * N + dest, sources * N)] : make_int2(0, 0);
+      const int2 p = ok ? pairs[MS_AT(i * PS + dest, sources * PS)] : make_int2(0, 0);
       const int first = (int)min((long long)p.y, p.x + before);
       const int len = min(p.y - first, d);
       __syncwarp();
-      if (ok && (peers >> lane) == 1u) pairs[MS_AT(i * N + dest, sources * N)].x = first + len;
+      if (ok && (peers >> lane) == 1u) pairs[MS_AT(i * PS + dest, sources * PS)].x = first + len;
       __syncwarp();
       if (keep) {
         c_start[lane * IS + i] = first;
@@ -151,29 +181,28 @@ __global__ void __launch_bounds__(1024) slots_kernel(const SlotArgs a) {
         __syncthreads();
       }
       cluster_sync_all();
-      constexpr int HELD = 16 * 1024 / 1024;                       // pairs per thread: N * N / threads with 1024 threads
-      int held[HELD];
+      // every CTA adds up its share of the pairs for all CTAs, two pairs at a time
+      const int quads = (N * PS + 1) / 2, q_begin = (int)((long long)quads * part / a.CS), q_end = (int)((long long)quads * (part + 1) / a.CS);
+      for (int q = q_begin + threadIdx.x; q < q_end; q += threads) {
+        int4 v[SLOT_MAX_PARTS];
 #pragma unroll
-      for (int h = 0; h < HELD; ++h) {
-        const int q = threadIdx.x + h * threads;
-        long long sum = 0;
-        if (q < N * N) {
-          for (int c = 0; c < part; ++c) sum += *map_to_cta(&pairs[q].x, c);
-          sum = min(sum, (long long)pairs[q].y);
+        for (int c = 0; c < SLOT_MAX_PARTS; ++c)
+          if (c < a.CS) v[c] = *reinterpret_cast<const int4*>(map_to_cta(&pairs[2 * q].x, c));
+        unsigned lo = 0, hi = 0;
+#pragma unroll
+        for (int c = 0; c < SLOT_MAX_PARTS; ++c) {
+          if (c >= a.CS) break;
+          const unsigned more_lo = min(lo + (unsigned)v[c].x, (unsigned)v[c].y), more_hi = min(hi + (unsigned)v[c].z, (unsigned)v[c].w);
+          *reinterpret_cast<int4*>(map_to_cta(&pairs[2 * q].x, c)) = make_int4((int)lo, v[c].y, (int)hi, v[c].w);
+          lo = more_lo, hi = more_hi;
         }
-        held[h] = (int)sum;
       }
       cluster_sync_all();
-#pragma unroll
-      for (int h = 0; h < HELD; ++h) {
-        const int q = threadIdx.x + h * threads;
-        if (q < N * N) pairs[q].x = held[h];
-      }
-      __syncthreads();
-      for (int j = threadIdx.x; j < N; j += threads) {
-        long long sum = 0;
-        for (int i = 0; i < N; ++i) sum += pairs[i * N + j].x;
-        received[j] = sum;
+      for (int q = threadIdx.x; q < N * (threads / N); q += threads) {
+        const int j = q % N, step = threads / N;
+        unsigned long long sum = 0;
+        for (int i = q / N; i < N; i += step) sum += (unsigned)pairs[i * PS + j].x;
+        atomicAdd(reinterpret_cast<unsigned long long*>(received + j), sum);
       }
     }
   }
@@ -187,7 +216,7 @@ __global__ void __launch_bounds__(1024) slots_kernel(const SlotArgs a) {
       walk_sources(k0, true);
     } else {
       for (int q = threadIdx.x; q < held * N; q += threads) {
-        const int kk = q / N, i = q - kk * N;
+        const int kk = slot_row(q, a.per_n), i = q - kk * N;
         const size_t g = (b * a.K + k0) * N + q;
         const int len = a.length[g];
         c_start[kk * IS + i] = a.start[g];
@@ -200,8 +229,26 @@ __global__ void __launch_bounds__(1024) slots_kernel(const SlotArgs a) {
     if constexpr (RECEIVERS) {
       const int k = k0 + lane;
       for (int j = warp; j < N; j += warps) {
-        const int len = c_begins[lane * IS + j], i = c_source[lane * IS + j];
+        const int i = c_source[lane * IS + j];
+        const bool live = k < count && i >= 0;
         bad |= k < count && i < 0;                                 // no source: another receiver has two
+        const int len = live ? c_begins[lane * IS + j] : 0;
+        // the first choices by expert of the pair, on their way while the rows are summed
+        const int32_t* share = a.offsets == nullptr ? nullptr : a.counts + (b * N + (live ? i : 0)) * ((size_t)N * P) + (size_t)j * P;
+        int held_share[4];
+        const auto fetch = [&](int e0) {
+          if (a.quads) {
+            int4 v = make_int4(0, 0, 0, 0);
+            if (live && share != nullptr) v = *reinterpret_cast<const int4*>(share + e0);
+            held_share[0] = v.x, held_share[1] = v.y, held_share[2] = v.z, held_share[3] = v.w;
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) held_share[e] = live && share != nullptr && e0 + e < P ? share[e0 + e] : 0;
+          }
+        };
+        fetch(0);
+        const int pair = !live || share == nullptr ? 0 : SOURCES ? pairs[i * PS + j].y : D[(size_t)i * N + j];
+        const int first = live ? c_start[lane * IS + i] : 0;
         int incl = len;
         bool over = false;                                         // lengths are < 2^31: the sum of 32 may pass that
 #pragma unroll
@@ -209,7 +256,7 @@ __global__ void __launch_bounds__(1024) slots_kernel(const SlotArgs a) {
           const int v = __shfl_up_sync(FULL, incl, o);
           if (lane >= o) {
             over |= incl > 0x7fffffff - v;
-            incl = (int)((unsigned)incl + (unsigned)v) & 0x7fffffff;
+            incl = (int)(((unsigned)incl + (unsigned)v) & 0x7fffffffu);
           }
         }
         const long long run = received[j];
@@ -219,29 +266,35 @@ __global__ void __launch_bounds__(1024) slots_kernel(const SlotArgs a) {
         const int begins = over ? 0 : (int)(run + incl - len);
         __syncwarp();
         if (lane == 0) received[j] = min(run + total, 0x7fffffffLL);
-        c_begins[lane * IS + j] = k < count ? begins : 0;
-        if (a.offsets != nullptr && lane < held) {
-          int32_t* to = a.offsets + (b * N + j) * ((size_t)a.K * P + 1) + (size_t)k * P;
-          if (k < count && i >= 0) {
-            const int32_t* share = a.counts + (b * N + i) * ((size_t)N * P) + (size_t)j * P;
-            const int first = c_start[lane * IS + i];
-            long long ahead = 0;
-            for (int e = 0; e < P; ++e) {
-              to[e] = begins + (int)max(0LL, min(ahead - first, (long long)len));
-              const int v = share[e];
-              bad |= v < 0;
-              ahead += v;
+        c_begins[lane * IS + j] = begins;
+        if (share != nullptr) {
+          int32_t* to = a.offsets + (b * N + j) * ((size_t)a.K * P + 1) + (size_t)k0 * P;
+          long long ahead = 0;
+          for (int e0 = 0; e0 < P; e0 += 4) {
+            if (e0 > 0) fetch(e0);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              if (e0 + e >= P) break;
+              const int v = begins + (int)max(0LL, min(ahead - first, (long long)len));
+              if (P <= SLOT_STAGED_P) staged[lane * P + e0 + e] = v;
+              else if (lane < held) to[lane * P + e0 + e] = v;
+              bad |= held_share[e] < 0;
+              ahead += held_share[e];
             }
-            bad |= ahead != D[(size_t)i * N + j];
-          } else {
-            for (int e = 0; e < P; ++e) to[e] = begins;
+          }
+          bad |= live && ahead != pair;
+          if (P <= SLOT_STAGED_P) {
+            __syncwarp();
+            for (int q = lane; q < held * P; q += 32) to[q] = staged[q];
+            __syncwarp();
           }
         }
       }
       __syncthreads();
     }
+    const unsigned per = sources == N ? a.per_n : sources == SLOT_BLOCK ? a.per_sources : slot_reciprocal(sources);
     for (int q = threadIdx.x; q < held * sources; q += threads) {
-      const int kk = q / sources, i = q - kk * sources;
+      const int kk = slot_row(q, per), i = q - kk * sources;
       const size_t g = (b * a.K + k0 + kk) * N + i0 + i;
       const bool live = k0 + kk < count;
       if constexpr (SOURCES) {
@@ -295,30 +348,45 @@ __global__ void __launch_bounds__(1024) slots_kernel(const SlotArgs a) {
   }
 }
 
+template <bool SOURCES, bool RECEIVERS>
+static cudaError_t launch_slots(const SlotArgs& a, dim3 grid, int warps, size_t smem, cudaStream_t stream) {
+  const auto kern = slots_kernel<SOURCES, RECEIVERS>;
+  if (cudaError_t e = permit_shared_memory(kern, smem); e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(32 * warps);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  if (a.CS > 1) {
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = a.CS;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+  }
+  return cudaLaunchKernelEx(&cfg, kern, a);
+}
+
 cudaError_t run_slots(int B, int N, const int32_t* demand, int K, const uint8_t* perm, const int32_t* dur, const int32_t* count,
                       int P, const int32_t* counts, int32_t* start, int32_t* length, int32_t* row, int32_t* rows,
                       int32_t* offsets, int32_t* status, cudaStream_t stream) {
-  SlotArgs a{N, K, P, 1, demand, perm, dur, count, counts, start, length, row, rows, offsets, status};
-  const int threads = 32 * (N >= 32 ? 32 : N < 4 ? 4 : N);
+  if (offsets == nullptr) P = 0;
+  SlotArgs a{N, K, P, 1, slot_reciprocal(N), slot_reciprocal(SLOT_BLOCK), N % 4 == 0 && (reinterpret_cast<uintptr_t>(perm) & 3) == 0,
+             P % 4 == 0 && (reinterpret_cast<uintptr_t>(counts) & 15) == 0, demand, perm, dur, count, counts, start, length, row, rows,
+             offsets, status};
+  int warps = N >= 16 ? 16 : N < 4 ? 4 : N;
   if (N <= SLOT_FUSED_N) {
-    const auto kern = slots_kernel<true, true>;
-    const size_t smem = slot_smem(N, N, true, N).bytes;
-    if (cudaError_t e = permit_shared_memory(kern, smem); e != cudaSuccess) return e;
-    kern<<<(unsigned)B, threads, smem, stream>>>(a);
-    return cudaGetLastError();
+    while (a.CS < SLOT_MAX_PARTS && (long long)B * a.CS * 2 <= sm_count() && K >= 2 * a.CS * SLOT_CHUNK) a.CS *= 2;
+    if (a.CS > 1 && N >= 32) warps = 32;
+    return launch_slots<true, true>(a, dim3((unsigned)(B * a.CS)), warps, slot_smem(N, N, true, N, warps, slot_staged(P)).bytes, stream);
   }
   cudaError_t e = cudaMemsetAsync(status, 0, (size_t)B * sizeof(int32_t), stream);
   if (e != cudaSuccess) return e;
-  const auto by_source = slots_kernel<true, false>;
-  const auto by_receiver = slots_kernel<false, true>;
-  size_t smem = slot_smem(N, SLOT_BLOCK, true, 0).bytes;
-  if ((e = permit_shared_memory(by_source, smem)) != cudaSuccess) return e;
-  by_source<<<dim3((unsigned)B, (unsigned)((N + SLOT_BLOCK - 1) / SLOT_BLOCK)), threads, smem, stream>>>(a);
-  if ((e = cudaGetLastError()) != cudaSuccess) return e;
-  smem = slot_smem(N, N, false, N).bytes;
-  if ((e = permit_shared_memory(by_receiver, smem)) != cudaSuccess) return e;
-  by_receiver<<<(unsigned)B, threads, smem, stream>>>(a);
-  return cudaGetLastError();
+  e = launch_slots<true, false>(a, dim3((unsigned)B, (unsigned)((N + SLOT_BLOCK - 1) / SLOT_BLOCK)), warps,
+                                slot_smem(N, SLOT_BLOCK, true, 0, warps, 0).bytes, stream);
+  if (e != cudaSuccess) return e;
+  return launch_slots<false, true>(a, dim3((unsigned)B), warps, slot_smem(N, N, false, N, warps, slot_staged(P)).bytes, stream);
 }
 
 }  // namespace moesched
