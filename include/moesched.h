@@ -503,15 +503,16 @@ int moesched_schedule_slots(int B, int N, const int32_t* d_demand, int k_stride,
  *   d_w_gate, d_w_up  in  [E][I][D];  d_w_down  in  [E][D][I];  E <= MOESCHED_MAX_EXPERTS
  *   d_offsets  in   [groups + 1] int32
  *   d_y        out  [R][D]
- *   d_gate, d_up  out  [R][I] a and u, rounded to the type, for the backward pass; both may be NULL
+ *   d_gate, d_up  out  [R][I] float: a and u for the backward pass (in 32 bits: in 16 the gradients of the weights would be
+ *                   half as far again from exact ones); both may be NULL
  *   d_scratch  tmp  moesched_expert_scratch_bytes(R, I, groups, 0) bytes, 256-byte aligned; calls that overlap need their own
  *   d_status   out  [1] int32: OK, or BAD_INPUT where the offsets are not in order or not within 0 .. R: the outputs then
  *                   hold nothing of use
  */
 size_t moesched_expert_scratch_bytes(int R, int I, int groups, int backward);
 int moesched_expert_ffn(int R, int D, int I, int E, int groups, int dtype, int act, const void* d_x, const void* d_w_gate,
-                        const void* d_w_up, const void* d_w_down, const int32_t* d_offsets, void* d_y, void* d_gate,
-                        void* d_up, void* d_scratch, int32_t* d_status, void* stream);
+                        const void* d_w_up, const void* d_w_down, const int32_t* d_offsets, void* d_y, float* d_gate,
+                        float* d_up, void* d_scratch, int32_t* d_status, void* stream);
 
 /*
  * Its backward pass: from dY, the inputs, and a and u as moesched_expert_ffn wrote them
@@ -526,7 +527,7 @@ int moesched_expert_ffn(int R, int D, int I, int E, int groups, int dtype, int a
  */
 int moesched_expert_ffn_backward(int R, int D, int I, int E, int groups, int dtype, int act, const void* d_dy, const void* d_x,
                                  const void* d_w_gate, const void* d_w_up, const void* d_w_down, const int32_t* d_offsets,
-                                 const void* d_gate, const void* d_up, void* d_dx, void* d_dw_gate, void* d_dw_up,
+                                 const float* d_gate, const float* d_up, void* d_dx, void* d_dw_gate, void* d_dw_up,
                                  void* d_dw_down, void* d_scratch, int32_t* d_status, void* stream);
 
 /*

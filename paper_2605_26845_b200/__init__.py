@@ -571,7 +571,7 @@ def expert_ffn(x, w_gate, w_up, w_down, offsets, act="silu", save=False, out=Non
         raise MoeschedError("all tensors must be on one device")
     R, dev = x.shape[0], x.device
     out = _like(out, x, (R, D), "out")
-    saved = {k: torch.empty((R, I), dtype=x.dtype, device=dev) for k in ("gate", "up")} if save else {}
+    saved = {k: torch.empty((R, I), dtype=torch.float32, device=dev) for k in ("gate", "up")} if save else {}
     scratch = _expert_scratch(scratch, x, I, groups, 0)
     _call("moesched_expert_ffn", dev, R, D, I, E, groups, dtype, _act(act), _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(w_down),
           _ptr(offsets), _ptr(out), _ptr(saved.get("gate")), _ptr(saved.get("up")), _ptr(scratch), _ptr(_status_of(status, dev)))
@@ -587,10 +587,12 @@ def expert_ffn_backward(dy, x, w_gate, w_up, w_down, offsets, saved, act="silu",
     R, dev = x.shape[0], x.device
     if offsets.device != dev:
         raise MoeschedError("all tensors must be on one device")
-    for t, shape, what in ((dy, (R, D), "dy"), (saved["gate"], (R, I), "saved['gate']"), (saved["up"], (R, I), "saved['up']")):
-        if t is None:
-            raise MoeschedError(f"{what} is missing")
-        _like(t, x, shape, what)
+    if dy is None:
+        raise MoeschedError("dy is missing")
+    _like(dy, x, (R, D), "dy")
+    for k in ("gate", "up"):
+        if _dev(saved[k], torch.float32, f"saved['{k}']").shape != (R, I) or saved[k].device != dev:
+            raise MoeschedError(f"saved['{k}'] must be [R, I], on the device of x")
     shapes = dict(dx=(R, D), dw_gate=(E, I, D), dw_up=(E, I, D), dw_down=(E, D, I))
     grads = {k: _like(None if out is None else out[k], x, v, k) for k, v in shapes.items()}
     scratch = _expert_scratch(scratch, x, I, groups, 1)

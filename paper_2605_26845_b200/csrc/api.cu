@@ -382,8 +382,8 @@ size_t moesched_expert_scratch_bytes(int R, int I, int groups, int backward) {
 }
 
 int moesched_expert_ffn(int R, int D, int I, int E, int groups, int dtype, int act, const void* d_x, const void* d_w_gate,
-                        const void* d_w_up, const void* d_w_down, const int32_t* d_offsets, void* d_y, void* d_gate,
-                        void* d_up, void* d_scratch, int32_t* d_status, void* stream) {
+                        const void* d_w_up, const void* d_w_down, const int32_t* d_offsets, void* d_y, float* d_gate,
+                        float* d_up, void* d_scratch, int32_t* d_status, void* stream) {
   if (!expert_sizes_ok(R, E, groups, dtype, act) || !ffn_width_ok(D) || !ffn_width_ok(I)) return MOESCHED_EINVAL;
   if ((d_gate == nullptr) != (d_up == nullptr) || !d_offsets || !aligned4(d_offsets) || !d_status || !aligned4(d_status))
     return MOESCHED_EINVAL;
@@ -398,7 +398,7 @@ int moesched_expert_ffn(int R, int D, int I, int E, int groups, int dtype, int a
 
 int moesched_expert_ffn_backward(int R, int D, int I, int E, int groups, int dtype, int act, const void* d_dy, const void* d_x,
                                  const void* d_w_gate, const void* d_w_up, const void* d_w_down, const int32_t* d_offsets,
-                                 const void* d_gate, const void* d_up, void* d_dx, void* d_dw_gate, void* d_dw_up,
+                                 const float* d_gate, const float* d_up, void* d_dx, void* d_dw_gate, void* d_dw_up,
                                  void* d_dw_down, void* d_scratch, int32_t* d_status, void* stream) {
   if (!expert_sizes_ok(R, E, groups, dtype, act) || !ffn_width_ok(D) || !ffn_width_ok(I)) return MOESCHED_EINVAL;
   if (!d_offsets || !aligned4(d_offsets) || !d_status || !aligned4(d_status) || !d_dw_gate || !d_dw_up || !d_dw_down ||

@@ -259,8 +259,8 @@ cudaError_t run_slots(int B, int N, const int32_t* demand, int K, const uint8_t*
 
 // products of a few rows with their experts' weights (few_kernel.cu); group 0: weights in 16 bits
 cudaError_t run_few(int R, int K, int N, int E, int groups, int group, int dtype, int act, const void* x, const void* w,
-                    const void* scale, const void* w_up, const void* scale_up, const int32_t* offsets, void* y, void* sum,
-                    void* sum_up, int32_t* status, cudaStream_t stream);
+                    const void* scale, const void* w_up, const void* scale_up, const int32_t* offsets, void* y, float* sum,
+                    float* sum_up, int32_t* status, cudaStream_t stream);
 
 // gated feed-forward block of the experts (expert_kernel.cu); scratch in bytes from its start
 struct ExpertScratch {
@@ -269,11 +269,11 @@ struct ExpertScratch {
 ExpertScratch expert_scratch(int R, int I, int groups, bool backward);
 constexpr int EXPERT_FEW_ROWS = 64;
 cudaError_t run_expert_ffn(int R, int D, int I, int E, int groups, int dtype, int act, const void* x, const void* w_gate,
-                           const void* w_up, const void* w_down, const int32_t* offsets, void* y, void* gate, void* up,
+                           const void* w_up, const void* w_down, const int32_t* offsets, void* y, float* gate, float* up,
                            void* scratch, int32_t* status, cudaStream_t stream);
 cudaError_t run_expert_backward(int R, int D, int I, int E, int groups, int dtype, int act, const void* dy, const void* x,
                                 const void* w_gate, const void* w_up, const void* w_down, const int32_t* offsets,
-                                const void* gate, const void* up, void* dx, void* dw_gate, void* dw_up, void* dw_down,
+                                const float* gate, const float* up, void* dx, void* dw_gate, void* dw_up, void* dw_down,
                                 void* scratch, int32_t* status, cudaStream_t stream);
 
 // All of an SM's memory that can be shared memory is, while the kernel runs there. (A preference: failing is harmless.)

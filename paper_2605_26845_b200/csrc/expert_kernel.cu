@@ -7,10 +7,13 @@
 //   DINPUT   dX = da Wg + du Wu                        (one contraction over 2 I)
 //   DWEIGHT  dWg = da^T X, dWu = du^T X, dWd = dY^T h  (contractions over the rows of an expert)
 //
-// A persistent CTA per SM takes tiles of 128 x 256 (GLU: 128 columns of a and the same 128 of u). One warp fetches the operands with TMA,
-// 64 deep, into a ring of stages; one thread issues the matrix instructions, whose sums are in tensor memory, twice, so that four
-// warps empty one while the other fills. Operands stay as they are in memory: where the contraction runs over
-// the slower axis (Wd in DHIDDEN, Wg and Wu in DINPUT, everything in DWEIGHT) the instruction takes them transposed.
+// Persistent CTAs take tiles of 128 x 128 (GLU: 64 columns of a and the same 64 of u), or pairs of CTAs on two SMs tiles of
+// 256 x 256, each with half of the rows of either operand: every byte that a pair fetches serves twice as many products. One warp fetches
+// the operands with TMA, 64 deep, into a ring of stages; one thread (of a pair: of its first CTA) issues the matrix instructions, whose
+// sums are in tensor memory, twice, so that four warps empty one while the other fills; those warps turn what they
+// read by way of shared memory, so that neighbouring lanes load and store neighbouring columns. Operands stay as they are in memory:
+// where the contraction runs over the slower axis (Wd in DHIDDEN, Wg and Wu in DINPUT, everything in DWEIGHT) the instruction
+// takes them transposed.
 // Row tiles of the groups are laid out by a small kernel first (plan_kernel): a tile never spans two groups, what lies behind its
 // group's last row is computed and not stored. In DWEIGHT the rows are the contraction: there the rows behind
 // a group's last, up to the next multiple of 16, are zeroed in shared memory (0 x NaN would not be nothing).
@@ -22,12 +25,13 @@ namespace moesched {
 
 enum { GLU, DOWN, DHIDDEN, DINPUT, DWEIGHT };
 
-constexpr int BM = 128, BN = 256, BK = 64;
-constexpr int STAGES = 4;
-constexpr int A_BYTES = BM * BK * 2, B_BYTES = BN * BK * 2, STAGE_BYTES = A_BYTES + B_BYTES;
+constexpr int CTA_M = 128, CTA_N = 128, BK = 64;           // rows of the operands that a CTA fetches, and how deep
+constexpr int STAGES = 6;
+constexpr int A_BYTES = CTA_M * BK * 2, B_BYTES = CTA_N * BK * 2, STAGE_BYTES = A_BYTES + B_BYTES;
 constexpr int GEMM_THREADS = 256;
-constexpr int MAP_BOX_BYTES = 64 * 64 * 2;                 // one box of a transposed operand
-constexpr int RASTER = 16;                                 // row tiles that share a pass over the columns
+constexpr int BOX_BYTES = 64 * 64 * 2;                     // one box of B, and of a transposed A
+constexpr int TURN_BYTES = 2 * 32 * 16 * 4;                // of a warp that empties tensor memory
+constexpr int RASTER_ROWS = 2048;                          // rows of row tiles that share a pass over the columns
 
 struct alignas(64) GemmArgs {
   CUtensorMap a[3], b[3];
@@ -35,7 +39,8 @@ struct alignas(64) GemmArgs {
   const int32_t* offsets;
   int R, D, I, E, groups;
   void* out[3];
-  const void* in[2];
+  const float* in[2];                                      // a and u of the forward pass
+  float* keep[2];                                          // and where it leaves them, or NULL
   int32_t* status;
 };
 
@@ -62,16 +67,48 @@ __device__ __forceinline__ bool barrier_wait(unsigned bar, unsigned parity, vola
   *failed = 1;
   return false;
 }
+// the address of `local` in CTA `rank` of the cluster
+__device__ __forceinline__ unsigned in_cta(unsigned local, unsigned rank) {
+  unsigned out;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(out) : "r"(local), "r"(rank));
+  return out;
+}
+__device__ __forceinline__ void barrier_arrive_in(unsigned remote) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(remote) : "memory");
+}
 __device__ __forceinline__ void tma_load(unsigned dst, const CUtensorMap* map, unsigned bar, int x, int y, int z) {
   asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
                ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
 }
-__device__ __forceinline__ void mma_issue(unsigned d, unsigned long long a, unsigned long long b, unsigned idesc, bool add) {
-  asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
-               ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((unsigned)add) : "memory");
+// into this CTA, counted on a barrier that may be the other CTA's of the pair
+__device__ __forceinline__ void tma_load_pair(unsigned dst, const CUtensorMap* map, unsigned bar, int x, int y, int z) {
+  asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+               ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
 }
+template <bool PAIR>
+__device__ __forceinline__ void mma_issue(unsigned d, unsigned long long a, unsigned long long b, unsigned idesc, bool add) {
+  if constexpr (PAIR)
+    asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((unsigned)add) : "memory");
+  else
+    asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((unsigned)add) : "memory");
+}
+// an arrival at the barrier (of a pair: of both CTAs) when the matrix instructions issued so far are done
+template <bool PAIR>
 __device__ __forceinline__ void mma_commit(unsigned bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+  if constexpr (PAIR)
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                 ::"r"(bar), "h"((unsigned short)3) : "memory");
+  else
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tmem_load16(unsigned addr, float (&v)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]),
+        "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
+      : "r"(addr));
 }
 __device__ __forceinline__ void tmem_load32(unsigned addr, float (&v)[32]) {
   asm volatile(
@@ -91,14 +128,14 @@ __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::aft
 // Transposed (a row of 128 bytes holds 64 rows or columns of the result at one k): 8 k are 1024 bytes, the next 64 rows or
 // columns of the result one box further on.
 __device__ __forceinline__ unsigned long long operand(unsigned addr, bool transposed) {
-  const unsigned long long lead = transposed ? MAP_BOX_BYTES >> 4 : 1;
+  const unsigned long long lead = transposed ? BOX_BYTES >> 4 : 1;
   return (unsigned long long)((addr >> 4) & 0x3fff) | lead << 16 | (1024ull >> 4) << 32 | 1ull << 46 | 2ull << 61;
 }
 
 // ---- row tiles ------------------------------------------------------------------------------------------
 
-// Tiles of up to 128 rows of the groups, by expert, so that tiles with the same weights follow one another. One CTA.
-__global__ void __launch_bounds__(1024) plan_kernel(int R, int E, int groups, const int32_t* __restrict__ offsets,
+// Tiles of up to `high` rows of the groups, by expert, so that tiles with the same weights follow one another. One CTA.
+__global__ void __launch_bounds__(1024) plan_kernel(int R, int E, int groups, int high, const int32_t* __restrict__ offsets,
                                                     int4* __restrict__ plan, int32_t* __restrict__ status) {
   __shared__ int warp_sum[32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, per = groups / E;
@@ -112,7 +149,7 @@ __global__ void __launch_bounds__(1024) plan_kernel(int R, int E, int groups, co
   for (int q0 = 0; q0 < groups && !bad; q0 += 1024) {
     const int q = q0 + threadIdx.x, e = q / per;
     const int2 span = q < groups ? rows_of_group(offsets, (q - e * per) * E + e, R) : make_int2(0, 0);
-    const int tiles = (span.y - span.x + BM - 1) / BM;
+    const int tiles = (span.y - span.x + high - 1) / high;
     int incl = tiles;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -127,7 +164,7 @@ __global__ void __launch_bounds__(1024) plan_kernel(int R, int E, int groups, co
       all += warp_sum[w];
     }
     for (int i = 0; i < tiles; ++i)
-      plan[1 + before + incl - tiles + i] = make_int4(span.x + i * BM, min(BM, span.y - span.x - i * BM), e, 0);
+      plan[1 + before + incl - tiles + i] = make_int4(span.x + i * high, min(high, span.y - span.x - i * high), e, 0);
     base = all;
     __syncthreads();
   }
@@ -140,41 +177,48 @@ __global__ void __launch_bounds__(1024) plan_kernel(int R, int E, int groups, co
 // ---- the products ---------------------------------------------------------------------------------------
 
 struct Tile {
-  int row, rows, e, n;      // rows of the result, expert, first column
+  int row, rows, e, n;      // first row of the result and rows, expert, first column
   int which;                // DWEIGHT: 0 gate, 1 up, 2 down
 };
+// a tile of MODE is M rows high and N columns wide; GLU's are made of as many products again
+template <int MODE, bool PAIR>
+struct Shape {
+  static constexpr int M = PAIR ? 2 * CTA_M : CTA_M, SUMS = PAIR ? 2 * CTA_N : CTA_N, N = MODE == GLU ? SUMS / 2 : SUMS;
+};
+__host__ __device__ constexpr long long div_up(long long a, long long b) { return (a + b - 1) / b; }
 
-template <int MODE>
+template <int MODE, bool PAIR>
 __device__ __forceinline__ int tile_total(const GemmArgs& a, const int4 head) {
+  using S = Shape<MODE, PAIR>;
   if constexpr (MODE == DWEIGHT) {
-    const int gu = ((a.I + BM - 1) / BM) * ((a.D + BN - 1) / BN), dn = ((a.D + BM - 1) / BM) * ((a.I + BN - 1) / BN);
+    const int gu = (int)(div_up(a.I, S::M) * div_up(a.D, S::N)), dn = (int)(div_up(a.D, S::M) * div_up(a.I, S::N));
     return head.y ? a.E * (2 * gu + dn) : 0;
   } else {
-    const int cols = MODE == GLU || MODE == DHIDDEN ? a.I : a.D, wide = MODE == GLU ? BN / 2 : BN;
-    return head.x * ((cols + wide - 1) / wide);
+    return head.x * (int)div_up(MODE == GLU || MODE == DHIDDEN ? a.I : a.D, S::N);
   }
 }
-template <int MODE>
+template <int MODE, bool PAIR>
 __device__ __forceinline__ Tile tile_at(const GemmArgs& a, const int4 head, int t) {
+  using S = Shape<MODE, PAIR>;
   Tile w;
   if constexpr (MODE == DWEIGHT) {
-    const int gu = ((a.I + BM - 1) / BM) * ((a.D + BN - 1) / BN), dn = ((a.D + BM - 1) / BM) * ((a.I + BN - 1) / BN);
+    const int gu = (int)(div_up(a.I, S::M) * div_up(a.D, S::N)), dn = (int)(div_up(a.D, S::M) * div_up(a.I, S::N));
     const int each = 2 * gu + dn;
     w.e = t / each;
     t -= w.e * each;
     w.which = t < gu ? 0 : t < 2 * gu ? 1 : 2;
     t -= w.which * gu;
-    const int M = w.which < 2 ? a.I : a.D, m_tiles = (M + BM - 1) / BM;
-    w.row = t % m_tiles * BM;
-    w.rows = min(BM, M - w.row);
-    w.n = t / m_tiles * BN;
+    const int M = w.which < 2 ? a.I : a.D, m_tiles = (int)div_up(M, S::M);
+    w.row = t % m_tiles * S::M;
+    w.rows = min(S::M, M - w.row);
+    w.n = t / m_tiles * S::N;
   } else {
-    const int cols = MODE == GLU || MODE == DHIDDEN ? a.I : a.D, wide = MODE == GLU ? BN / 2 : BN;
-    const int n_tiles = (cols + wide - 1) / wide;
+    constexpr int RASTER = RASTER_ROWS / S::M;
+    const int n_tiles = (int)div_up(MODE == GLU || MODE == DHIDDEN ? a.I : a.D, S::N);
     const int block = t / (RASTER * n_tiles), first = block * RASTER, high = min(RASTER, head.x - first);
     t -= first * n_tiles;
     const int4 row = a.plan[1 + first + t % high];
-    w.row = row.x, w.rows = row.y, w.e = row.z, w.n = t / high * wide, w.which = 0;
+    w.row = row.x, w.rows = row.y, w.e = row.z, w.n = t / high * S::N, w.which = 0;
   }
   return w;
 }
@@ -196,69 +240,99 @@ __device__ __forceinline__ bool each_block(const GemmArgs& a, const Tile& w, F&&
   return true;
 }
 
-template <int MODE, typename T, int ACT>
+// place of the four words `part` of row `row` in a warp's 32 x 16 words: rows that lanes store and rows that they load together
+// lie in different banks
+__device__ __forceinline__ float4* turned(float* base, int row, int part) {
+  return reinterpret_cast<float4*>(base + row * 16 + ((part ^ (row >> 1 & 3)) << 2));
+}
+
+template <int MODE, bool PAIR, typename T, int ACT>
 __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_constant__ GemmArgs a) {
+  using S = Shape<MODE, PAIR>;
   constexpr bool A_T = MODE == DWEIGHT, B_T = MODE == DHIDDEN || MODE == DINPUT || MODE == DWEIGHT;
+  constexpr int TMEM_COLUMNS = 2 * S::SUMS;
   extern __shared__ unsigned char raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
-  unsigned long long* bars = reinterpret_cast<unsigned long long*>(smem + STAGES * STAGE_BYTES);
+  unsigned long long* bars = reinterpret_cast<unsigned long long*>(smem + STAGES * STAGE_BYTES + 4 * TURN_BYTES);
   const unsigned ring = smem_addr(smem);
-  const unsigned full = smem_addr(bars), empty = full + 8 * STAGES, fixed = empty + 8 * STAGES, done = fixed + 8 * STAGES,
-                 free_ = done + 16, drain = free_ + 16;
-  int* words = reinterpret_cast<int*>(bars + 3 * STAGES + 5);
+  // full, done: operands there, sums there; empty, free_: may be overwritten; partly, fixed: blocks that end within (DWEIGHT)
+  const unsigned full = smem_addr(bars), empty = full + 8 * STAGES, partly = empty + 8 * STAGES, fixed = partly + 8 * STAGES,
+                 done = fixed + 8 * STAGES, free_ = done + 16, drain = free_ + 16;
+  int* words = reinterpret_cast<int*>(bars + 4 * STAGES + 5);
   volatile int* failed = words;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const unsigned rank = PAIR ? cluster_ctarank() : 0;      // the first CTA of a pair issues
+  const int first_tile = PAIR ? blockIdx.x / 2 : blockIdx.x, step = PAIR ? gridDim.x / 2 : gridDim.x;
 
   if (threadIdx.x == 0) {
     *failed = 0;
     for (int s = 0; s < STAGES; ++s) {
       barrier_init(full + 8 * s, 1);
       barrier_init(empty + 8 * s, 1);
-      barrier_init(fixed + 8 * s, 1);
+      barrier_init(partly + 8 * s, 1);
+      barrier_init(fixed + 8 * s, PAIR ? 2 : 1);
     }
     for (int q = 0; q < 2; ++q) {
       barrier_init(done + 8 * q, 1);
-      barrier_init(free_ + 8 * q, 4);
+      barrier_init(free_ + 8 * q, PAIR ? 8 : 4);
     }
     barrier_init(drain, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(words + 1)) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    if constexpr (PAIR) {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(words + 1)), "n"(TMEM_COLUMNS) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(words + 1)), "n"(TMEM_COLUMNS) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
   }
   fence_before();
   __syncthreads();
+  if constexpr (PAIR) cluster_sync_all();                  // the other CTA's barriers are there
   fence_after();
   const unsigned tmem = *reinterpret_cast<volatile unsigned*>(words + 1);
   const int4 head = a.plan[0];
-  const int total = tile_total<MODE>(a, head);
+  const int total = tile_total<MODE, PAIR>(a, head);
 
   if (warp == 0) {
     if (lane == 0) {
       int stage = 0, issued = 0;
       unsigned phase = 0;
       bool ok = true;
-      for (int t = blockIdx.x; t < total && ok; t += gridDim.x) {
-        const Tile w = tile_at<MODE>(a, head, t);
-        ok = each_block<MODE>(a, w, [&](int k, int, int part) {
+      const unsigned lead_full = PAIR ? in_cta(full, 0) : full;
+      for (int t = first_tile; t < total && ok; t += step) {
+        const Tile w = tile_at<MODE, PAIR>(a, head, t);
+        const int row = w.row + (int)rank * CTA_M;
+        ok = each_block<MODE>(a, w, [&](int k, int held, int part) {
           if (!barrier_wait(empty + 8 * stage, phase ^ 1, failed)) return false;
-          const unsigned bar = full + 8 * stage, to = ring + stage * STAGE_BYTES, tb = to + A_BYTES;
-          barrier_expect(bar, STAGE_BYTES);
+          const unsigned to = ring + stage * STAGE_BYTES, tb = to + A_BYTES;
+          // a block that ends within is counted by each CTA for itself, for the warp that zeroes its end
+          const bool own = MODE == DWEIGHT && held < BK;
+          const unsigned bar = own ? partly + 8 * stage : lead_full + 8 * stage;
+          if (own) barrier_expect(bar, STAGE_BYTES);
+          else if (rank == 0) barrier_expect(full + 8 * stage, (PAIR ? 2 : 1) * STAGE_BYTES);
+          const auto load = [&](unsigned dst, const CUtensorMap* map, int x, int y, int z) {
+            if (PAIR && !own) tma_load_pair(dst, map, bar, x, y, z);
+            else tma_load(dst, map, bar, x, y, z);
+          };
           if constexpr (A_T) {
-            for (int q = 0; q < 2; ++q) tma_load(to + q * MAP_BOX_BYTES, &a.a[part], bar, w.row + 64 * q, k, 0);
+            for (int q = 0; q < 2; ++q) load(to + q * BOX_BYTES, &a.a[part], row + 64 * q, k, 0);
           } else {
-            tma_load(to, &a.a[MODE == DINPUT ? part : 0], bar, k, w.row, 0);
+            load(to, &a.a[MODE == DINPUT ? part : 0], k, row, 0);
           }
-          if constexpr (MODE == GLU) {
-            tma_load(tb, &a.b[0], bar, k, w.n, w.e);
-            tma_load(tb + B_BYTES / 2, &a.b[1], bar, k, w.n, w.e);
-          } else if constexpr (MODE == DOWN) {
-            tma_load(tb, &a.b[0], bar, k, w.n, w.e);
-            tma_load(tb + B_BYTES / 2, &a.b[0], bar, k, w.n + 128, w.e);
-          } else {
-            for (int q = 0; q < 4; ++q)
-              tma_load(tb + q * MAP_BOX_BYTES, &a.b[MODE == DHIDDEN ? 0 : part], bar, w.n + 64 * q, k, MODE == DWEIGHT ? 0 : w.e);
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            const unsigned dst = tb + q * BOX_BYTES;
+            if constexpr (MODE == GLU) {                   // a pair: a of the first CTA, u of the second
+              if constexpr (PAIR) load(dst, &a.b[rank], k, w.n + 64 * q, w.e);
+              else load(dst, &a.b[q], k, w.n, w.e);
+            } else {
+              const int n = w.n + (int)rank * CTA_N + 64 * q;
+              if constexpr (MODE == DOWN) load(dst, &a.b[0], k, n, w.e);
+              else load(dst, &a.b[MODE == DHIDDEN ? 0 : part], n, k, MODE == DWEIGHT ? 0 : w.e);
+            }
           }
           ++issued;
           if (++stage == STAGES) stage = 0, phase ^= 1;
@@ -266,31 +340,30 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
         });
       }
       if (!ok) {                                            // nothing may land in shared memory that is no longer ours
-        for (int q = max(0, issued - STAGES); q < issued; ++q) {
-          int never = 0;
-          barrier_wait(full + 8 * (q % STAGES), q / STAGES & 1, &never);
-        }
+        const long long now = clock64();
+        while (clock64() - now < 10'000'000) __nanosleep(1000);
       }
     }
   } else if (warp == 1) {
-    if (lane == 0) {
+    if (lane == 0 && rank == 0) {
       constexpr unsigned FORMAT = std::is_same_v<T, __half> ? 0 : 1;
       constexpr unsigned IDESC = 1u << 4 | FORMAT << 7 | FORMAT << 10 | (A_T ? 1u : 0u) << 15 | (B_T ? 1u : 0u) << 16 |
-                                 (BN / 8) << 17 | (BM / 16) << 24;
+                                 (S::SUMS / 8) << 17 | (S::M / 16) << 24;
       int stage = 0, slot = 0;
-      unsigned phase = 0, slot_phase = 0, fixed_phase = 0;
+      unsigned phase = 0, slot_phase = 0, fixed_phase = 0, full_phase = 0;
       bool ok = true;
-      for (int t = blockIdx.x; t < total && ok; t += gridDim.x) {
-        const Tile w = tile_at<MODE>(a, head, t);
+      for (int t = first_tile; t < total && ok; t += step) {
+        const Tile w = tile_at<MODE, PAIR>(a, head, t);
         bool first = true;
-        const unsigned d = tmem + slot * BN;
+        const unsigned d = tmem + slot * S::SUMS;
         ok = each_block<MODE>(a, w, [&](int, int held, int) {
           if (first && !barrier_wait(free_ + 8 * slot, slot_phase ^ 1, failed)) return false;
           if (MODE == DWEIGHT && held < BK) {
             if (!barrier_wait(fixed + 8 * stage, fixed_phase >> stage & 1, failed)) return false;
             fixed_phase ^= 1u << stage;
-          } else if (!barrier_wait(full + 8 * stage, phase, failed)) {
-            return false;
+          } else {                                          // (blocks that end within pass `full` by)
+            if (!barrier_wait(full + 8 * stage, MODE == DWEIGHT ? full_phase >> stage & 1 : phase, failed)) return false;
+            full_phase ^= 1u << stage;
           }
           fence_after();
           const unsigned at = ring + stage * STAGE_BYTES;
@@ -298,20 +371,20 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
           const int steps = MODE == DWEIGHT ? (held + 15) / 16 : BK / 16;
           for (int s = 0; s < steps; ++s) {
             // 16 k: 32 bytes of a row, or 16 rows of 128 bytes
-            mma_issue(d, da + s * (A_T ? 2048 >> 4 : 32 >> 4), db + s * (B_T ? 2048 >> 4 : 32 >> 4), IDESC, !first || s > 0);
+            mma_issue<PAIR>(d, da + s * (A_T ? 2048 >> 4 : 32 >> 4), db + s * (B_T ? 2048 >> 4 : 32 >> 4), IDESC, !first || s > 0);
           }
           first = false;
-          mma_commit(empty + 8 * stage);
+          mma_commit<PAIR>(empty + 8 * stage);
           if (++stage == STAGES) stage = 0, phase ^= 1;
           return true;
         });
         if (!first) {
-          mma_commit(done + 8 * slot);
+          mma_commit<PAIR>(done + 8 * slot);
           if (++slot == 2) slot = 0, slot_phase ^= 1;
         }
       }
       if (!ok) {
-        mma_commit(drain);
+        mma_commit<PAIR>(drain);
         int never = 0;
         barrier_wait(drain, 0, &never);
       }
@@ -319,121 +392,182 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
   } else if (warp == 2) {
     if constexpr (MODE == DWEIGHT) {                        // zeroes what a block holds behind its group's last row
       int stage = 0;
-      unsigned phase = 0;
+      unsigned part_phase = 0;
       bool ok = true;
-      for (int t = blockIdx.x; t < total && ok; t += gridDim.x) {
-        const Tile w = tile_at<MODE>(a, head, t);
+      const unsigned lead_fixed = PAIR ? in_cta(fixed, 0) : fixed;
+      for (int t = first_tile; t < total && ok; t += step) {
+        const Tile w = tile_at<MODE, PAIR>(a, head, t);
         ok = each_block<MODE>(a, w, [&](int, int held, int) {
-          // (every block is waited for: a parity says nothing about a phase that is two ahead)
-          if (!__all_sync(FULL, barrier_wait(full + 8 * stage, phase, failed))) return false;
           if (held < BK) {
+            if (!__all_sync(FULL, barrier_wait(partly + 8 * stage, part_phase >> stage & 1, failed))) return false;
+            part_phase ^= 1u << stage;
             const int to = (held + 15) / 16 * 16, bytes16 = (to - held) * 8;
-            for (int q = lane; q < 6 * bytes16; q += 32) {
+            for (int q = lane; q < 4 * bytes16; q += 32) {
               const int box = q / bytes16, at = q - box * bytes16;
-              *reinterpret_cast<uint4*>(smem + stage * STAGE_BYTES + box * MAP_BOX_BYTES + held * 128 + at * 16) = make_uint4(0, 0, 0, 0);
+              *reinterpret_cast<uint4*>(smem + stage * STAGE_BYTES + box * BOX_BYTES + held * 128 + at * 16) = make_uint4(0, 0, 0, 0);
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
-            if (lane == 0) barrier_arrive(fixed + 8 * stage);
+            if (lane == 0) {
+              if constexpr (PAIR) barrier_arrive_in(lead_fixed + 8 * stage);
+              else barrier_arrive(fixed + 8 * stage);
+            }
           }
-          if (++stage == STAGES) stage = 0, phase ^= 1;
+          if (++stage == STAGES) stage = 0;
           return true;
         });
       }
     }
   } else if (warp >= 4) {
-    const int quarter = warp - 4, row = quarter * 32 + lane;
+    const int quarter = warp - 4;
     const unsigned mine = tmem + ((unsigned)quarter << 21);
+    const unsigned lead_free = PAIR ? in_cta(free_, 0) : free_;
+    float* turn = reinterpret_cast<float*>(smem + STAGES * STAGE_BYTES + quarter * TURN_BYTES);
+    // after the turn a lane has, in round q, four words of row 8 q + lane / 4
+    const int t_row = lane >> 2, t_part = lane & 3;
     int slot = 0;
     unsigned slot_phase = 0;
-    for (int t = blockIdx.x; t < total; t += gridDim.x) {
-      const Tile w = tile_at<MODE>(a, head, t);
+    for (int t = first_tile; t < total; t += step) {
+      const Tile w = tile_at<MODE, PAIR>(a, head, t);
+      const int row = w.row + (int)rank * CTA_M + quarter * 32 + t_row;       // of round 0
+      const int rows = w.rows - ((int)rank * CTA_M + quarter * 32 + t_row);  // round q is inside if 8 q < rows
+      const unsigned d = mine + slot * S::SUMS;
       bool any = true;
       if constexpr (MODE == DWEIGHT) {
         any = false;
         each_block<MODE>(a, w, [&](int, int, int) { any = true; return false; });
       }
-      if (any) {
-        if (!__all_sync(FULL, barrier_wait(done + 8 * slot, slot_phase, failed))) break;
+      const auto wait_sums = [&]() {
+        if (!__all_sync(FULL, barrier_wait(done + 8 * slot, slot_phase, failed))) return false;
         fence_after();
-      }
-      const unsigned d = mine + slot * BN;
-      const bool in = row < w.rows;
-      if constexpr (MODE == GLU || MODE == DHIDDEN) {
-        const size_t at = (size_t)(w.row + row) * a.I + w.n;
-        constexpr int COLS = MODE == GLU ? BN / 2 : BN;
+        return true;
+      };
+      if constexpr (MODE == GLU) {
+        if (!wait_sums()) break;
+        const size_t at = (size_t)row * a.I + w.n + 4 * t_part;
 #pragma unroll 1
-        for (int c = 0; c < COLS; c += 32) {
-          float p[32], q[32];
-          tmem_load32(d + c, p);
-          if constexpr (MODE == GLU) tmem_load32(d + COLS + c, q);
+        for (int c = 0; c < S::N; c += 16) {
+          float p[16], q[16];
+          tmem_load16(d + c, p);
+          tmem_load16(d + S::N + c, q);
           tmem_load_wait();
+          __syncwarp();
 #pragma unroll
-          for (int s = 0; s < 32; s += 8) {
-            if (!in || w.n + c + s >= a.I) continue;
-            if constexpr (MODE == GLU) {
-              unsigned h[4], g[4], u[4];
+          for (int v = 0; v < 4; ++v) {
+            *turned(turn, lane, v) = make_float4(p[4 * v], p[4 * v + 1], p[4 * v + 2], p[4 * v + 3]);
+            *turned(turn + 512, lane, v) = make_float4(q[4 * v], q[4 * v + 1], q[4 * v + 2], q[4 * v + 3]);
+          }
+          __syncwarp();
+          if (w.n + c + 4 * t_part < a.I) {
 #pragma unroll
-              for (int v = 0; v < 4; ++v) {
-                const int i = s + 2 * v;
-                h[v] = Pair<T>::from_float(activation<ACT>(p[i]) * q[i], activation<ACT>(p[i + 1]) * q[i + 1]);
-                g[v] = Pair<T>::from_float(p[i], p[i + 1]);
-                u[v] = Pair<T>::from_float(q[i], q[i + 1]);
+            for (int v = 0; v < 4; ++v) {
+              if (8 * v >= rows) continue;
+              const float4 g = *turned(turn, 8 * v + t_row, t_part), u = *turned(turn + 512, 8 * v + t_row, t_part);
+              const size_t to = at + (size_t)(8 * v) * a.I + c;
+              *reinterpret_cast<uint2*>(static_cast<T*>(a.out[0]) + to) =
+                  make_uint2(Pair<T>::from_float(activation<ACT>(g.x) * u.x, activation<ACT>(g.y) * u.y),
+                             Pair<T>::from_float(activation<ACT>(g.z) * u.z, activation<ACT>(g.w) * u.w));
+              if (a.keep[0] != nullptr) {
+                *reinterpret_cast<float4*>(a.keep[0] + to) = g;
+                *reinterpret_cast<float4*>(a.keep[1] + to) = u;
               }
-              *reinterpret_cast<uint4*>(static_cast<T*>(a.out[0]) + at + c + s) = make_uint4(h[0], h[1], h[2], h[3]);
-              if (a.out[1] != nullptr) {
-                *reinterpret_cast<uint4*>(static_cast<T*>(a.out[1]) + at + c + s) = make_uint4(g[0], g[1], g[2], g[3]);
-                *reinterpret_cast<uint4*>(static_cast<T*>(a.out[2]) + at + c + s) = make_uint4(u[0], u[1], u[2], u[3]);
-              }
-            } else {
-              const uint4 gv = *reinterpret_cast<const uint4*>(static_cast<const T*>(a.in[0]) + at + c + s);
-              const uint4 uv = *reinterpret_cast<const uint4*>(static_cast<const T*>(a.in[1]) + at + c + s);
-              const unsigned gw[4] = {gv.x, gv.y, gv.z, gv.w}, uw[4] = {uv.x, uv.y, uv.z, uv.w};
-              unsigned h[4], g[4], u[4];
-#pragma unroll
-              for (int v = 0; v < 4; ++v) {
-                const float2 gate = Pair<T>::to_float(gw[v]), up = Pair<T>::to_float(uw[v]);
-                const float x0 = p[s + 2 * v], x1 = p[s + 2 * v + 1];
-                float f0, s0, f1, s1;
-                activation_slope<ACT>(gate.x, f0, s0);
-                activation_slope<ACT>(gate.y, f1, s1);
-                h[v] = Pair<T>::from_float(f0 * up.x, f1 * up.y);
-                g[v] = Pair<T>::from_float(x0 * up.x * s0, x1 * up.y * s1);
-                u[v] = Pair<T>::from_float(x0 * f0, x1 * f1);
-              }
-              *reinterpret_cast<uint4*>(static_cast<T*>(a.out[0]) + at + c + s) = make_uint4(h[0], h[1], h[2], h[3]);
-              *reinterpret_cast<uint4*>(static_cast<T*>(a.out[1]) + at + c + s) = make_uint4(g[0], g[1], g[2], g[3]);
-              *reinterpret_cast<uint4*>(static_cast<T*>(a.out[2]) + at + c + s) = make_uint4(u[0], u[1], u[2], u[3]);
             }
           }
         }
-      } else {
-        const int cols = MODE == DWEIGHT && w.which == 2 ? a.I : a.D;
-        const size_t first = MODE == DWEIGHT ? (size_t)w.e * a.I * a.D + (size_t)(w.row + row) * cols : (size_t)(w.row + row) * cols;
-        T* out = static_cast<T*>(a.out[MODE == DWEIGHT ? w.which : 0]) + first + w.n;
+      } else if constexpr (MODE == DHIDDEN) {
+        const size_t at = (size_t)row * a.I + w.n + 4 * t_part;
+        struct Held {
+          float4 g[4], u[4];
+        };
+        const auto fetch = [&](int c, Held& h) {           // a and u of 16 columns, on their way while others are worked on
+          const bool in = c < S::N && w.n + c + 4 * t_part < a.I;
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            const size_t from = at + (size_t)(8 * v) * a.I + c;
+            h.g[v] = h.u[v] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            if (in && 8 * v < rows) {
+              h.g[v] = __ldcs(reinterpret_cast<const float4*>(a.in[0] + from));
+              h.u[v] = __ldcs(reinterpret_cast<const float4*>(a.in[1] + from));
+            }
+          }
+        };
+        const auto work = [&](int c, const Held& h) {
+          float p[16];
+          tmem_load16(d + c, p);
+          tmem_load_wait();
+          __syncwarp();
+#pragma unroll
+          for (int v = 0; v < 4; ++v) *turned(turn, lane, v) = make_float4(p[4 * v], p[4 * v + 1], p[4 * v + 2], p[4 * v + 3]);
+          __syncwarp();
+          if (w.n + c + 4 * t_part >= a.I) return;
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            if (8 * v >= rows) continue;
+            const float4 x = *turned(turn, 8 * v + t_row, t_part);
+            const float xs[4] = {x.x, x.y, x.z, x.w}, gs[4] = {h.g[v].x, h.g[v].y, h.g[v].z, h.g[v].w},
+                        us[4] = {h.u[v].x, h.u[v].y, h.u[v].z, h.u[v].w};
+            float hid[4], dg[4], du[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              float f, s;
+              activation_slope<ACT>(gs[i], f, s);
+              hid[i] = f * us[i], dg[i] = xs[i] * us[i] * s, du[i] = xs[i] * f;
+            }
+            const size_t to = at + (size_t)(8 * v) * a.I + c;
+            *reinterpret_cast<uint2*>(static_cast<T*>(a.out[0]) + to) = make_uint2(Pair<T>::from_float(hid[0], hid[1]), Pair<T>::from_float(hid[2], hid[3]));
+            *reinterpret_cast<uint2*>(static_cast<T*>(a.out[1]) + to) = make_uint2(Pair<T>::from_float(dg[0], dg[1]), Pair<T>::from_float(dg[2], dg[3]));
+            *reinterpret_cast<uint2*>(static_cast<T*>(a.out[2]) + to) = make_uint2(Pair<T>::from_float(du[0], du[1]), Pair<T>::from_float(du[2], du[3]));
+          }
+        };
+        Held even, odd;
+        fetch(0, even);
+        if (!wait_sums()) break;
 #pragma unroll 1
-        for (int c = 0; c < BN; c += 32) {
-          float p[32];
+        for (int c = 0; c < S::N; c += 32) {
+          fetch(c + 16, odd);
+          work(c, even);
+          fetch(c + 32, even);
+          work(c + 16, odd);
+        }
+      } else {
+        if (any && !wait_sums()) break;
+        const int cols = MODE == DWEIGHT && w.which == 2 ? a.I : a.D;
+        const size_t first = MODE == DWEIGHT ? (size_t)w.e * a.I * a.D + (size_t)row * cols : (size_t)row * cols;
+        T* out = static_cast<T*>(a.out[MODE == DWEIGHT ? w.which : 0]) + first + w.n + 8 * t_part;
+#pragma unroll 1
+        for (int c = 0; c < S::N; c += 32) {
           if (any) {
+            float p[32];
             tmem_load32(d + c, p);
             tmem_load_wait();
-          } else {
+            __syncwarp();
 #pragma unroll
-            for (int s = 0; s < 32; ++s) p[s] = 0.0f;
+            for (int v = 0; v < 4; ++v) {
+              float4 words4;
+              words4.x = __uint_as_float(Pair<T>::from_float(p[8 * v], p[8 * v + 1]));
+              words4.y = __uint_as_float(Pair<T>::from_float(p[8 * v + 2], p[8 * v + 3]));
+              words4.z = __uint_as_float(Pair<T>::from_float(p[8 * v + 4], p[8 * v + 5]));
+              words4.w = __uint_as_float(Pair<T>::from_float(p[8 * v + 6], p[8 * v + 7]));
+              *turned(turn, lane, v) = words4;
+            }
+            __syncwarp();
           }
+          if (w.n + c + 8 * t_part < cols) {
 #pragma unroll
-          for (int s = 0; s < 32; s += 8) {
-            if (!in || w.n + c + s >= cols) continue;
-            *reinterpret_cast<uint4*>(out + c + s) =
-                make_uint4(Pair<T>::from_float(p[s], p[s + 1]), Pair<T>::from_float(p[s + 2], p[s + 3]),
-                           Pair<T>::from_float(p[s + 4], p[s + 5]), Pair<T>::from_float(p[s + 6], p[s + 7]));
+            for (int v = 0; v < 4; ++v)
+              if (8 * v < rows)
+                *reinterpret_cast<float4*>(out + (size_t)(8 * v) * cols + c) =
+                    any ? *turned(turn, 8 * v + t_row, t_part) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
           }
         }
       }
       if (any) {
         fence_before();
         __syncwarp();
-        if (lane == 0) barrier_arrive(free_ + 8 * slot);
+        if (lane == 0) {
+          if constexpr (PAIR) barrier_arrive_in(lead_free + 8 * slot);
+          else barrier_arrive(free_ + 8 * slot);
+        }
         if (++slot == 2) slot = 0, slot_phase ^= 1;
       }
     }
@@ -441,9 +575,12 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
   fence_before();
   __syncthreads();
   if (threadIdx.x == 0 && *failed) *a.status = MOESCHED_ST_INTERNAL;
+  __syncwarp();
+  if constexpr (PAIR) cluster_sync_all();                  // the other CTA may still use our barriers and operands
   if (warp == 1) {
     fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+    if constexpr (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(TMEM_COLUMNS));
+    else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(TMEM_COLUMNS));
   }
 }
 
@@ -481,7 +618,7 @@ static cudaError_t make_map(EncodeFn encode, CUtensorMap* map, int dtype, const 
 ExpertScratch expert_scratch(int R, int I, int groups, bool backward) {
   ExpertScratch s;
   size_t at = 0;
-  const size_t table = ((size_t)R / BM + groups + 1) * sizeof(int4), rows = (size_t)R * I * 2;
+  const size_t table = ((size_t)R / CTA_M + groups + 1) * sizeof(int4), rows = (size_t)R * I * 2;
   auto take = [&](size_t bytes) {
     const size_t first = at;
     at += (bytes + 255) / 256 * 256;
@@ -495,24 +632,49 @@ ExpertScratch expert_scratch(int R, int I, int groups, bool backward) {
   return s;
 }
 
-template <int MODE, typename T>
-static cudaError_t launch_gemm(const GemmArgs& args, int act, long long tiles, cudaStream_t stream) {
-  const auto kern = (MODE == GLU || MODE == DHIDDEN) && act == MOESCHED_ACT_GELU ? gemm_kernel<MODE, T, MOESCHED_ACT_GELU>
-                                                                               : gemm_kernel<MODE, T, MOESCHED_ACT_SILU>;
-  const size_t smem = 1024 + STAGES * STAGE_BYTES + 256;
+template <int MODE, bool PAIR, typename T>
+static cudaError_t launch_gemm(const GemmArgs& args, int act, cudaStream_t stream) {
+  using S = Shape<MODE, PAIR>;
+  auto kern = gemm_kernel<MODE, PAIR, T, MOESCHED_ACT_SILU>;
+  if constexpr (MODE == GLU || MODE == DHIDDEN)            // (the others have no activation)
+    if (act == MOESCHED_ACT_GELU) kern = gemm_kernel<MODE, PAIR, T, MOESCHED_ACT_GELU>;
+  const size_t smem = 1024 + STAGES * STAGE_BYTES + 4 * TURN_BYTES + 8 * (4 * STAGES + 5) + 16;
+  static_assert(1024 + STAGES * STAGE_BYTES + 4 * TURN_BYTES + 8 * (4 * STAGES + 5) + 16 <= SMEM_LIMIT, "shared memory");
   if (cudaError_t e = permit_shared_memory(kern, smem); e != cudaSuccess) return e;
-  const long long sms = sm_count();
-  kern<<<(unsigned)(tiles < sms ? tiles : sms), GEMM_THREADS, smem, stream>>>(args);
-  return cudaGetLastError();
+  long long tiles;                                         // at most
+  if (MODE == DWEIGHT)
+    tiles = args.E * (2 * div_up(args.I, S::M) * div_up(args.D, S::N) + div_up(args.D, S::M) * div_up(args.I, S::N));
+  else
+    tiles = ((long long)args.R / S::M + (args.groups < args.R ? args.groups : args.R)) * div_up(MODE == GLU || MODE == DHIDDEN ? args.I : args.D, S::N);
+  const long long most = PAIR ? sm_count() / 2 : sm_count();
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)((tiles < most ? tiles : most) * (PAIR ? 2 : 1)));
+  cfg.blockDim = dim3(GEMM_THREADS);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  if (PAIR) {
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 2;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+  }
+  return cudaLaunchKernelEx(&cfg, kern, args);
 }
 template <int MODE>
-static cudaError_t launch_gemm(const GemmArgs& args, int dtype, int act, long long tiles, cudaStream_t stream) {
-  return dtype == MOESCHED_BF16 ? launch_gemm<MODE, __nv_bfloat16>(args, act, tiles, stream)
-                                : launch_gemm<MODE, __half>(args, act, tiles, stream);
+static cudaError_t launch_gemm(const GemmArgs& args, bool pair, int dtype, int act, cudaStream_t stream) {
+  if (dtype == MOESCHED_BF16)
+    return pair ? launch_gemm<MODE, true, __nv_bfloat16>(args, act, stream) : launch_gemm<MODE, false, __nv_bfloat16>(args, act, stream);
+  return pair ? launch_gemm<MODE, true, __half>(args, act, stream) : launch_gemm<MODE, false, __half>(args, act, stream);
 }
 
+// Tiles of pairs where the groups have 128 rows or more on the average: below, more than half of a tile of 256 rows would
+// be empty.
+static bool tiles_of_pairs(int R, int groups) { return R / CTA_M >= groups; }
+
 cudaError_t run_expert_ffn(int R, int D, int I, int E, int groups, int dtype, int act, const void* x, const void* w_gate,
-                           const void* w_up, const void* w_down, const int32_t* offsets, void* y, void* gate, void* up,
+                           const void* w_up, const void* w_down, const int32_t* offsets, void* y, float* gate, float* up,
                            void* scratch, int32_t* status, cudaStream_t stream) {
   const ExpertScratch at = expert_scratch(R, I, groups, false);
   unsigned char* base = static_cast<unsigned char*>(scratch);
@@ -526,38 +688,44 @@ cudaError_t run_expert_ffn(int R, int D, int I, int E, int groups, int dtype, in
   }
   EncodeFn encode;
   if ((e = encoder(&encode)) != cudaSuccess) return e;
+  const bool pair = tiles_of_pairs(R, groups);
   int4* plan = reinterpret_cast<int4*>(base + at.plan);
-  GemmArgs first = {}, second = {};
-  first.plan = second.plan = plan;
-  first.offsets = second.offsets = offsets;
-  first.R = second.R = R, first.D = second.D = D, first.I = second.I = I, first.E = second.E = E;
-  first.groups = second.groups = groups;
-  first.status = second.status = status;
-  if ((e = make_map(encode, &first.a[0], dtype, x, D, R, 1, BM)) != cudaSuccess) return e;
-  if ((e = make_map(encode, &first.b[0], dtype, w_gate, D, I, E, BN / 2)) != cudaSuccess) return e;
-  if ((e = make_map(encode, &first.b[1], dtype, w_up, D, I, E, BN / 2)) != cudaSuccess) return e;
-  first.out[0] = hidden, first.out[1] = gate, first.out[2] = up;
-  if ((e = make_map(encode, &second.a[0], dtype, hidden, I, R, 1, BM)) != cudaSuccess) return e;
-  if ((e = make_map(encode, &second.b[0], dtype, w_down, I, D, E, BN / 2)) != cudaSuccess) return e;
-  second.out[0] = y;
-  plan_kernel<<<1, 1024, 0, stream>>>(R, E, groups, offsets, plan, status);
+  GemmArgs args[2] = {};
+  for (GemmArgs& g : args) {
+    g.plan = plan;
+    g.offsets = offsets;
+    g.R = R, g.D = D, g.I = I, g.E = E, g.groups = groups;
+    g.status = status;
+  }
+  const auto map = [&](CUtensorMap* m, const void* p, int cols, int rows, int deep, int high) {
+    if (e == cudaSuccess) e = make_map(encode, m, dtype, p, cols, rows, deep, high);
+  };
+  map(&args[0].a[0], x, D, R, 1, CTA_M);
+  map(&args[0].b[0], w_gate, D, I, E, 64);
+  map(&args[0].b[1], w_up, D, I, E, 64);
+  args[0].out[0] = hidden, args[0].keep[0] = gate, args[0].keep[1] = up;
+  map(&args[1].a[0], hidden, I, R, 1, CTA_M);
+  map(&args[1].b[0], w_down, I, D, E, 64);
+  args[1].out[0] = y;
+  if (e != cudaSuccess) return e;
+  plan_kernel<<<1, 1024, 0, stream>>>(R, E, groups, pair ? 2 * CTA_M : CTA_M, offsets, plan, status);
   if ((e = cudaGetLastError()) != cudaSuccess) return e;
-  const long long m_tiles = (long long)R / BM + (groups < R ? groups : R);
-  if ((e = launch_gemm<GLU>(first, dtype, act, m_tiles * ((I + BN / 2 - 1) / (BN / 2)), stream)) != cudaSuccess) return e;
-  return launch_gemm<DOWN>(second, dtype, act, m_tiles * ((D + BN - 1) / BN), stream);
+  if ((e = launch_gemm<GLU>(args[0], pair, dtype, act, stream)) != cudaSuccess) return e;
+  return launch_gemm<DOWN>(args[1], pair, dtype, act, stream);
 }
 
 cudaError_t run_expert_backward(int R, int D, int I, int E, int groups, int dtype, int act, const void* dy, const void* x,
                                 const void* w_gate, const void* w_up, const void* w_down, const int32_t* offsets,
-                                const void* gate, const void* up, void* dx, void* dw_gate, void* dw_up, void* dw_down,
+                                const float* gate, const float* up, void* dx, void* dw_gate, void* dw_up, void* dw_down,
                                 void* scratch, int32_t* status, cudaStream_t stream) {
   cudaError_t e;
   const size_t weights = (size_t)E * I * D * 2;
+  const bool pair = tiles_of_pairs(R, groups);
   if (R == 0) {                                             // no rows: no tensor maps, and gradients of nothing
     if ((e = cudaMemsetAsync(dw_gate, 0, weights, stream)) != cudaSuccess) return e;
     if ((e = cudaMemsetAsync(dw_up, 0, weights, stream)) != cudaSuccess) return e;
     if ((e = cudaMemsetAsync(dw_down, 0, weights, stream)) != cudaSuccess) return e;
-    plan_kernel<<<1, 1024, 0, stream>>>(R, E, groups, offsets, static_cast<int4*>(scratch), status);
+    plan_kernel<<<1, 1024, 0, stream>>>(R, E, groups, CTA_M, offsets, static_cast<int4*>(scratch), status);
     return cudaGetLastError();
   }
   const ExpertScratch at = expert_scratch(R, I, groups, true);
@@ -573,15 +741,15 @@ cudaError_t run_expert_backward(int R, int D, int I, int E, int groups, int dtyp
     g.R = R, g.D = D, g.I = I, g.E = E, g.groups = groups;
     g.status = status;
   }
-  auto map = [&](CUtensorMap* m, const void* p, int cols, int rows, int deep, int high) {
+  const auto map = [&](CUtensorMap* m, const void* p, int cols, int rows, int deep, int high) {
     if (e == cudaSuccess) e = make_map(encode, m, dtype, p, cols, rows, deep, high);
   };
-  map(&args[0].a[0], dy, D, R, 1, BM);
+  map(&args[0].a[0], dy, D, R, 1, CTA_M);
   map(&args[0].b[0], w_down, I, D, E, BK);
   args[0].in[0] = gate, args[0].in[1] = up;
   args[0].out[0] = hidden, args[0].out[1] = d_gate, args[0].out[2] = d_up;
-  map(&args[1].a[0], d_gate, I, R, 1, BM);
-  map(&args[1].a[1], d_up, I, R, 1, BM);
+  map(&args[1].a[0], d_gate, I, R, 1, CTA_M);
+  map(&args[1].a[1], d_up, I, R, 1, CTA_M);
   map(&args[1].b[0], w_gate, D, I, E, BK);
   map(&args[1].b[1], w_up, D, I, E, BK);
   args[1].out[0] = dx;
@@ -593,13 +761,11 @@ cudaError_t run_expert_backward(int R, int D, int I, int E, int groups, int dtyp
   map(&args[2].b[2], hidden, I, R, 1, BK);
   args[2].out[0] = dw_gate, args[2].out[1] = dw_up, args[2].out[2] = dw_down;
   if (e != cudaSuccess) return e;
-  plan_kernel<<<1, 1024, 0, stream>>>(R, E, groups, offsets, plan, status);
+  plan_kernel<<<1, 1024, 0, stream>>>(R, E, groups, pair ? 2 * CTA_M : CTA_M, offsets, plan, status);
   if ((e = cudaGetLastError()) != cudaSuccess) return e;
-  const long long m_tiles = (long long)R / BM + (groups < R ? groups : R);
-  if ((e = launch_gemm<DHIDDEN>(args[0], dtype, act, m_tiles * ((I + BN - 1) / BN), stream)) != cudaSuccess) return e;
-  if ((e = launch_gemm<DINPUT>(args[1], dtype, act, m_tiles * ((D + BN - 1) / BN), stream)) != cudaSuccess) return e;
-  const long long gu = (long long)((I + BM - 1) / BM) * ((D + BN - 1) / BN), dn = (long long)((D + BM - 1) / BM) * ((I + BN - 1) / BN);
-  return launch_gemm<DWEIGHT>(args[2], dtype, act, E * (2 * gu + dn), stream);
+  if ((e = launch_gemm<DHIDDEN>(args[0], pair, dtype, act, stream)) != cudaSuccess) return e;
+  if ((e = launch_gemm<DINPUT>(args[1], pair, dtype, act, stream)) != cudaSuccess) return e;
+  return launch_gemm<DWEIGHT>(args[2], pair, dtype, act, stream);
 }
 
 }  // namespace moesched
