@@ -426,7 +426,7 @@ int moesched_expert_matvec4(int R, int K, int N, int E, int groups, int group, i
     if ((R > 0 && p == nullptr) || !aligned16(p)) return MOESCHED_EINVAL;
   if (!aligned16(d_w_up) || !aligned16(d_scale_up)) return MOESCHED_EINVAL;
   cudaError_t e = run_few(R, K, N, E, groups, group, dtype, act, d_x, d_w, d_scale, d_w_up, d_scale_up, d_offsets, d_y, nullptr,
-                          nullptr, d_status, static_cast<cudaStream_t>(stream));
+                          nullptr, d_status, false, static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? MOESCHED_OK : fail_cuda(e);
 }
 

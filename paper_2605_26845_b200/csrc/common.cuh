@@ -257,10 +257,11 @@ cudaError_t run_slots(int B, int N, const int32_t* demand, int K, const uint8_t*
                       int P, const int32_t* counts, int32_t* start, int32_t* length, int32_t* row, int32_t* rows,
                       int32_t* offsets, int32_t* status, cudaStream_t stream);
 
-// products of a few rows with their experts' weights (few_kernel.cu); group 0: weights in 16 bits
+// products of a few rows with their experts' weights (few_kernel.cu); group 0: weights in 16 bits; early: may be started before the
+// kernel before it is over (which is one of the same call)
 cudaError_t run_few(int R, int K, int N, int E, int groups, int group, int dtype, int act, const void* x, const void* w,
                     const void* scale, const void* w_up, const void* scale_up, const int32_t* offsets, void* y, float* sum,
-                    float* sum_up, int32_t* status, cudaStream_t stream);
+                    float* sum_up, int32_t* status, bool early, cudaStream_t stream);
 
 // gated feed-forward block of the experts (expert_kernel.cu); scratch in bytes from its start
 struct ExpertScratch {

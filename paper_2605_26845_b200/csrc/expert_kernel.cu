@@ -10,7 +10,7 @@
 // Persistent CTAs take tiles of 128 x 128 (GLU: 64 columns of a and the same 64 of u), or pairs of CTAs on two SMs tiles of
 // 256 x 256, each with half of the rows of either operand: every byte that a pair fetches serves twice as many products. One warp fetches
 // the operands with TMA, 64 deep, into a ring of stages; one thread (of a pair: of its first CTA) issues the matrix instructions, whose
-// sums are in tensor memory, twice, so that four warps empty one while the other fills; those warps turn what they
+// sums are in tensor memory, twice, so that eight warps empty one while the other fills; those warps turn what they
 // read by way of shared memory, so that neighbouring lanes load and store neighbouring columns. Operands stay as they are in memory:
 // where the contraction runs over the slower axis (Wd in DHIDDEN, Wg and Wu in DINPUT, everything in DWEIGHT) the instruction
 // takes them transposed.
@@ -26,9 +26,10 @@ namespace moesched {
 enum { GLU, DOWN, DHIDDEN, DINPUT, DWEIGHT };
 
 constexpr int CTA_M = 128, CTA_N = 128, BK = 64;           // rows of the operands that a CTA fetches, and how deep
-constexpr int STAGES = 6;
+constexpr int STAGES = 5;
 constexpr int A_BYTES = CTA_M * BK * 2, B_BYTES = CTA_N * BK * 2, STAGE_BYTES = A_BYTES + B_BYTES;
-constexpr int GEMM_THREADS = 256;
+constexpr int EMPTIERS = 8;                                // warps that empty tensor memory: two for each quarter of its lanes
+constexpr int GEMM_THREADS = 128 + 32 * EMPTIERS;
 constexpr int BOX_BYTES = 64 * 64 * 2;                     // one box of B, and of a transposed A
 constexpr int TURN_BYTES = 2 * 32 * 16 * 4;                // of a warp that empties tensor memory
 constexpr int RASTER_ROWS = 2048;                          // rows of row tiles that share a pass over the columns
@@ -139,6 +140,7 @@ __global__ void __launch_bounds__(1024) plan_kernel(int R, int E, int groups, in
                                                     int4* __restrict__ plan, int32_t* __restrict__ status) {
   __shared__ int warp_sum[32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, per = groups / E;
+  let_next_start();
   bool bad = false;
   for (int g = threadIdx.x; g <= groups; g += 1024) {
     const int v = offsets[g];
@@ -222,14 +224,23 @@ __device__ __forceinline__ Tile tile_at(const GemmArgs& a, const int4 head, int 
   }
   return w;
 }
+// The groups of an expert, for DWEIGHT: the first one's rows are kept from tile to tile, the next one's are on their way while
+// one is worked on.
+struct Spans {
+  int expert = -1, begin = 0, end = 0;
+};
 // calls f(k-block's first row or column, what it holds (64 or less), which operands) for every block of the contraction
 template <int MODE, typename F>
-__device__ __forceinline__ bool each_block(const GemmArgs& a, const Tile& w, F&& f) {
+__device__ __forceinline__ bool each_block(const GemmArgs& a, const Tile& w, Spans& kept, F&& f) {
   if constexpr (MODE == DWEIGHT) {
+    if (kept.expert != w.e) kept = {w.e, a.offsets[w.e], a.offsets[w.e + 1]};
+    int begin = kept.begin, end = kept.end;
     for (int g = w.e; g < a.groups; g += a.E) {
-      const int2 span = rows_of_group(a.offsets, g, a.R);
-      for (int r = span.x; r < span.y; r += BK)
-        if (!f(r, min(BK, span.y - r), w.which)) return false;
+      const bool more = g + a.E < a.groups;
+      const int next_begin = more ? a.offsets[g + a.E] : 0, next_end = more ? a.offsets[g + a.E + 1] : 0;
+      for (int r = begin; r < end; r += BK)                // (the plan has found all offsets in order)
+        if (!f(r, min(BK, end - r), w.which)) return false;
+      begin = next_begin, end = next_end;
     }
   } else {
     const int K = MODE == GLU || MODE == DHIDDEN ? a.D : a.I;
@@ -253,7 +264,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
   constexpr int TMEM_COLUMNS = 2 * S::SUMS;
   extern __shared__ unsigned char raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
-  unsigned long long* bars = reinterpret_cast<unsigned long long*>(smem + STAGES * STAGE_BYTES + 4 * TURN_BYTES);
+  unsigned long long* bars = reinterpret_cast<unsigned long long*>(smem + STAGES * STAGE_BYTES + EMPTIERS * TURN_BYTES);
   const unsigned ring = smem_addr(smem);
   // full, done: operands there, sums there; empty, free_: may be overwritten; partly, fixed: blocks that end within (DWEIGHT)
   const unsigned full = smem_addr(bars), empty = full + 8 * STAGES, partly = empty + 8 * STAGES, fixed = partly + 8 * STAGES,
@@ -263,6 +274,8 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const unsigned rank = PAIR ? cluster_ctarank() : 0;      // the first CTA of a pair issues
   const int first_tile = PAIR ? blockIdx.x / 2 : blockIdx.x, step = PAIR ? gridDim.x / 2 : gridDim.x;
+  Spans spans;
+  let_next_start();
 
   if (threadIdx.x == 0) {
     *failed = 0;
@@ -274,7 +287,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
     }
     for (int q = 0; q < 2; ++q) {
       barrier_init(done + 8 * q, 1);
-      barrier_init(free_ + 8 * q, PAIR ? 8 : 4);
+      barrier_init(free_ + 8 * q, (PAIR ? 2 : 1) * EMPTIERS);
     }
     barrier_init(drain, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -293,6 +306,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
   if constexpr (PAIR) cluster_sync_all();                  // the other CTA's barriers are there
   fence_after();
   const unsigned tmem = *reinterpret_cast<volatile unsigned*>(words + 1);
+  wait_for_previous();                                     // nothing of other kernels is read, and nothing written, before
   const int4 head = a.plan[0];
   const int total = tile_total<MODE, PAIR>(a, head);
 
@@ -305,7 +319,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
       for (int t = first_tile; t < total && ok; t += step) {
         const Tile w = tile_at<MODE, PAIR>(a, head, t);
         const int row = w.row + (int)rank * CTA_M;
-        ok = each_block<MODE>(a, w, [&](int k, int held, int part) {
+        ok = each_block<MODE>(a, w, spans, [&](int k, int held, int part) {
           if (!barrier_wait(empty + 8 * stage, phase ^ 1, failed)) return false;
           const unsigned to = ring + stage * STAGE_BYTES, tb = to + A_BYTES;
           // a block that ends within is counted by each CTA for itself, for the warp that zeroes its end
@@ -356,7 +370,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
         const Tile w = tile_at<MODE, PAIR>(a, head, t);
         bool first = true;
         const unsigned d = tmem + slot * S::SUMS;
-        ok = each_block<MODE>(a, w, [&](int, int held, int) {
+        ok = each_block<MODE>(a, w, spans, [&](int, int held, int) {
           if (first && !barrier_wait(free_ + 8 * slot, slot_phase ^ 1, failed)) return false;
           if (MODE == DWEIGHT && held < BK) {
             if (!barrier_wait(fixed + 8 * stage, fixed_phase >> stage & 1, failed)) return false;
@@ -397,7 +411,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
       const unsigned lead_fixed = PAIR ? in_cta(fixed, 0) : fixed;
       for (int t = first_tile; t < total && ok; t += step) {
         const Tile w = tile_at<MODE, PAIR>(a, head, t);
-        ok = each_block<MODE>(a, w, [&](int, int held, int) {
+        ok = each_block<MODE>(a, w, spans, [&](int, int held, int) {
           if (held < BK) {
             if (!__all_sync(FULL, barrier_wait(partly + 8 * stage, part_phase >> stage & 1, failed))) return false;
             part_phase ^= 1u << stage;
@@ -419,10 +433,11 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
       }
     }
   } else if (warp >= 4) {
-    const int quarter = warp - 4;
+    const int quarter = warp & 3, half = (warp - 4) >> 2;  // lanes of tensor memory, and which half of the columns
+    const int c_begin = half * (S::N / 2), c_end = c_begin + S::N / 2;
     const unsigned mine = tmem + ((unsigned)quarter << 21);
     const unsigned lead_free = PAIR ? in_cta(free_, 0) : free_;
-    float* turn = reinterpret_cast<float*>(smem + STAGES * STAGE_BYTES + quarter * TURN_BYTES);
+    float* turn = reinterpret_cast<float*>(smem + STAGES * STAGE_BYTES + (warp - 4) * TURN_BYTES);
     // after the turn a lane has, in round q, four words of row 8 q + lane / 4
     const int t_row = lane >> 2, t_part = lane & 3;
     int slot = 0;
@@ -435,7 +450,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
       bool any = true;
       if constexpr (MODE == DWEIGHT) {
         any = false;
-        each_block<MODE>(a, w, [&](int, int, int) { any = true; return false; });
+        each_block<MODE>(a, w, spans, [&](int, int, int) { any = true; return false; });
       }
       const auto wait_sums = [&]() {
         if (!__all_sync(FULL, barrier_wait(done + 8 * slot, slot_phase, failed))) return false;
@@ -446,7 +461,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
         if (!wait_sums()) break;
         const size_t at = (size_t)row * a.I + w.n + 4 * t_part;
 #pragma unroll 1
-        for (int c = 0; c < S::N; c += 16) {
+        for (int c = c_begin; c < c_end; c += 16) {
           float p[16], q[16];
           tmem_load16(d + c, p);
           tmem_load16(d + S::N + c, q);
@@ -480,7 +495,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
           float4 g[4], u[4];
         };
         const auto fetch = [&](int c, Held& h) {           // a and u of 16 columns, on their way while others are worked on
-          const bool in = c < S::N && w.n + c + 4 * t_part < a.I;
+          const bool in = c < c_end && w.n + c + 4 * t_part < a.I;
 #pragma unroll
           for (int v = 0; v < 4; ++v) {
             const size_t from = at + (size_t)(8 * v) * a.I + c;
@@ -520,10 +535,10 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
           }
         };
         Held even, odd;
-        fetch(0, even);
+        fetch(c_begin, even);
         if (!wait_sums()) break;
 #pragma unroll 1
-        for (int c = 0; c < S::N; c += 32) {
+        for (int c = c_begin; c < c_end; c += 32) {
           fetch(c + 16, odd);
           work(c, even);
           fetch(c + 32, even);
@@ -535,7 +550,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
         const size_t first = MODE == DWEIGHT ? (size_t)w.e * a.I * a.D + (size_t)row * cols : (size_t)row * cols;
         T* out = static_cast<T*>(a.out[MODE == DWEIGHT ? w.which : 0]) + first + w.n + 8 * t_part;
 #pragma unroll 1
-        for (int c = 0; c < S::N; c += 32) {
+        for (int c = c_begin; c < c_end; c += 32) {
           if (any) {
             float p[32];
             tmem_load32(d + c, p);
@@ -638,8 +653,8 @@ static cudaError_t launch_gemm(const GemmArgs& args, int act, cudaStream_t strea
   auto kern = gemm_kernel<MODE, PAIR, T, MOESCHED_ACT_SILU>;
   if constexpr (MODE == GLU || MODE == DHIDDEN)            // (the others have no activation)
     if (act == MOESCHED_ACT_GELU) kern = gemm_kernel<MODE, PAIR, T, MOESCHED_ACT_GELU>;
-  const size_t smem = 1024 + STAGES * STAGE_BYTES + 4 * TURN_BYTES + 8 * (4 * STAGES + 5) + 16;
-  static_assert(1024 + STAGES * STAGE_BYTES + 4 * TURN_BYTES + 8 * (4 * STAGES + 5) + 16 <= SMEM_LIMIT, "shared memory");
+  const size_t smem = 1024 + STAGES * STAGE_BYTES + EMPTIERS * TURN_BYTES + 8 * (4 * STAGES + 5) + 16;
+  static_assert(1024 + STAGES * STAGE_BYTES + EMPTIERS * TURN_BYTES + 8 * (4 * STAGES + 5) + 16 <= SMEM_LIMIT, "shared memory");
   if (cudaError_t e = permit_shared_memory(kern, smem); e != cudaSuccess) return e;
   long long tiles;                                         // at most
   if (MODE == DWEIGHT)
@@ -652,14 +667,13 @@ static cudaError_t launch_gemm(const GemmArgs& args, int act, cudaStream_t strea
   cfg.blockDim = dim3(GEMM_THREADS);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
-  if (PAIR) {
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = 2;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-  }
+  cudaLaunchAttribute attr[2];
+  attr[0] = start_early();
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = 2;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = PAIR ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kern, args);
 }
 template <int MODE>
@@ -681,10 +695,11 @@ cudaError_t run_expert_ffn(int R, int D, int I, int E, int groups, int dtype, in
   void* hidden = base + at.hidden;
   cudaError_t e;
   if (R <= EXPERT_FEW_ROWS) {
-    e = run_few(R, D, I, E, groups, 0, dtype, act, x, w_gate, nullptr, w_up, nullptr, offsets, hidden, gate, up, status, stream);
+    e = run_few(R, D, I, E, groups, 0, dtype, act, x, w_gate, nullptr, w_up, nullptr, offsets, hidden, gate, up, status, false,
+                stream);
     if (e != cudaSuccess) return e;
     return run_few(R, I, D, E, groups, 0, dtype, act, hidden, w_down, nullptr, nullptr, nullptr, offsets, y, nullptr, nullptr,
-                   status, stream);
+                   status, true, stream);
   }
   EncodeFn encode;
   if ((e = encoder(&encode)) != cudaSuccess) return e;

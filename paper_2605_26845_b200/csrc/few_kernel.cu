@@ -135,6 +135,7 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, 1) few_kernel(const FewArgs a)
   const int tiles = (N + OUTPUTS - 1) / OUTPUTS;
   const int gr = lane >> 2, t = lane & 3;
 
+  let_next_start();
   // experts with rows, and the units up to the end of each
   bool bad = false;
   if (blockIdx.x == 0) {                                  // one CTA looks at all offsets
@@ -143,7 +144,6 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, 1) few_kernel(const FewArgs a)
       bad |= v < 0 || v > R || (g > 0 && a.offsets[g - 1] > v);
     }
     bad = __syncthreads_or(bad);
-    if (threadIdx.x == 0) *a.status = bad ? MOESCHED_ST_BAD_INPUT : MOESCHED_ST_OK;
   }
   int experts = 0;
   long long units = 0;
@@ -229,6 +229,8 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, 1) few_kernel(const FewArgs a)
     if (get.pass > 0) find_rows(get);
   }
   __syncthreads();                                        // the rings are the warps' own from here on
+  wait_for_previous();                                    // x may come from the kernel before this one
+  if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = bad ? MOESCHED_ST_BAD_INPUT : MOESCHED_ST_OK;
   if (mine <= 0) return;
   const auto next_unit = [&](FewCursor& c) {
     --c.left;
@@ -455,40 +457,47 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, 1) few_kernel(const FewArgs a)
 }
 
 template <typename T, int GROUP, bool GATED, int ACT>
-static cudaError_t launch_few(const FewArgs& a, cudaStream_t stream) {
+static cudaError_t launch_few(const FewArgs& a, bool early, cudaStream_t stream) {
   const auto kern = few_kernel<T, GROUP, GATED, ACT>;
   const size_t smem = FewShape<GROUP>::SMEM;
   if (cudaError_t e = permit_shared_memory(kern, smem); e != cudaSuccess) return e;
   const long long tiles = (a.N + (GATED ? 15 : 31)) / (GATED ? 16 : 32), teams = FEW_WARPS / a.split;
   const long long units = (a.R / FEW_ROWS + (a.E < a.R ? a.E : a.R)) * tiles, ctas = (units + teams - 1) / teams, sms = sm_count();
-  kern<<<(unsigned)(ctas < 1 ? 1 : ctas < sms ? ctas : sms), 32 * FEW_WARPS, smem, stream>>>(a);
-  return cudaGetLastError();
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(ctas < 1 ? 1 : ctas < sms ? ctas : sms));
+  cfg.blockDim = dim3(32 * FEW_WARPS);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr = start_early();
+  cfg.attrs = &attr;
+  cfg.numAttrs = early ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, kern, a);
 }
 template <typename T, int GROUP>
-static cudaError_t launch_few(const FewArgs& a, bool gated, int act, cudaStream_t stream) {
-  if (!gated) return launch_few<T, GROUP, false, MOESCHED_ACT_SILU>(a, stream);
-  if (act == MOESCHED_ACT_SILU) return launch_few<T, GROUP, true, MOESCHED_ACT_SILU>(a, stream);
-  return launch_few<T, GROUP, true, MOESCHED_ACT_GELU>(a, stream);
+static cudaError_t launch_few(const FewArgs& a, bool gated, int act, bool early, cudaStream_t stream) {
+  if (!gated) return launch_few<T, GROUP, false, MOESCHED_ACT_SILU>(a, early, stream);
+  if (act == MOESCHED_ACT_SILU) return launch_few<T, GROUP, true, MOESCHED_ACT_SILU>(a, early, stream);
+  return launch_few<T, GROUP, true, MOESCHED_ACT_GELU>(a, early, stream);
 }
 
 cudaError_t run_few(int R, int K, int N, int E, int groups, int group, int dtype, int act, const void* x, const void* w,
                     const void* scale, const void* w_up, const void* scale_up, const int32_t* offsets, void* y, float* sum,
-                    float* sum_up, int32_t* status, cudaStream_t stream) {
+                    float* sum_up, int32_t* status, bool early, cudaStream_t stream) {
   FewArgs a{R, K, N, E, groups, 1, x, {w, w_up}, {scale, scale_up}, offsets, y, {sum, sum_up}, status};
   const bool gated = w_up != nullptr;
   // as few warps share the k of an output as still give every warp of the GPU a few units (which differ in length by one)
   const long long units = (long long)(E < R ? E : R) * ((N + (gated ? 15 : 31)) / (gated ? 16 : 32));
   while (a.split < FEW_WARPS && units * a.split < 4LL * FEW_WARPS * sm_count()) a.split *= 2;
   if (dtype == MOESCHED_BF16) {
-    if (group == 0) return launch_few<__nv_bfloat16, 0>(a, gated, act, stream);
-    if (group == 32) return launch_few<__nv_bfloat16, 32>(a, gated, act, stream);
-    if (group == 64) return launch_few<__nv_bfloat16, 64>(a, gated, act, stream);
-    return launch_few<__nv_bfloat16, 128>(a, gated, act, stream);
+    if (group == 0) return launch_few<__nv_bfloat16, 0>(a, gated, act, early, stream);
+    if (group == 32) return launch_few<__nv_bfloat16, 32>(a, gated, act, early, stream);
+    if (group == 64) return launch_few<__nv_bfloat16, 64>(a, gated, act, early, stream);
+    return launch_few<__nv_bfloat16, 128>(a, gated, act, early, stream);
   }
-  if (group == 0) return launch_few<__half, 0>(a, gated, act, stream);
-  if (group == 32) return launch_few<__half, 32>(a, gated, act, stream);
-  if (group == 64) return launch_few<__half, 64>(a, gated, act, stream);
-  return launch_few<__half, 128>(a, gated, act, stream);
+  if (group == 0) return launch_few<__half, 0>(a, gated, act, early, stream);
+  if (group == 32) return launch_few<__half, 32>(a, gated, act, early, stream);
+  if (group == 64) return launch_few<__half, 64>(a, gated, act, early, stream);
+  return launch_few<__half, 128>(a, gated, act, early, stream);
 }
 
 }  // namespace moesched
