@@ -438,14 +438,12 @@ def best_budget(count, prefix_overlap_ns, prefix_unserved_tokens, ns_per_unserve
 MAX_EXPERTS = 1024
 
 
-def _empty(shape, dtype, device):
-    """torch.empty for a densely packed tensor. (empty_strided takes two thirds of its time, which counts beside kernels of a few
-    microseconds.)"""
-    strides, n = [], 1
-    for s in reversed(shape):
-        strides.append(n)
-        n *= max(1, s)
-    return torch.empty_strided(shape, strides[::-1], dtype=dtype, device=device)
+def _empty(dtype, device, *shape):
+    """torch.empty for a densely packed tensor of one to three dimensions. (empty_strided, and empty_like where there is a like, take
+    two thirds of its time, which counts beside kernels of a few microseconds.)"""
+    n = len(shape)
+    strides = (1,) if n == 1 else (shape[1], 1) if n == 2 else (shape[1] * shape[2], shape[2], 1)
+    return torch.empty_strided(shape, strides, dtype=dtype, device=device)
 
 
 def route_demand(experts, num_experts, out=None) -> dict:
@@ -458,11 +456,13 @@ def route_demand(experts, num_experts, out=None) -> dict:
         raise MoeschedError("experts must have shape [B, N, S]")
     B, N, S = experts.shape
     E, dev = int(num_experts), experts.device
-    shapes = dict(demand=(B, N, N), counts=(B, N, E), slot=(B, N, S), status=(B, N))
     if out is None:
-        out = {k: _empty(v, torch.int32, dev) for k, v in shapes.items()}
-    elif any(_dev(out[k], torch.int32, f"out['{k}']").shape != v or out[k].device != dev for k, v in shapes.items()):
-        raise MoeschedError("out has the wrong shape or device")
+        out = dict(demand=_empty(torch.int32, dev, B, N, N), counts=_empty(torch.int32, dev, B, N, E), slot=torch.empty_like(experts),
+                   status=_empty(torch.int32, dev, B, N))
+    else:
+        for k, shape in dict(demand=(B, N, N), counts=(B, N, E), slot=(B, N, S), status=(B, N)).items():
+            if _dev(out[k], torch.int32, f"out['{k}']").shape != shape or out[k].device != dev:
+                raise MoeschedError("out has the wrong shape or device")
     _call("moesched_route_demand", dev, B, N, S, E, _ptr(experts), _ptr(out["demand"]), _ptr(out["counts"]), _ptr(out["slot"]),
           _ptr(out["status"]))
     return out
@@ -486,12 +486,13 @@ def schedule_slots(demand, perm, dur, count, counts=None) -> dict:
         if counts.dim() != 3 or counts.shape[:2] != (B, N) or counts.shape[2] % N != 0:
             raise MoeschedError("counts must be [B, N, N * experts per rank]")
         P = counts.shape[2] // N
-    if any(t is not None and t.device != dev for t in (perm, dur, count, counts)):
+    if perm.device != dev or dur.device != dev or count.device != dev or (counts is not None and counts.device != dev):
         raise MoeschedError("all tensors must be on one device")
-    shapes = dict(start=(B, K, N), length=(B, K, N), row=(B, K, N), rows=(B, N), status=(B,))
+    start = _empty(torch.int32, dev, B, K, N)
+    res = dict(start=start, length=torch.empty_like(start), row=torch.empty_like(start), rows=_empty(torch.int32, dev, B, N),
+               status=torch.empty_like(count))
     if counts is not None:
-        shapes["offsets"] = (B, N, K * P + 1)
-    res = {k: _empty(v, torch.int32, dev) for k, v in shapes.items()}
+        res["offsets"] = _empty(torch.int32, dev, B, N, K * P + 1)
     _call("moesched_schedule_slots", dev, B, N, _ptr(demand), K, _ptr(perm), _ptr(dur), _ptr(count), P, _ptr(counts), _ptr(res["start"]),
           _ptr(res["length"]), _ptr(res["row"]), _ptr(res["rows"]), _ptr(res.get("offsets")), _ptr(res["status"]))
     return res
@@ -522,7 +523,7 @@ def _expert_rows(x, offsets, num_experts):
 def _like(t, like, shape, what):
     """`t`, or a new tensor, of the type and device of `like` and the given shape."""
     if t is None:
-        return _empty(shape, like.dtype, like.device)
+        return _empty(like.dtype, like.device, *shape)
     _dev(t, like.dtype, what)
     if t.shape != tuple(shape) or t.device != like.device:
         raise MoeschedError(f"{what} must have shape {tuple(shape)}, on the device of x")
@@ -533,10 +534,10 @@ def _expert_weights(x, w_gate, w_up, w_down):
     if not isinstance(w_gate, torch.Tensor) or w_gate.dim() != 3 or x.dim() != 2:
         raise MoeschedError("x must be [R, D], w_gate and w_up [E, I, D] and w_down [E, D, I]")
     E, I, D = w_gate.shape
+    dtype, dev = x.dtype, x.device
     for t, shape, what in ((w_gate, (E, I, D), "w_gate"), (w_up, (E, I, D), "w_up"), (w_down, (E, D, I), "w_down")):
-        if t is None:
-            raise MoeschedError(f"{what} is missing")
-        _like(t, x, shape, what)
+        if _dev(t, dtype, what).shape != shape or t.device != dev:
+            raise MoeschedError(f"{what} must have shape {shape}, on the device of x")
     if x.shape[1] != D:
         raise MoeschedError("x must be [R, D] with the D of the weights")
     return E, I, D
@@ -544,7 +545,7 @@ def _expert_weights(x, w_gate, w_up, w_down):
 
 def _status_of(status, device):
     if status is None:
-        return _empty((1,), torch.int32, device)
+        return _empty(torch.int32, device, 1)
     _dev(status, torch.int32, "status")
     if status.numel() != 1 or status.device != device:
         raise MoeschedError("status must hold one int32, on the device of x")
@@ -555,7 +556,7 @@ def _expert_scratch(scratch, x, I, groups, backward):
     """256-byte aligned working memory: the caller's (uint8), or new."""
     need = int(load_library().moesched_expert_scratch_bytes(x.shape[0], I, groups, backward))
     if scratch is None:
-        return _empty((max(1, need),), torch.uint8, x.device)
+        return _empty(torch.uint8, x.device, max(1, need))
     _dev(scratch, torch.uint8, "scratch")
     if scratch.numel() < need or scratch.device != x.device:
         raise MoeschedError("scratch is smaller than expert_scratch_bytes, or on another device")
@@ -580,7 +581,7 @@ def expert_ffn(x, w_gate, w_up, w_down, offsets, act="silu", save=False, out=Non
         raise MoeschedError("all tensors must be on one device")
     R, dev = x.shape[0], x.device
     out = _like(out, x, (R, D), "out")
-    saved = {k: _empty((R, I), torch.float32, dev) for k in ("gate", "up")} if save else {}
+    saved = {k: _empty(torch.float32, dev, R, I) for k in ("gate", "up")} if save else {}
     scratch = _expert_scratch(scratch, x, I, groups, 0)
     _call("moesched_expert_ffn", dev, R, D, I, E, groups, dtype, _act(act), _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(w_down),
           _ptr(offsets), _ptr(out), _ptr(saved.get("gate")), _ptr(saved.get("up")), _ptr(scratch), _ptr(_status_of(status, dev)))
