@@ -26,12 +26,12 @@ namespace moesched {
 enum { GLU, DOWN, DHIDDEN, DINPUT, DWEIGHT };
 
 constexpr int CTA_M = 128, CTA_N = 128, BK = 64;           // rows of the operands that a CTA fetches, and how deep
-constexpr int STAGES = 5;
+constexpr int STAGES = 6;
 constexpr int A_BYTES = CTA_M * BK * 2, B_BYTES = CTA_N * BK * 2, STAGE_BYTES = A_BYTES + B_BYTES;
 constexpr int EMPTIERS = 8;                                // warps that empty tensor memory: two for each quarter of its lanes
 constexpr int GEMM_THREADS = 128 + 32 * EMPTIERS;
 constexpr int BOX_BYTES = 64 * 64 * 2;                     // one box of B, and of a transposed A
-constexpr int TURN_BYTES = 2 * 32 * 16 * 4;                // of a warp that empties tensor memory
+constexpr int TURN_BYTES = 32 * 16 * 4;                    // of a warp that empties tensor memory
 constexpr int RASTER_ROWS = 2048;                          // rows of row tiles that share a pass over the columns
 
 struct alignas(64) GemmArgs {
@@ -67,6 +67,17 @@ __device__ __forceinline__ bool barrier_wait(unsigned bar, unsigned parity, vola
   }
   *failed = 1;
   return false;
+}
+// For a whole warp: what follows is the same for all lanes, and the compiler sees it. (The descriptors of matrix instructions and
+// copies are read from the warp's common registers; out of a branch of one lane they were moved there one by one, which
+// took 80 to 130 cycles an instruction and was what bounded the products.)
+__device__ __forceinline__ bool warp_wait(unsigned bar, unsigned parity, volatile int* failed) {
+  return __all_sync(FULL, barrier_wait(bar, parity, failed)) != 0;
+}
+__device__ __forceinline__ bool elect_lane() {
+  unsigned is;
+  asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(is));
+  return is != 0;
 }
 // the address of `local` in CTA `rank` of the cluster
 __device__ __forceinline__ unsigned in_cta(unsigned local, unsigned rank) {
@@ -271,7 +282,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
                  done = fixed + 8 * STAGES, free_ = done + 16, drain = free_ + 16;
   int* words = reinterpret_cast<int*>(bars + 4 * STAGES + 5);
   volatile int* failed = words;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31, warp = __shfl_sync(FULL, (int)threadIdx.x >> 5, 0);
   const unsigned rank = PAIR ? cluster_ctarank() : 0;      // the first CTA of a pair issues
   const int first_tile = PAIR ? blockIdx.x / 2 : blockIdx.x, step = PAIR ? gridDim.x / 2 : gridDim.x;
   Spans spans;
@@ -311,20 +322,28 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
   const int total = tile_total<MODE, PAIR>(a, head);
 
   if (warp == 0) {
-    if (lane == 0) {
-      int stage = 0, issued = 0;
-      unsigned phase = 0;
-      bool ok = true;
-      const unsigned lead_full = PAIR ? in_cta(full, 0) : full;
-      for (int t = first_tile; t < total && ok; t += step) {
-        const Tile w = tile_at<MODE, PAIR>(a, head, t);
-        const int row = w.row + (int)rank * CTA_M;
-        ok = each_block<MODE>(a, w, spans, [&](int k, int held, int part) {
-          if (!barrier_wait(empty + 8 * stage, phase ^ 1, failed)) return false;
-          const unsigned to = ring + stage * STAGE_BYTES, tb = to + A_BYTES;
-          // a block that ends within is counted by each CTA for itself, for the warp that zeroes its end
-          const bool own = MODE == DWEIGHT && held < BK;
-          const unsigned bar = own ? partly + 8 * stage : lead_full + 8 * stage;
+    const bool elected = elect_lane();
+    int stage = 0, issued = 0;
+    unsigned phase = 0;
+    bool ok = true;
+    const unsigned lead_full = PAIR ? in_cta(full, 0) : full;
+    Tile next = first_tile < total ? tile_at<MODE, PAIR>(a, head, first_tile) : Tile{};
+    for (int t = first_tile; t < total && ok; t += step) {
+      const Tile w = next;
+      const int row = w.row + (int)rank * CTA_M, begun = issued;
+      bool looked = false;                               // where the next tile is, while there is a wait anyway
+      const auto look_ahead = [&]() {
+        looked = true;
+        if (t + step < total) next = tile_at<MODE, PAIR>(a, head, t + step);
+      };
+      ok = each_block<MODE>(a, w, spans, [&](int k, int held, int part) {
+        if (issued == begun + 3) look_ahead();
+        if (!warp_wait(empty + 8 * stage, phase ^ 1, failed)) return false;
+        const unsigned to = ring + stage * STAGE_BYTES, tb = to + A_BYTES;
+        // a block that ends within is counted by each CTA for itself, for the warp that zeroes its end
+        const bool own = MODE == DWEIGHT && held < BK;
+        const unsigned bar = own ? partly + 8 * stage : lead_full + 8 * stage;
+        if (elected) {
           if (own) barrier_expect(bar, STAGE_BYTES);
           else if (rank == 0) barrier_expect(full + 8 * stage, (PAIR ? 2 : 1) * STAGE_BYTES);
           const auto load = [&](unsigned dst, const CUtensorMap* map, int x, int y, int z) {
@@ -348,18 +367,20 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
               else load(dst, &a.b[MODE == DHIDDEN ? 0 : part], n, k, MODE == DWEIGHT ? 0 : w.e);
             }
           }
-          ++issued;
-          if (++stage == STAGES) stage = 0, phase ^= 1;
-          return true;
-        });
-      }
-      if (!ok) {                                            // nothing may land in shared memory that is no longer ours
-        const long long now = clock64();
-        while (clock64() - now < 10'000'000) __nanosleep(1000);
-      }
+        }
+        ++issued;
+        if (++stage == STAGES) stage = 0, phase ^= 1;
+        return true;
+      });
+      if (!looked) look_ahead();
+    }
+    if (!ok) {                                            // nothing may land in shared memory that is no longer ours
+      const long long now = clock64();
+      while (clock64() - now < 10'000'000) __nanosleep(1000);
     }
   } else if (warp == 1) {
-    if (lane == 0 && rank == 0) {
+    if (rank == 0) {
+      const bool elected = elect_lane();
       constexpr unsigned FORMAT = std::is_same_v<T, __half> ? 0 : 1;
       constexpr unsigned IDESC = 1u << 4 | FORMAT << 7 | FORMAT << 10 | (A_T ? 1u : 0u) << 15 | (B_T ? 1u : 0u) << 16 |
                                  (S::SUMS / 8) << 17 | (S::M / 16) << 24;
@@ -371,34 +392,42 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
         bool first = true;
         const unsigned d = tmem + slot * S::SUMS;
         ok = each_block<MODE>(a, w, spans, [&](int, int held, int) {
-          if (first && !barrier_wait(free_ + 8 * slot, slot_phase ^ 1, failed)) return false;
-          if (MODE == DWEIGHT && held < BK) {
-            if (!barrier_wait(fixed + 8 * stage, fixed_phase >> stage & 1, failed)) return false;
+          if (first && !warp_wait(free_ + 8 * slot, slot_phase ^ 1, failed)) return false;
+          const bool partial = MODE == DWEIGHT && held < BK;
+          if (partial) {
+            if (!warp_wait(fixed + 8 * stage, fixed_phase >> stage & 1, failed)) return false;
             fixed_phase ^= 1u << stage;
           } else {                                          // (blocks that end within pass `full` by)
-            if (!barrier_wait(full + 8 * stage, MODE == DWEIGHT ? full_phase >> stage & 1 : phase, failed)) return false;
+            if (!warp_wait(full + 8 * stage, MODE == DWEIGHT ? full_phase >> stage & 1 : phase, failed)) return false;
             full_phase ^= 1u << stage;
           }
           fence_after();
           const unsigned at = ring + stage * STAGE_BYTES;
           const unsigned long long da = operand(at, A_T), db = operand(at + A_BYTES, B_T);
-          const int steps = MODE == DWEIGHT ? (held + 15) / 16 : BK / 16;
-          for (int s = 0; s < steps; ++s) {
-            // 16 k: 32 bytes of a row, or 16 rows of 128 bytes
-            mma_issue<PAIR>(d, da + s * (A_T ? 2048 >> 4 : 32 >> 4), db + s * (B_T ? 2048 >> 4 : 32 >> 4), IDESC, !first || s > 0);
+          // 16 k: 32 bytes of a row, or 16 rows of 128 bytes
+          constexpr int A_STEP = A_T ? 2048 >> 4 : 32 >> 4, B_STEP = B_T ? 2048 >> 4 : 32 >> 4;
+          if (elected) {
+            mma_issue<PAIR>(d, da, db, IDESC, !first);
+            if (!partial) {
+#pragma unroll
+              for (int s = 1; s < BK / 16; ++s) mma_issue<PAIR>(d, da + s * A_STEP, db + s * B_STEP, IDESC, true);
+            } else {
+              for (int s = 1; s < (held + 15) / 16; ++s) mma_issue<PAIR>(d, da + s * A_STEP, db + s * B_STEP, IDESC, true);
+            }
+            mma_commit<PAIR>(empty + 8 * stage);
           }
+          __syncwarp();
           first = false;
-          mma_commit<PAIR>(empty + 8 * stage);
           if (++stage == STAGES) stage = 0, phase ^= 1;
           return true;
         });
         if (!first) {
-          mma_commit<PAIR>(done + 8 * slot);
+          if (elected) mma_commit<PAIR>(done + 8 * slot);
           if (++slot == 2) slot = 0, slot_phase ^= 1;
         }
       }
       if (!ok) {
-        mma_commit<PAIR>(drain);
+        if (elected) mma_commit<PAIR>(drain);
         int never = 0;
         barrier_wait(drain, 0, &never);
       }
@@ -463,21 +492,25 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
 #pragma unroll 1
         for (int c = c_begin; c < c_end; c += 16) {
           float p[16], q[16];
+          float4 gate[4];
           tmem_load16(d + c, p);
           tmem_load16(d + S::N + c, q);
           tmem_load_wait();
           __syncwarp();
 #pragma unroll
-          for (int v = 0; v < 4; ++v) {
-            *turned(turn, lane, v) = make_float4(p[4 * v], p[4 * v + 1], p[4 * v + 2], p[4 * v + 3]);
-            *turned(turn + 512, lane, v) = make_float4(q[4 * v], q[4 * v + 1], q[4 * v + 2], q[4 * v + 3]);
-          }
+          for (int v = 0; v < 4; ++v) *turned(turn, lane, v) = make_float4(p[4 * v], p[4 * v + 1], p[4 * v + 2], p[4 * v + 3]);
+          __syncwarp();
+#pragma unroll
+          for (int v = 0; v < 4; ++v) gate[v] = *turned(turn, 8 * v + t_row, t_part);
+          __syncwarp();
+#pragma unroll
+          for (int v = 0; v < 4; ++v) *turned(turn, lane, v) = make_float4(q[4 * v], q[4 * v + 1], q[4 * v + 2], q[4 * v + 3]);
           __syncwarp();
           if (w.n + c + 4 * t_part < a.I) {
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
               if (8 * v >= rows) continue;
-              const float4 g = *turned(turn, 8 * v + t_row, t_part), u = *turned(turn + 512, 8 * v + t_row, t_part);
+              const float4 g = gate[v], u = *turned(turn, 8 * v + t_row, t_part);
               const size_t to = at + (size_t)(8 * v) * a.I + c;
               *reinterpret_cast<uint2*>(static_cast<T*>(a.out[0]) + to) =
                   make_uint2(Pair<T>::from_float(activation<ACT>(g.x) * u.x, activation<ACT>(g.y) * u.y),
