@@ -268,7 +268,6 @@ struct ExpertScratch {
   size_t plan, hidden, d_gate, d_up, bytes;
 };
 ExpertScratch expert_scratch(int R, int I, int groups, bool backward);
-constexpr int EXPERT_FEW_ROWS = 64;
 cudaError_t run_expert_ffn(int R, int D, int I, int E, int groups, int dtype, int act, const void* x, const void* w_gate,
                            const void* w_up, const void* w_down, const int32_t* offsets, void* y, float* gate, float* up,
                            void* scratch, int32_t* status, cudaStream_t stream);

@@ -716,9 +716,20 @@ static cudaError_t launch_gemm(const GemmArgs& args, bool pair, int dtype, int a
   return pair ? launch_gemm<MODE, true, __half>(args, act, stream) : launch_gemm<MODE, false, __half>(args, act, stream);
 }
 
-// Tiles of pairs where the groups have 128 rows or more on the average: below, more than half of a tile of 256 rows would
-// be empty.
-static bool tiles_of_pairs(int R, int groups) { return R / CTA_M >= groups; }
+// A handful of rows for each expert: the kernel that streams the weights, once for every eight rows of an expert. (Four experts of
+// 7168 x 2048: 25 us for one row and 68 for 24, row tiles 49 and 84; from nine rows an expert on it would read weights twice, 130
+// us for 48 rows and 69. Rows may be spread unevenly, hence four, and eight more, which few experts can take.)
+static bool few_rows(int R, int E) { return R <= 4LL * E + 8; }
+
+// Tiles of pairs or of single CTAs? A pair does some 1.4 times as much as its two SMs would alone, but its tiles are four times
+// as large. Single CTAs where their tiles of every product find an SM each (one expert, 4096 x 2048, 512 rows: 39 us, pairs 45;
+// 700 rows, two rounds: 64 and 47), or where groups have less than 128 rows on the average, more than half of a tile of 256
+// rows then being empty. (Each group is taken to fill half of its last tile.)
+static bool tiles_of_pairs(int R, int D, int I, int groups) {
+  if (R / CTA_M < groups) return false;
+  const long long high = div_up(R + (long long)groups * (CTA_M / 2), CTA_M);
+  return high * div_up(I, CTA_N / 2) > sm_count() || high * div_up(D, CTA_N) > sm_count();
+}
 
 cudaError_t run_expert_ffn(int R, int D, int I, int E, int groups, int dtype, int act, const void* x, const void* w_gate,
                            const void* w_up, const void* w_down, const int32_t* offsets, void* y, float* gate, float* up,
@@ -727,7 +738,7 @@ cudaError_t run_expert_ffn(int R, int D, int I, int E, int groups, int dtype, in
   unsigned char* base = static_cast<unsigned char*>(scratch);
   void* hidden = base + at.hidden;
   cudaError_t e;
-  if (R <= EXPERT_FEW_ROWS) {
+  if (few_rows(R, E)) {
     e = run_few(R, D, I, E, groups, 0, dtype, act, x, w_gate, nullptr, w_up, nullptr, offsets, hidden, gate, up, status, false,
                 stream);
     if (e != cudaSuccess) return e;
@@ -736,7 +747,7 @@ cudaError_t run_expert_ffn(int R, int D, int I, int E, int groups, int dtype, in
   }
   EncodeFn encode;
   if ((e = encoder(&encode)) != cudaSuccess) return e;
-  const bool pair = tiles_of_pairs(R, groups);
+  const bool pair = tiles_of_pairs(R, D, I, groups);
   int4* plan = reinterpret_cast<int4*>(base + at.plan);
   GemmArgs args[2] = {};
   for (GemmArgs& g : args) {
@@ -768,7 +779,7 @@ cudaError_t run_expert_backward(int R, int D, int I, int E, int groups, int dtyp
                                 void* scratch, int32_t* status, cudaStream_t stream) {
   cudaError_t e;
   const size_t weights = (size_t)E * I * D * 2;
-  const bool pair = tiles_of_pairs(R, groups);
+  const bool pair = tiles_of_pairs(R, D, I, groups);
   if (R == 0) {                                             // no rows: no tensor maps, and gradients of nothing
     if ((e = cudaMemsetAsync(dw_gate, 0, weights, stream)) != cudaSuccess) return e;
     if ((e = cudaMemsetAsync(dw_up, 0, weights, stream)) != cudaSuccess) return e;

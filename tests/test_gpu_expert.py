@@ -140,7 +140,8 @@ def check(x, wg, wu, wd, dy, offsets, kind, train=True):
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
 @pytest.mark.parametrize("R,D,I,lengths,E", [
-    (1, 8, 8, [1], 1), (5, 16, 24, [0, 2, 3], 3), (37, 72, 200, [9, 0, 17, 11], 2), (64, 264, 136, [64], 1), (64, 128, 64, [1] * 64, 64)])
+    (1, 8, 8, [1], 1), (5, 16, 24, [0, 2, 3], 3), (37, 72, 200, [9, 0, 17, 11], 2), (64, 264, 136, [64], 1), (64, 128, 64, [1] * 64, 64),
+    (12, 200, 72, [12], 1), (40, 72, 136, [33, 0, 0, 5, 0, 2, 0, 0], 8), (40, 1000, 264, [0, 1, 0, 9, 2, 3, 0, 25], 4)])
 def test_few_rows(R, D, I, lengths, E, dtype):
     check(*inputs(R, D, I, E, TYPES[dtype], R + D), offsets_of(lengths), "silu")
 
