@@ -19,6 +19,7 @@ constexpr int SLOT_BLOCK = 64;         // sources per CTA above
 struct SlotArgs {
   int N, K, P, CS;                     // CS: CTAs of a cluster, each with a stretch of the matchings
   unsigned per_n, per_sources;         // 2^22 / N and 2^22 / (sources of a CTA), rounded up (see slot_row)
+  unsigned per_p;                      // 2^16 / P, rounded up
   bool words, quads;                   // four destinations, four choices by expert at a time
   const int32_t* demand;
   const uint8_t* perm;
@@ -40,10 +41,10 @@ constexpr int SLOT_STAGED_P = 8;
 __host__ __device__ inline int slot_staged(int P) { return P <= SLOT_STAGED_P ? SLOT_CHUNK * P : 0; }
 
 struct SlotSmem {
-  size_t pairs, received, start, len, begins, perm, source, dur, bad, seen, staged, bytes;
+  size_t pairs, received, start, len, begins, perm, source, dur, bad, seen, staged, inside, bytes;
 };
 // `sources` in this CTA (with their pairs if it walks them), and `receivers` (all of them, or none)
-__host__ __device__ inline SlotSmem slot_smem(int N, int sources, bool pairs, int receivers, int warps, int staged) {
+__host__ __device__ inline SlotSmem slot_smem(int N, int sources, bool pairs, int receivers, int warps, int staged, int inside) {
   SlotSmem m;
   size_t at = 0;
   m.pairs = at, at += pairs ? align16((size_t)sources * slot_int_stride(N) * sizeof(int2)) : 0;
@@ -57,6 +58,7 @@ __host__ __device__ inline SlotSmem slot_smem(int N, int sources, bool pairs, in
   m.bad = at, at += 16;
   m.seen = at, at += pairs ? align16((size_t)warps * slot_byte_stride(N)) : 0;
   m.staged = at, at += (size_t)warps * staged * 4;
+  m.inside = at, at += (size_t)receivers * inside * 4;
   m.bytes = at;
   return m;
 }
@@ -65,7 +67,10 @@ __host__ __device__ inline SlotSmem slot_smem(int N, int sources, bool pairs, in
 // RECEIVERS: rows and offsets are computed (all sources in one CTA).
 // SPLIT: a cluster of CTAs shares the matchings (one CTA to an SM: a receiver's gathers are then fetched one receiver ahead; with
 // several CTAs to an SM that costs more than it hides, 138 in place of 123 us for 1024 x 64 ranks).
-template <bool SOURCES, bool RECEIVERS, bool SPLIT>
+// INSIDE: the choices by expert of a pair are fetched where its source is walked (32 destinations lie in the one or two KB of a source's
+// row, 32 sources of a receiver in as many rows) and the starts within the transfer left for the receiver in shared memory, where
+// that leaves room for two CTAs on an SM: 1024 x 64 ranks x 4 experts 104 us in place of 119.
+template <bool SOURCES, bool RECEIVERS, bool SPLIT, bool INSIDE>
 __global__ void __launch_bounds__(1024) slots_kernel(const SlotArgs a) {
   extern __shared__ __align__(16) unsigned char smem[];
   const int N = a.N, P = a.P;
@@ -74,7 +79,8 @@ __global__ void __launch_bounds__(1024) slots_kernel(const SlotArgs a) {
   const size_t b = SPLIT ? blockIdx.x / a.CS : blockIdx.x;
   const int i0 = SOURCES && !RECEIVERS ? blockIdx.y * SLOT_BLOCK : 0;
   const int sources = SOURCES && !RECEIVERS ? min(SLOT_BLOCK, N - i0) : N;
-  const SlotSmem at = slot_smem(N, SOURCES && !RECEIVERS ? SLOT_BLOCK : N, SOURCES, RECEIVERS ? N : 0, blockDim.x >> 5, 0);
+  const SlotSmem at = slot_smem(N, SOURCES && !RECEIVERS ? SLOT_BLOCK : N, SOURCES, RECEIVERS ? N : 0, blockDim.x >> 5,
+                               INSIDE ? 0 : slot_staged(P), INSIDE ? SLOT_CHUNK * P : 0);
   const int IS = slot_int_stride(SOURCES && !RECEIVERS ? SLOT_BLOCK : N), BS = slot_byte_stride(N), PS = slot_int_stride(N);
   int2* pairs = reinterpret_cast<int2*>(smem + at.pairs);          // x used, y demand
   long long* received = reinterpret_cast<long long*>(smem + at.received);
@@ -107,6 +113,7 @@ __global__ void __launch_bounds__(1024) slots_kernel(const SlotArgs a) {
   }
   uint8_t* seen = smem + at.seen + warp * BS;                      // by receiver: a lane that has named it
   int* staged = reinterpret_cast<int*>(smem + at.staged) + warp * slot_staged(P);
+  int* inside = reinterpret_cast<int*>(smem + at.inside);          // [receiver][matching][expert]
   const int chunks = (a.K + SLOT_CHUNK - 1) / SLOT_CHUNK;
   const int c_begin = (int)((long long)chunks * part / a.CS), c_end = (int)((long long)chunks * (part + 1) / a.CS);
 
@@ -132,6 +139,16 @@ __global__ void __launch_bounds__(1024) slots_kernel(const SlotArgs a) {
       c_dur[threadIdx.x] = max(d, 0);
     }
   };
+  const auto fetch = [&](const int32_t* at, bool live, int (&share)[4], int e0) {
+    if (a.quads) {
+      int4 v = make_int4(0, 0, 0, 0);
+      if (live) v = *reinterpret_cast<const int4*>(at + e0);
+      share[0] = v.x, share[1] = v.y, share[2] = v.z, share[3] = v.w;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) share[e] = live && e0 + e < P ? at[e0 + e] : 0;
+    }
+  };
   // a warp per source, a lane per matching; keep = false: only the pairs' used tokens move on
   auto walk_sources = [&](int k0, bool keep) {
     const bool live = k0 + lane < count;
@@ -141,6 +158,9 @@ __global__ void __launch_bounds__(1024) slots_kernel(const SlotArgs a) {
       bad |= live && dest >= N;
       dest = ok ? dest : 0;
       const int d = ok ? c_dur[lane] : 0;
+      int share[4];
+      const int32_t* shares = INSIDE ? a.counts + (b * N + i) * ((size_t)N * P) + (size_t)dest * P : nullptr;
+      if constexpr (INSIDE) fetch(shares, ok, share, 0);
       // Do two lanes name one receiver? Each leaves its number there and looks whether it is still there. (Only then a
       // vote on equal destinations, which takes some 300 cycles for 32 different ones.)
       if (ok) seen[dest] = (uint8_t)lane;
@@ -166,6 +186,29 @@ __global__ void __launch_bounds__(1024) slots_kernel(const SlotArgs a) {
         c_len[lane * IS + i] = len;
         if constexpr (RECEIVERS) {
           if (ok) c_begins[lane * IS + dest] = len, c_source[lane * IS + dest] = (short)i;
+        }
+        if constexpr (INSIDE) {
+          int* to = inside + (dest * SLOT_CHUNK + lane) * P;
+          long long ahead = -(long long)first;
+          for (int e0 = 0; e0 < P; e0 += 4) {
+            if (e0 > 0) fetch(shares, ok, share, e0);
+            int v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              v[e] = (int)max(0LL, min(ahead, (long long)len));
+              bad |= share[e] < 0;                                 // (0 behind the last expert)
+              ahead += share[e];
+            }
+            if (!ok) continue;
+            if (a.quads) {
+              *reinterpret_cast<int4*>(to + e0) = make_int4(v[0], v[1], v[2], v[3]);
+            } else {
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (e0 + e < P) to[e0 + e] = v[e];
+            }
+          }
+          bad |= ok && ahead + first != p.y;
         }
       }
     }
@@ -235,16 +278,6 @@ __global__ void __launch_bounds__(1024) slots_kernel(const SlotArgs a) {
         int i, pair, share[4];
         const int32_t* at;
       };
-      const auto fetch = [&](const int32_t* at, bool live, int (&share)[4], int e0) {
-        if (a.quads) {
-          int4 v = make_int4(0, 0, 0, 0);
-          if (live) v = *reinterpret_cast<const int4*>(at + e0);
-          share[0] = v.x, share[1] = v.y, share[2] = v.z, share[3] = v.w;
-        } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) share[e] = live && e0 + e < P ? at[e0 + e] : 0;
-        }
-      };
       const auto meet = [&](int j) {
         Arrival r;
         r.i = j < N ? c_source[lane * IS + j] : -1;
@@ -252,7 +285,7 @@ __global__ void __launch_bounds__(1024) slots_kernel(const SlotArgs a) {
         bad |= j < N && k < count && r.i < 0;                      // no source: another receiver has two
         r.pair = 0;
         r.at = nullptr;
-        if (a.offsets != nullptr) {
+        if (!INSIDE && a.offsets != nullptr) {
           r.at = a.counts + (b * N + (live ? r.i : 0)) * ((size_t)N * P) + (size_t)(live ? j : 0) * P;
           fetch(r.at, live, r.share, 0);
           if (live) r.pair = SOURCES ? pairs[r.i * PS + j].y : D[(size_t)r.i * N + j];
@@ -285,7 +318,16 @@ __global__ void __launch_bounds__(1024) slots_kernel(const SlotArgs a) {
         __syncwarp();
         if (lane == 0) received[j] = min(run + total, 0x7fffffffLL);
         c_begins[lane * IS + j] = begins;
-        if (a.offsets != nullptr) {
+        if constexpr (INSIDE) {
+          int32_t* to = a.offsets + (b * N + j) * ((size_t)a.K * P + 1) + (size_t)k0 * P;
+          const int* from = inside + j * SLOT_CHUNK * P;
+          const unsigned some = __ballot_sync(FULL, live);
+          for (int q0 = 0; q0 < held * P; q0 += 32) {
+            const int q = q0 + lane, kk = (int)((unsigned)q * a.per_p >> 16);    // (q < 32 P, P <= 8: exact)
+            const int v = __shfl_sync(FULL, begins, kk & 31);
+            if (q < held * P) to[q] = v + ((some >> kk & 1u) ? from[q] : 0);
+          }
+        } else if (a.offsets != nullptr) {
           int32_t* to = a.offsets + (b * N + j) * ((size_t)a.K * P + 1) + (size_t)k0 * P;
           long long ahead = 0;
           for (int e0 = 0; e0 < P; e0 += 4) {
@@ -366,9 +408,9 @@ __global__ void __launch_bounds__(1024) slots_kernel(const SlotArgs a) {
   }
 }
 
-template <bool SOURCES, bool RECEIVERS, bool SPLIT>
+template <bool SOURCES, bool RECEIVERS, bool SPLIT, bool INSIDE>
 static cudaError_t launch_slots(const SlotArgs& a, dim3 grid, int warps, size_t smem, cudaStream_t stream) {
-  const auto kern = slots_kernel<SOURCES, RECEIVERS, SPLIT>;
+  const auto kern = slots_kernel<SOURCES, RECEIVERS, SPLIT, INSIDE>;
   if (cudaError_t e = permit_shared_memory(kern, smem); e != cudaSuccess) return e;
   if (a.CS > 8)                                                    // beyond what every GPU of this kind must offer
     if (cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1); e != cudaSuccess) return e;
@@ -392,23 +434,26 @@ cudaError_t run_slots(int B, int N, const int32_t* demand, int K, const uint8_t*
                       int P, const int32_t* counts, int32_t* start, int32_t* length, int32_t* row, int32_t* rows,
                       int32_t* offsets, int32_t* status, cudaStream_t stream) {
   if (offsets == nullptr) P = 0;
-  SlotArgs a{N, K, P, 1, slot_reciprocal(N), slot_reciprocal(SLOT_BLOCK), N % 4 == 0 && (reinterpret_cast<uintptr_t>(perm) & 3) == 0,
+  SlotArgs a{N, K, P, 1, slot_reciprocal(N), slot_reciprocal(SLOT_BLOCK), P > 0 ? (65536u + P - 1) / P : 0, N % 4 == 0 && (reinterpret_cast<uintptr_t>(perm) & 3) == 0,
              P % 4 == 0 && (reinterpret_cast<uintptr_t>(counts) & 15) == 0, demand, perm, dur, count, counts, start, length, row, rows,
              offsets, status};
   int warps = N >= 16 ? 16 : N < 4 ? 4 : N;
   if (N <= SLOT_FUSED_N) {
     while (a.CS < SLOT_MAX_PARTS && (long long)B * a.CS * 2 <= sm_count() && K >= 2 * a.CS * SLOT_CHUNK) a.CS *= 2;
     if (a.CS > 1 && N >= 32) warps = 32;
-    const size_t smem = slot_smem(N, N, true, N, warps, slot_staged(P)).bytes;
-    return a.CS > 1 ? launch_slots<true, true, true>(a, dim3((unsigned)(B * a.CS)), warps, smem, stream)
-                    : launch_slots<true, true, false>(a, dim3((unsigned)B), warps, smem, stream);
+    const size_t smem = slot_smem(N, N, true, N, warps, slot_staged(P), 0).bytes;
+    if (a.CS > 1) return launch_slots<true, true, true, false>(a, dim3((unsigned)(B * a.CS)), warps, smem, stream);
+    const size_t more = slot_smem(N, N, true, N, warps, 0, SLOT_CHUNK * P).bytes;
+    return P >= 1 && P <= SLOT_STAGED_P && 2 * (more + 1024) <= SMEM_LIMIT + 1024
+               ? launch_slots<true, true, false, true>(a, dim3((unsigned)B), warps, more, stream)
+               : launch_slots<true, true, false, false>(a, dim3((unsigned)B), warps, smem, stream);
   }
   cudaError_t e = cudaMemsetAsync(status, 0, (size_t)B * sizeof(int32_t), stream);
   if (e != cudaSuccess) return e;
-  e = launch_slots<true, false, false>(a, dim3((unsigned)B, (unsigned)((N + SLOT_BLOCK - 1) / SLOT_BLOCK)), warps,
-                                slot_smem(N, SLOT_BLOCK, true, 0, warps, 0).bytes, stream);
+  e = launch_slots<true, false, false, false>(a, dim3((unsigned)B, (unsigned)((N + SLOT_BLOCK - 1) / SLOT_BLOCK)), warps,
+                                slot_smem(N, SLOT_BLOCK, true, 0, warps, 0, 0).bytes, stream);
   if (e != cudaSuccess) return e;
-  return launch_slots<false, true, false>(a, dim3((unsigned)B), warps, slot_smem(N, N, false, N, warps, slot_staged(P)).bytes, stream);
+  return launch_slots<false, true, false, false>(a, dim3((unsigned)B), warps, slot_smem(N, N, false, N, warps, slot_staged(P), 0).bytes, stream);
 }
 
 }  // namespace moesched
