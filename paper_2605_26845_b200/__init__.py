@@ -638,6 +638,62 @@ def expert_matvec4(x, weight, scale, offsets, weight_up=None, scale_up=None, act
     return out
 
 
+def probe_expert(weights, tokens=(1, 16, 64, 256, 1024, 4096), act="silu", base=None, reps=20) -> dict:
+    """Compute model of the experts of one rank, measured (the paper profiles its experts, Fig. 1): the batches of expert_ffn
+    are timed for every count in `tokens`, spread evenly over the experts, and the model's curve is laid through the times: a fixed cost up
+    to a knee, linear beyond. weights = (w_gate, w_up, w_down) as expert_ffn takes them, or three (weight, scale) pairs in 4
+    bits, timed with expert_matvec4. Returns 'model' (base, or DEFAULT_MODEL, with the experts' three numbers and the bytes of a token,
+    as schedule_eval, Path and the others take it), 'tokens' and 'ns'. Synchronises: a measurement, not for a serving loop."""
+    quantised = isinstance(weights[0], (tuple, list))
+    first = weights[0][0] if quantised else weights[0]
+    typed = weights[0][1] if quantised else weights[0]
+    if not isinstance(first, torch.Tensor) or not first.is_cuda or first.dim() != 3:
+        raise MoeschedError("weights must be CUDA tensors of three dimensions, or pairs of them")
+    tokens = sorted({int(g) for g in tokens})
+    if not tokens or tokens[0] < 1:
+        raise MoeschedError("tokens must be counts of at least 1")
+    E, dev = first.shape[0], first.device
+    D = first.shape[2] * (2 if quantised else 1)
+    gen = torch.Generator(dev)
+    gen.manual_seed(0)
+    times = []
+    with torch.cuda.device(dev):
+        for g in tokens:
+            x = torch.randn((g, D), generator=gen, device=dev).to(typed.dtype)
+            offsets = torch.tensor([g * e // E for e in range(E + 1)], dtype=torch.int32, device=dev)
+            if quantised:
+                (wg, sg), (wu, su), (wd, sd) = weights
+
+                def batch():
+                    return expert_matvec4(expert_matvec4(x, wg, sg, offsets, wu, su, act=act), wd, sd, offsets)
+            else:
+                def batch():
+                    return expert_ffn(x, *weights, offsets, act=act)
+            for _ in range(3):
+                batch()
+            events = [(torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)) for _ in range(reps)]
+            for start, end in events:
+                start.record()
+                batch()
+                end.record()
+            torch.cuda.current_stream(dev).synchronize()
+            times.append(sorted(s.elapsed_time(e) for s, e in events)[reps // 2] * 1e6)
+    # of all counts as the knee the one whose curve is nearest to the times, relative to them
+    best = None
+    for knee in tokens:
+        flat = [ns for g, ns in zip(tokens, times) if g <= knee]
+        fixed = sum(flat) / len(flat)
+        beyond = [(g - knee, ns - fixed) for g, ns in zip(tokens, times) if g > knee]
+        slope = max(0.0, sum(g * ns for g, ns in beyond) / sum(g * g for g, _ in beyond)) if beyond else 0.0
+        off = sum(((fixed + max(0, g - knee) * slope) / ns - 1) ** 2 for g, ns in zip(tokens, times))
+        if best is None or off < best[0]:
+            best = off, fixed, slope, knee
+    _, fixed, slope, knee = best
+    model = dict(base or DEFAULT_MODEL, bytes_per_token=2 * D, expert_fixed_ns=round(fixed), expert_knee_tokens=knee,
+                 expert_ps_per_token=round(slope * 1000))
+    return {"model": model, "tokens": tokens, "ns": times}
+
+
 class Path:
     """The whole path for batches of one shape: greedy max-weight and BvN decomposition, both scored.
 

@@ -114,7 +114,7 @@ __global__ void __launch_bounds__(1024) slots_kernel(const SlotArgs a) {
   uint8_t* seen = smem + at.seen + warp * BS;                      // by receiver: a lane that has named it
   int* staged = reinterpret_cast<int*>(smem + at.staged) + warp * slot_staged(P);
   int* inside = reinterpret_cast<int*>(smem + at.inside);          // [receiver][matching][expert]
-  const int chunks = (a.K + SLOT_CHUNK - 1) / SLOT_CHUNK;
+  const int chunks = (a.K - 1) / SLOT_CHUNK + 1;
   const int c_begin = (int)((long long)chunks * part / a.CS), c_end = (int)((long long)chunks * (part + 1) / a.CS);
 
   auto load_chunk = [&](int k0) {
@@ -392,7 +392,7 @@ __global__ void __launch_bounds__(1024) slots_kernel(const SlotArgs a) {
     __syncthreads();
     if (threadIdx.x == 0 && part == 0) a.status[b] = any ? MOESCHED_ST_BAD_INPUT : MOESCHED_ST_OK;
     if (any) {                                                     // a rejected schedule moves nothing
-      const int k0 = c_begin * SLOT_CHUNK, k1 = min(a.K, c_end * SLOT_CHUNK);
+      const long long k0 = (long long)c_begin * SLOT_CHUNK, k1 = min((long long)a.K, (long long)c_end * SLOT_CHUNK);
       for (size_t q = (size_t)k0 * N + threadIdx.x; q < (size_t)k1 * N; q += threads) {
         const size_t g = b * a.K * N + q;
         a.start[g] = a.length[g] = a.row[g] = 0;

@@ -383,3 +383,61 @@ def test_schedules_offsets_of_a_random_demand():
     for j in (0, 5):
         R = int(slots["rows"][0, j])
         check(*inputs(R, 72, 64, 2, torch.bfloat16, j), slots["offsets"][0, j], "silu")
+
+
+def test_probed_experts_make_a_model_that_schedules_are_scored_with():
+    _, wg, wu, wd, _ = inputs(1, 256, 128, 2, torch.bfloat16, 30)
+    pairs = [quantised(2, n, k, 64, torch.bfloat16, n)[:2] for n, k in ((128, 256), (128, 256), (256, 128))]
+    d = torch.from_numpy(random_matrices(2, 8, seed=1, high=500)).cuda()
+    s = ms.mw_decompose(d, 8)
+    for weights in ((wg, wu, wd), pairs):
+        probe = ms.probe_expert(weights, tokens=(1, 8, 300), base=dict(ms.DEFAULT_MODEL, reconfig_ns=7), reps=3)
+        m = probe["model"]
+        assert probe["tokens"] == [1, 8, 300] and len(probe["ns"]) == 3 and min(probe["ns"]) > 0
+        assert m["bytes_per_token"] == 512 and m["reconfig_ns"] == 7 and m["expert_fixed_ns"] > 0
+        assert m["expert_ps_per_token"] >= 0 and m["expert_knee_tokens"] in (1, 8, 300)
+        score = ms.schedule_eval(d, s.perm, s.dur, s.count, m)
+        assert (score["status"] == 0).all() and (score["makespan_overlap_ns"] >= m["expert_fixed_ns"]).all()
+    with pytest.raises(ms.MoeschedError):
+        ms.probe_expert((wg, wu, wd), tokens=(0, 4))
+
+
+def test_two_experts_layers_in_4_bits():
+    """An expert in 4 bits is two calls: gate and up with the activation, then down."""
+    dtype, E, D, I = torch.float16, 3, 192, 128
+    rnd = Rounded(dtype)
+    x = torch.randn((11, D), generator=torch.Generator("cuda").manual_seed(2), device="cuda").to(dtype)
+    g, u, w = quantised(E, I, D, 64, dtype, 1), quantised(E, I, D, 64, dtype, 2), quantised(E, D, I, 32, dtype, 3)
+    offsets = offsets_of([2, 9, 0])
+    h = ms.expert_matvec4(x, g[0], g[1], offsets, u[0], u[1], act="gelu")
+    y = ms.expert_matvec4(h, w[0], w[1], offsets)
+    for e, s in spans(offsets, E):
+        a, b = x[s].double() @ g[2][e].T, x[s].double() @ u[2][e].T
+        ea, eb = gamma(D) * (x[s].double().abs() @ g[2][e].abs().T), gamma(D) * (x[s].double().abs() @ u[2][e].abs().T)
+        f, _ = act_of(a, "gelu")
+        v = f * b
+        ev = rnd(v, SLOPE * ea * (b.abs() + eb) + f.abs() * eb + F32 * (v.abs() + a.abs() * b.abs()))
+        want = v @ w[2][e].T
+        close(y[s], want, rnd(want, ev @ w[2][e].abs().T + gamma(I) * ((v.abs() + ev) @ w[2][e].abs().T)), "y")
+
+
+@pytest.mark.parametrize("E,per", [(600, 1), (1024, 1), (1024, 2)])
+def test_as_many_experts_as_there_may_be(E, per):
+    g = torch.Generator().manual_seed(E)
+    lengths = torch.randint(0, 3, (E * per,), generator=g).tolist()
+    R = sum(lengths)
+    assert R <= 4 * E + 8                                 # the few-row kernel; and below row tiles of the same
+    data = inputs(R, 72, 24, E, torch.bfloat16, E)
+    check(*data, offsets_of(lengths), "silu")
+    x, wg, wu, wd, dy = inputs(5 * E, 72, 24, E, torch.bfloat16, E)
+    lengths = [0] * E
+    lengths[E - 1], lengths[3] = 3 * E, 2 * E
+    check(x, wg, wu, wd, dy, offsets_of(lengths), "silu", train=False)
+    q, scale, w = quantised(E, 24, 64, 32, torch.bfloat16, E)
+    v = x[:R, :64].contiguous()
+    lengths = torch.randint(0, 3, (E * per,), generator=torch.Generator().manual_seed(E)).tolist()
+    y = ms.expert_matvec4(v, q, scale, offsets_of(lengths))
+    rnd = Rounded(torch.bfloat16)
+    for e, s in spans(offsets_of(lengths), E)[::37]:
+        want = v[s].double() @ w[e].T
+        close(y[s], want, rnd(want, gamma(64) * (v[s].double().abs() @ w[e].abs().T)), "y")

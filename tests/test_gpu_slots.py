@@ -117,8 +117,9 @@ def test_schedule_slots(N, kind):
     assert (score["unserved_tokens"] == left).all()
 
 
+@pytest.mark.parametrize("P", [3, 4])
 @pytest.mark.parametrize("B,N,K", [(1, 4, 700), (2, 8, 333), (1, 64, 500), (3, 100, 260), (1, 128, 1000), (2, 16, 64), (1, 17, 33), (40, 12, 129), (200, 6, 40)])
-def test_repeated_pairs_and_long_schedules(B, N, K):
+def test_repeated_pairs_and_long_schedules(B, N, K, P):
     """Random permutations and durations: the pairs come back in any distance, also within 32 matchings, and after they are empty."""
     rng = np.random.default_rng(K)
     D = rng.integers(0, 200, size=(B, N, N)).astype(np.int32)
@@ -129,7 +130,6 @@ def test_repeated_pairs_and_long_schedules(B, N, K):
     dur[0, 5:8] = 2 ** 31 - 1
     count = rng.integers(K - K // 4, K + 1, size=B).astype(np.int32)
     count[-1] = K
-    P = 3
     counts = split(D, P, K)
     same(ms.schedule_slots(dev(D), dev(perm), dev(dur), dev(count), dev(counts)), plain_slots(D, perm, dur, count, counts))
 
@@ -215,3 +215,29 @@ def test_on_another_stream_and_replayed_from_a_graph():
         same(r2, dict(demand=demand, counts=counts, slot=slot))
         same(got2, plain_slots(demand, *(t.cpu().numpy() for t in (s2.perm, s2.dur, s2.count)), counts))
     assert (got["rows"].sum(1) == r["demand"].sum((1, 2))).all()
+
+
+@pytest.mark.parametrize("N,P", [(5, 1), (5, 2), (64, 4), (60, 7), (16, 8), (33, 9), (7, 12), (85, 12), (128, 8), (200, 4), (200, 5), (3, 341), (1, 1024)])
+@pytest.mark.parametrize("B,K", [(2, 40), (1, 300)])
+def test_any_number_of_experts_on_a_rank(N, P, B, K):
+    rng = np.random.default_rng(N * P)
+    D = rng.integers(0, 300, size=(B, N, N)).astype(np.int32)
+    perm = np.stack([np.stack([rng.permutation(N) for _ in range(K)]) for _ in range(B)]).astype(np.uint8)
+    dur, count = rng.integers(0, 90, size=(B, K)).astype(np.int32), np.full(B, K - 3, np.int32)
+    counts = split(D, P, K)
+    want = plain_slots(D, perm, dur, count, counts)
+    same(ms.schedule_slots(dev(D), dev(perm), dev(dur), dev(count), dev(counts)), want)
+    # tensors that do not begin at 16 bytes
+    def shifted(a):
+        flat = torch.zeros(a.size + 1, dtype=dev(a).dtype, device="cuda")
+        flat[1:] = dev(a).reshape(-1)
+        return flat[1:].view(a.shape)
+    same(ms.schedule_slots(*(shifted(a) for a in (D, perm, dur, count, counts))), want)
+
+
+def test_a_batch_of_no_matrices():
+    z = torch.zeros((0, 4, 4), dtype=torch.int32, device="cuda")
+    assert ms.route_demand(torch.zeros((0, 4, 9), dtype=torch.int32, device="cuda"), 8)["demand"].shape == (0, 4, 4)
+    got = ms.schedule_slots(z, torch.zeros((0, 3, 4), dtype=torch.uint8, device="cuda"), torch.zeros((0, 3), dtype=torch.int32, device="cuda"),
+                            torch.zeros(0, dtype=torch.int32, device="cuda"), torch.zeros((0, 4, 8), dtype=torch.int32, device="cuda"))
+    assert got["offsets"].shape == (0, 4, 7)
