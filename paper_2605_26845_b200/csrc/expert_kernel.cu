@@ -146,20 +146,21 @@ __device__ __forceinline__ unsigned long long operand(unsigned addr, bool transp
 
 // ---- row tiles ------------------------------------------------------------------------------------------
 
-// Tiles of up to `high` rows of the groups, by expert, so that tiles with the same weights follow one another. One CTA.
+// Tiles of up to `high` rows of the groups, by expert, so that tiles with the same weights follow one another. One CTA, of a thread
+// for each group up to 1024.
 __global__ void __launch_bounds__(1024) plan_kernel(int R, int E, int groups, int high, const int32_t* __restrict__ offsets,
                                                     int4* __restrict__ plan, int32_t* __restrict__ status) {
   __shared__ int warp_sum[32];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, per = groups / E;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, threads = blockDim.x, per = groups / E;
   let_next_start();
   bool bad = false;
-  for (int g = threadIdx.x; g <= groups; g += 1024) {
-    const int v = offsets[g];
-    bad |= v < 0 || v > R || (g > 0 && offsets[g - 1] > v);
+  for (int g = threadIdx.x; g < groups; g += threads) {
+    const int v = offsets[g], w = offsets[g + 1];
+    bad |= v < 0 || v > w || w > R;
   }
   bad = __syncthreads_or(bad);
   int base = 0;
-  for (int q0 = 0; q0 < groups && !bad; q0 += 1024) {
+  for (int q0 = 0; q0 < groups && !bad; q0 += threads) {
     const int q = q0 + threadIdx.x, e = q / per;
     const int2 span = q < groups ? rows_of_group(offsets, (q - e * per) * E + e, R) : make_int2(0, 0);
     const int tiles = (span.y - span.x + high - 1) / high;
@@ -172,7 +173,7 @@ __global__ void __launch_bounds__(1024) plan_kernel(int R, int E, int groups, in
     if (lane == 31) warp_sum[warp] = incl;
     __syncthreads();
     int before = base, all = base;
-    for (int w = 0; w < 32; ++w) {
+    for (int w = 0; w < threads / 32; ++w) {
       before += w < warp ? warp_sum[w] : 0;
       all += warp_sum[w];
     }
@@ -716,6 +717,8 @@ static cudaError_t launch_gemm(const GemmArgs& args, bool pair, int dtype, int a
   return pair ? launch_gemm<MODE, true, __half>(args, act, stream) : launch_gemm<MODE, false, __half>(args, act, stream);
 }
 
+static int plan_threads(int groups) { return groups >= 1024 ? 1024 : (groups + 31) / 32 * 32; }
+
 // A handful of rows for each expert: the kernel that streams the weights, once for every eight rows of an expert. (Four experts of
 // 7168 x 2048: 25 us for one row and 68 for 24, row tiles 49 and 84; from nine rows an expert on it would read weights twice, 130
 // us for 48 rows and 69. Rows may be spread unevenly, hence four, and eight more, which few experts can take.)
@@ -767,7 +770,7 @@ cudaError_t run_expert_ffn(int R, int D, int I, int E, int groups, int dtype, in
   map(&args[1].b[0], w_down, I, D, E, 64);
   args[1].out[0] = y;
   if (e != cudaSuccess) return e;
-  plan_kernel<<<1, 1024, 0, stream>>>(R, E, groups, pair ? 2 * CTA_M : CTA_M, offsets, plan, status);
+  plan_kernel<<<1, plan_threads(groups), 0, stream>>>(R, E, groups, pair ? 2 * CTA_M : CTA_M, offsets, plan, status);
   if ((e = cudaGetLastError()) != cudaSuccess) return e;
   if ((e = launch_gemm<GLU>(args[0], pair, dtype, act, stream)) != cudaSuccess) return e;
   return launch_gemm<DOWN>(args[1], pair, dtype, act, stream);
@@ -784,7 +787,7 @@ cudaError_t run_expert_backward(int R, int D, int I, int E, int groups, int dtyp
     if ((e = cudaMemsetAsync(dw_gate, 0, weights, stream)) != cudaSuccess) return e;
     if ((e = cudaMemsetAsync(dw_up, 0, weights, stream)) != cudaSuccess) return e;
     if ((e = cudaMemsetAsync(dw_down, 0, weights, stream)) != cudaSuccess) return e;
-    plan_kernel<<<1, 1024, 0, stream>>>(R, E, groups, CTA_M, offsets, static_cast<int4*>(scratch), status);
+    plan_kernel<<<1, plan_threads(groups), 0, stream>>>(R, E, groups, CTA_M, offsets, static_cast<int4*>(scratch), status);
     return cudaGetLastError();
   }
   const ExpertScratch at = expert_scratch(R, I, groups, true);
@@ -820,7 +823,7 @@ cudaError_t run_expert_backward(int R, int D, int I, int E, int groups, int dtyp
   map(&args[2].b[2], hidden, I, R, 1, BK);
   args[2].out[0] = dw_gate, args[2].out[1] = dw_up, args[2].out[2] = dw_down;
   if (e != cudaSuccess) return e;
-  plan_kernel<<<1, 1024, 0, stream>>>(R, E, groups, pair ? 2 * CTA_M : CTA_M, offsets, plan, status);
+  plan_kernel<<<1, plan_threads(groups), 0, stream>>>(R, E, groups, pair ? 2 * CTA_M : CTA_M, offsets, plan, status);
   if ((e = cudaGetLastError()) != cudaSuccess) return e;
   if ((e = launch_gemm<DHIDDEN>(args[0], pair, dtype, act, stream)) != cudaSuccess) return e;
   if ((e = launch_gemm<DINPUT>(args[1], pair, dtype, act, stream)) != cudaSuccess) return e;

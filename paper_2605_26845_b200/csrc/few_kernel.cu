@@ -97,7 +97,10 @@ struct FewShape {
   // times its latency is some 43 KB
   static constexpr int STAGES = !Q4 ? 4 : GROUP == 32 ? 2 : 3;
   static constexpr int RING = FEW_WARPS * STAGES * STAGE;
-  static constexpr int SUMS = FEW_WARPS * 2 * FEW_ROWS * 16 * 4;
+  // the sums of the warps of a team: two sets where they fit, so that a warp need not wait until the others have read its last
+  static constexpr int SUM_SETS = Q4 ? 1 : 2;
+  static constexpr int SET = FEW_WARPS * 2 * FEW_ROWS * 16;       // floats: [warp][tile][token][16]
+  static constexpr int SUMS = SUM_SETS * SET * 4;
   static constexpr int SMEM = RING + SUMS + MOESCHED_MAX_EXPERTS * 2 + 64;
   static_assert(SMEM <= SMEM_LIMIT, "shared memory");
   static_assert(RING >= MOESCHED_MAX_EXPERTS * 8, "units of the experts lie in the rings at first");
@@ -328,7 +331,7 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, 1) few_kernel(const FewArgs a)
   FewCursor use = get;
 #pragma unroll 1
   for (int u = 0; u < STAGES - 1; ++u) issue();
-  int stage = 0;
+  int stage = 0, set = 0;
   for (;;) {
     float acc[2][4];
 #pragma unroll
@@ -420,7 +423,7 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, 1) few_kernel(const FewArgs a)
       __syncwarp();
     }
     // lane (gr, t) has outputs gr, gr + 8 of the tokens 2t, 2t + 1
-    float* to_sums = sums + warp * (2 * FEW_ROWS * 16);
+    float* to_sums = sums + set * Shape::SET + warp * (2 * FEW_ROWS * 16);
 #pragma unroll
     for (int m = 0; m < 2; ++m)
 #pragma unroll
@@ -428,7 +431,7 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, 1) few_kernel(const FewArgs a)
     const int team_bar = 1 + warp / split, team_threads = 32 * split;
     if (split == 1) __syncwarp();
     else asm volatile("bar.sync %0, %1;" ::"r"(team_bar), "r"(team_threads) : "memory");
-    const float* team_sums = sums + (warp - part) * (2 * FEW_ROWS * 16);
+    const float* team_sums = sums + set * Shape::SET + (warp - part) * (2 * FEW_ROWS * 16);
     for (int q = part * 32 + lane; q < FEW_ROWS * OUTPUTS; q += team_threads) {
       const int c = q % OUTPUTS, r = q / OUTPUTS, n = use.tile * OUTPUTS + c;
       const int row = __shfl_sync(FULL, use.row, r * 4 & 31);
@@ -450,8 +453,10 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, 1) few_kernel(const FewArgs a)
     }
     if (use.left == 0) break;
     next_unit(use);
-    if (split == 1) __syncwarp();                         // the sums are read before they are written again
-    else asm volatile("bar.sync %0, %1;" ::"r"(team_bar), "r"(team_threads) : "memory");
+    // the sums are read before they are written again: with two sets, by the barrier of the next unit
+    if constexpr (Shape::SUM_SETS == 2) set ^= 1;
+    else if (split > 1) asm volatile("bar.sync %0, %1;" ::"r"(team_bar), "r"(team_threads) : "memory");
+    __syncwarp();
   }
   asm volatile("cp.async.wait_group 0;" ::: "memory");
 }
@@ -485,9 +490,10 @@ cudaError_t run_few(int R, int K, int N, int E, int groups, int group, int dtype
                     float* sum_up, int32_t* status, bool early, cudaStream_t stream) {
   FewArgs a{R, K, N, E, groups, 1, x, {w, w_up}, {scale, scale_up}, offsets, y, {sum, sum_up}, status};
   const bool gated = w_up != nullptr;
-  // as few warps share the k of an output as still give every warp of the GPU a few units (which differ in length by one)
+  // Warps share the k of an output only until half of the GPU's warps have a unit: every sharing costs a barrier and a sum (four
+  // experts of 7168 x 2048 in 16 bits, 16 rows: 60 us; until all have one 64, four each 73, a quarter of them 69).
   const long long units = (long long)(E < R ? E : R) * ((N + (gated ? 15 : 31)) / (gated ? 16 : 32));
-  while (a.split < FEW_WARPS && units * a.split < 4LL * FEW_WARPS * sm_count()) a.split *= 2;
+  while (a.split < FEW_WARPS && 2 * units * a.split < (long long)FEW_WARPS * sm_count()) a.split *= 2;
   if (dtype == MOESCHED_BF16) {
     if (group == 0) return launch_few<__nv_bfloat16, 0>(a, gated, act, early, stream);
     if (group == 32) return launch_few<__nv_bfloat16, 32>(a, gated, act, early, stream);
