@@ -438,12 +438,25 @@ def best_budget(count, prefix_overlap_ns, prefix_unserved_tokens, ns_per_unserve
 MAX_EXPERTS = 1024
 
 
+try:
+    from torch._C._dynamo.guards import _empty_strided_cuda     # (an allocation on the current device, without the dispatcher)
+except ImportError:
+    _empty_strided_cuda = None
+
+
+def _allocator(device):
+    """Function of (shape, strides, dtype) that makes a tensor on `device`. (torch.empty takes 2.3 us, torch.empty_strided 1.5 and the
+    allocation underneath 0.8, which counts beside kernels of a few microseconds.)"""
+    if _empty_strided_cuda is not None and device.index == torch._C._cuda_getDevice():
+        return _empty_strided_cuda
+    return lambda shape, strides, dtype: torch.empty_strided(shape, strides, dtype=dtype, device=device)
+
+
 def _empty(dtype, device, *shape):
-    """torch.empty for a densely packed tensor of one to three dimensions. (empty_strided, and empty_like where there is a like, take
-    two thirds of its time, which counts beside kernels of a few microseconds.)"""
+    """Densely packed tensor of one to three dimensions."""
     n = len(shape)
     strides = (1,) if n == 1 else (shape[1], 1) if n == 2 else (shape[1] * shape[2], shape[2], 1)
-    return torch.empty_strided(shape, strides, dtype=dtype, device=device)
+    return _allocator(device)(shape, strides, dtype)
 
 
 def route_demand(experts, num_experts, out=None) -> dict:
@@ -457,8 +470,9 @@ def route_demand(experts, num_experts, out=None) -> dict:
     B, N, S = experts.shape
     E, dev = int(num_experts), experts.device
     if out is None:
-        out = dict(demand=_empty(torch.int32, dev, B, N, N), counts=_empty(torch.int32, dev, B, N, E), slot=torch.empty_like(experts),
-                   status=_empty(torch.int32, dev, B, N))
+        make, i32 = _allocator(dev), torch.int32
+        out = {"demand": make((B, N, N), (N * N, N, 1), i32), "counts": make((B, N, E), (N * E, E, 1), i32),
+               "slot": make((B, N, S), (N * S, S, 1), i32), "status": make((B, N), (N, 1), i32)}
     else:
         for k, shape in dict(demand=(B, N, N), counts=(B, N, E), slot=(B, N, S), status=(B, N)).items():
             if _dev(out[k], torch.int32, f"out['{k}']").shape != shape or out[k].device != dev:
@@ -478,9 +492,11 @@ def schedule_slots(demand, perm, dur, count, counts=None) -> dict:
     dur = _dev(dur, torch.int32, "dur")
     count = _dev(count, torch.int32, "count")
     B, N, _ = demand.shape
-    if perm.dim() != 3 or perm.shape[0] != B or perm.shape[2] != N or dur.shape != perm.shape[:2] or count.shape != (B,):
+    if perm.dim() != 3:
+        raise MoeschedError("perm must be [B, k_stride, N]")
+    K, P, dev = perm.shape[1], 0, demand.device
+    if N < 1 or perm.shape != (B, K, N) or dur.shape != (B, K) or count.shape != (B,):
         raise MoeschedError("perm must be [B, k_stride, N], dur [B, k_stride] and count [B]")
-    K, P, dev = int(perm.shape[1]), 0, demand.device
     if counts is not None:
         counts = _dev(counts, torch.int32, "counts")
         if counts.dim() != 3 or counts.shape[:2] != (B, N) or counts.shape[2] % N != 0:
@@ -488,13 +504,15 @@ def schedule_slots(demand, perm, dur, count, counts=None) -> dict:
         P = counts.shape[2] // N
     if perm.device != dev or dur.device != dev or count.device != dev or (counts is not None and counts.device != dev):
         raise MoeschedError("all tensors must be on one device")
-    start = _empty(torch.int32, dev, B, K, N)
-    res = dict(start=start, length=torch.empty_like(start), row=torch.empty_like(start), rows=_empty(torch.int32, dev, B, N),
-               status=torch.empty_like(count))
+    make, i32, shape, strides = _allocator(dev), torch.int32, (B, K, N), (K * N, N, 1)
+    start, length, row = make(shape, strides, i32), make(shape, strides, i32), make(shape, strides, i32)
+    rows, status = make((B, N), (N, 1), i32), make((B,), (1,), i32)
+    res = {"start": start, "length": length, "row": row, "rows": rows, "status": status}
+    offsets = None
     if counts is not None:
-        res["offsets"] = _empty(torch.int32, dev, B, N, K * P + 1)
-    _call("moesched_schedule_slots", dev, B, N, _ptr(demand), K, _ptr(perm), _ptr(dur), _ptr(count), P, _ptr(counts), _ptr(res["start"]),
-          _ptr(res["length"]), _ptr(res["row"]), _ptr(res["rows"]), _ptr(res.get("offsets")), _ptr(res["status"]))
+        res["offsets"] = offsets = make((B, N, K * P + 1), (N * (K * P + 1), K * P + 1, 1), i32)
+    _call("moesched_schedule_slots", dev, B, N, demand.data_ptr(), K, perm.data_ptr(), dur.data_ptr(), count.data_ptr(), P, _ptr(counts),
+          start.data_ptr(), length.data_ptr(), row.data_ptr(), rows.data_ptr(), _ptr(offsets), status.data_ptr())
     return res
 
 
@@ -616,25 +634,30 @@ def expert_matvec4(x, weight, scale, offsets, weight_up=None, scale_up=None, act
     """Products of a few rows with their experts' 4-bit weights: y[r, n] = sum_k (q - 8) scale[e, n, k // group] x[r, k], the q of
     k = 2m in the low half of byte m of weight [E, N, K / 2] uint8, scale [E, N, K / group] in the type of x (bfloat16
     or float16), group 32, 64 or 128. With weight_up and scale_up, act(x W^T) * (x W_up^T). Rows lie by group as in expert_ffn."""
-    if not isinstance(weight, torch.Tensor) or not isinstance(scale, torch.Tensor) or weight.dim() != 3 or scale.dim() != 3:
+    dtype, groups = _expert_rows(x, offsets, 1)
+    weight = _dev(weight, torch.uint8, "weight")
+    scale = _dev(scale, x.dtype, "scale")
+    if weight.dim() != 3 or scale.dim() != 3:
         raise MoeschedError("weight must be [E, N, K / 2] and scale [E, N, K / group]")
-    E, N = weight.shape[:2]
-    K = 2 * weight.shape[2]
-    dtype, groups = _expert_rows(x, offsets, E)
-    if K == 0 or x.shape[1] != K or scale.shape[2] == 0 or K % scale.shape[2] != 0:
+    E, N, half = weight.shape
+    R, K = x.shape
+    parts, dev = scale.shape[2], x.device
+    if half == 0 or K != 2 * half or scale.shape[:2] != (E, N) or parts == 0 or K % parts != 0:
         raise MoeschedError("x must be [R, K], weight [E, N, K / 2] and scale [E, N, K / group]")
+    if E < 1 or groups % E != 0:
+        raise MoeschedError("the groups of offsets must be a multiple of the number of experts")
     if (weight_up is None) != (scale_up is None):
         raise MoeschedError("weight_up and scale_up go together")
-    for w, s, what in ((weight, scale, ""), (weight_up, scale_up, "_up")):
-        if w is not None:
-            if _dev(w, torch.uint8, "weight" + what).shape != weight.shape or w.device != x.device:
-                raise MoeschedError("weight_up must be like weight, on the device of x")
-            _like(s, x, (E, N, scale.shape[2]), "scale" + what)
-    if offsets.device != x.device:
+    if weight.device != dev or scale.device != dev or offsets.device != dev:
         raise MoeschedError("all tensors must be on one device")
-    out = _like(out, x, (x.shape[0], N), "out")
-    _call("moesched_expert_matvec4", x.device, x.shape[0], K, N, E, groups, K // scale.shape[2], dtype, _act(act), _ptr(x), _ptr(weight),
-          _ptr(scale), _ptr(weight_up), _ptr(scale_up), _ptr(offsets), _ptr(out), _ptr(_status_of(status, x.device)))
+    if weight_up is not None:
+        if _dev(weight_up, torch.uint8, "weight_up").shape != weight.shape or weight_up.device != dev:
+            raise MoeschedError("weight_up must be like weight, on the device of x")
+        if _dev(scale_up, x.dtype, "scale_up").shape != scale.shape or scale_up.device != dev:
+            raise MoeschedError("scale_up must be like scale, on the device of x")
+    out = _like(out, x, (R, N), "out")
+    _call("moesched_expert_matvec4", dev, R, K, N, E, groups, K // parts, dtype, _act(act), x.data_ptr(), weight.data_ptr(),
+          scale.data_ptr(), _ptr(weight_up), _ptr(scale_up), offsets.data_ptr(), out.data_ptr(), _status_of(status, dev).data_ptr())
     return out
 
 
