@@ -470,14 +470,17 @@ int moesched_route_demand(int B, int N, int S, int E, const int32_t* d_experts, 
  *   d_start, d_length, d_row   out  [B][k_stride][N] int32
  *   d_rows     out  [B][N] int32
  *   d_offsets  out  [B][N][k_stride * P + 1] int32; NULL if and only if d_counts is
+ *   d_scratch  tmp  moesched_slots_scratch_bytes(B, N, k_stride) bytes (0 where none is used), or NULL: with it a long schedule of
+ *                   one of few matrices is done by many CTAs. Contents are undefined afterwards; calls that overlap need their own
  *   d_status   out  [B] int32 OK, or BAD_INPUT: a negative entry or duration, a row that is no permutation, a count out of
  *                   range, counts that do not add up to the demand of a pair that is served, or over 2^31-1 rows; all outputs of
  *                   that matrix are then 0
  */
 int moesched_schedule_slots(int B, int N, const int32_t* d_demand, int k_stride, const uint8_t* d_perm, const int32_t* d_dur,
                             const int32_t* d_count, int experts_per_rank, const int32_t* d_counts, int32_t* d_start,
-                            int32_t* d_length, int32_t* d_row, int32_t* d_rows, int32_t* d_offsets, int32_t* d_status,
-                            void* stream);
+                            int32_t* d_length, int32_t* d_row, int32_t* d_rows, int32_t* d_offsets, int32_t* d_scratch,
+                            int32_t* d_status, void* stream);
+size_t moesched_slots_scratch_bytes(int B, int N, int k_stride);
 
 /*
  * The expert batch itself: what expert_fixed_ns and expert_ps_per_token of the model stand for (paper Sec. 2.1 and Fig. 1: the

@@ -55,7 +55,7 @@ _SIGNATURES = {
     "moesched_sinkhorn_scale": "iipidipppppp", "moesched_sinkhorn_durations": "iipppipp",
     "moesched_schedule_order": "iipippp" + "p" * 8, "moesched_schedule_permute": "iiipppppp",
     "moesched_best_budget": "iipppqppp", "moesched_bvn_real_decompose": "iipdipppppppp",
-    "moesched_route_demand": "iiii" + "p" * 6, "moesched_schedule_slots": "iipipppi" + "p" * 8,
+    "moesched_route_demand": "iiii" + "p" * 6, "moesched_schedule_slots": "iipipppi" + "p" * 9,
     "moesched_expert_ffn": "i" * 7 + "p" * 11, "moesched_expert_ffn_backward": "i" * 7 + "p" * 15,
     "moesched_expert_matvec4": "i" * 8 + "p" * 9,
     "moesched_path_run": "piippip", "moesched_last_cuda_error": "",
@@ -76,6 +76,7 @@ def _open(path):
     lib.moesched_bvn_scratch_bytes.restype = ctypes.c_size_t
     lib.moesched_order_scratch_bytes.restype = ctypes.c_size_t
     lib.moesched_expert_scratch_bytes.restype = ctypes.c_size_t
+    lib.moesched_slots_scratch_bytes.restype = ctypes.c_size_t
     lib.moesched_probe_int_ops.restype = ctypes.c_longlong
     lib.moesched_debug_index_faults.restype = ctypes.c_longlong
     return lib
@@ -511,8 +512,14 @@ def schedule_slots(demand, perm, dur, count, counts=None) -> dict:
     offsets = None
     if counts is not None:
         res["offsets"] = offsets = make((B, N, K * P + 1), (N * (K * P + 1), K * P + 1, 1), i32)
+    scratch = None
+    if K > 224:                                          # (shorter schedules never use any)
+        with torch.cuda.device(dev):
+            need = int(load_library().moesched_slots_scratch_bytes(B, N, K))
+        if need:
+            scratch = make((need,), (1,), torch.uint8)
     _call("moesched_schedule_slots", dev, B, N, demand.data_ptr(), K, perm.data_ptr(), dur.data_ptr(), count.data_ptr(), P, _ptr(counts),
-          start.data_ptr(), length.data_ptr(), row.data_ptr(), rows.data_ptr(), _ptr(offsets), status.data_ptr())
+          start.data_ptr(), length.data_ptr(), row.data_ptr(), rows.data_ptr(), _ptr(offsets), _ptr(scratch), status.data_ptr())
     return res
 
 

@@ -359,20 +359,24 @@ int moesched_route_demand(int B, int N, int S, int E, const int32_t* d_experts, 
   return e == cudaSuccess ? MOESCHED_OK : fail_cuda(e);
 }
 
+size_t moesched_slots_scratch_bytes(int B, int N, int k_stride) {
+  return size_ok(B, N, k_stride) ? slots_scratch_bytes(B, N, k_stride) : 0;
+}
+
 int moesched_schedule_slots(int B, int N, const int32_t* d_demand, int k_stride, const uint8_t* d_perm, const int32_t* d_dur,
                             const int32_t* d_count, int experts_per_rank, const int32_t* d_counts, int32_t* d_start,
-                            int32_t* d_length, int32_t* d_row, int32_t* d_rows, int32_t* d_offsets, int32_t* d_status,
-                            void* stream) {
+                            int32_t* d_length, int32_t* d_row, int32_t* d_rows, int32_t* d_offsets, int32_t* d_scratch,
+                            int32_t* d_status, void* stream) {
   if (!size_ok(B, N, k_stride)) return MOESCHED_EINVAL;
   if ((d_counts == nullptr) != (d_offsets == nullptr)) return MOESCHED_EINVAL;
   if (d_counts != nullptr && (experts_per_rank < 1 || experts_per_rank > MOESCHED_MAX_EXPERTS / N)) return MOESCHED_EINVAL;
   if (B == 0) return MOESCHED_OK;
   if (!eval_pointers_ok(d_demand, d_perm, d_dur, d_count, d_status) || !d_start || !d_length || !d_row || !d_rows ||
       !aligned4(d_start) || !aligned4(d_length) || !aligned4(d_row) || !aligned4(d_rows) || !aligned4(d_counts) ||
-      !aligned4(d_offsets))
+      !aligned4(d_offsets) || !aligned4(d_scratch))
     return MOESCHED_EINVAL;
   cudaError_t e = run_slots(B, N, d_demand, k_stride, d_perm, d_dur, d_count, experts_per_rank, d_counts, d_start, d_length, d_row,
-                            d_rows, d_offsets, d_status, static_cast<cudaStream_t>(stream));
+                            d_rows, d_offsets, d_scratch, d_status, static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? MOESCHED_OK : fail_cuda(e);
 }
 

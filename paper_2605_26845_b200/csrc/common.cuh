@@ -255,7 +255,8 @@ cudaError_t run_route(int B, int N, int S, int E, const int32_t* experts, int32_
                       int32_t* status, cudaStream_t stream);
 cudaError_t run_slots(int B, int N, const int32_t* demand, int K, const uint8_t* perm, const int32_t* dur, const int32_t* count,
                       int P, const int32_t* counts, int32_t* start, int32_t* length, int32_t* row, int32_t* rows,
-                      int32_t* offsets, int32_t* status, cudaStream_t stream);
+                      int32_t* offsets, int32_t* scratch, int32_t* status, cudaStream_t stream);
+size_t slots_scratch_bytes(int B, int N, int K);
 
 // products of a few rows with their experts' weights (few_kernel.cu); group 0: weights in 16 bits; early: may be started before the
 // kernel before it is over (which is one of the same call)
@@ -289,6 +290,17 @@ void prefer_shared_memory(Kernel kern) {
 template <typename Kernel>
 cudaError_t permit_shared_memory(Kernel kern, size_t smem) {
   return smem > 48 * 1024 ? cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SMEM_LIMIT) : cudaSuccess;
+}
+
+// A kernel that follows another of the same call may be started before that one is over (start_early): it then waits itself,
+// before it touches anything the earlier one reads or writes. The earlier one says from when on that may be.
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+inline cudaLaunchAttribute start_early() {
+  cudaLaunchAttribute attr = {};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  return attr;
 }
 
 // Launch helper shared by the three kernels.

@@ -58,17 +58,6 @@ __device__ __forceinline__ void activation_slope(float a, float& value, float& s
   }
 }
 
-// A kernel that follows another of the same call may be started before that one is over (start_early): it then waits itself,
-// before it touches anything the earlier one reads or writes. The earlier one says from when on that may be.
-__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
-__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-inline cudaLaunchAttribute start_early() {
-  cudaLaunchAttribute attr = {};
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  return attr;
-}
-
 // Rows of group g, or none where the offsets are not in order: no offsets make a kernel leave its tensors.
 __device__ __forceinline__ int2 rows_of_group(const int32_t* offsets, int g, int R) {
   const int begin = offsets[g], end = offsets[g + 1];

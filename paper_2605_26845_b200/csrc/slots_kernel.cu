@@ -7,27 +7,26 @@
 // matchings at a time: a warp per source with a lane per matching (equal destinations among the 32 are summed by votes), then a warp
 // per receiver with a lane per matching and a prefix sum over the lanes, then coalesced stores by matching. The pairs'
 // `used` and demand are in shared memory. Bound by instructions and latency, not by bytes (1024 x 64 ranks x 64 matchings with
-// offsets for four experts: 104 us, the bytes 32): a step's gathers, sums and stores depend on one another.
+// offsets for four experts: 98 us, the bytes 32): a step's gathers, sums and stores depend on one another.
 #include "common.cuh"
 
 namespace moesched {
 
 constexpr int SLOT_CHUNK = 32;         // matchings per step: one per lane
 constexpr int SLOT_FUSED_N = 128;      // up to here the pairs of a whole matrix fit one CTA's shared memory
-constexpr int SLOT_MAX_PARTS = 16;     // CTAs that share the matchings of one matrix (4 x 128 ranks x 2304: 118 us, with 8 CTAs 175)
 constexpr int SLOT_BLOCK = 64;         // sources per CTA above
 
 struct SlotArgs {
-  int N, K, P, CS;                     // CS: CTAs of a cluster, each with a stretch of the matchings
+  int N, K, P, parts;                  // parts: CTAs of a matrix, each with a stretch of the matchings
   unsigned per_n, per_sources;         // 2^22 / N and 2^22 / (sources of a CTA), rounded up (see slot_row)
   unsigned per_p;                      // 2^16 / P, rounded up
-  bool words, quads;                   // four destinations, four choices by expert at a time
+  bool words, quads, rows4;            // four destinations, four choices by expert, four pairs at a time
   const int32_t* demand;
   const uint8_t* perm;
   const int32_t* dur;
   const int32_t* count;
   const int32_t* counts;               // [B][N][N * P] or NULL
-  int32_t *start, *length, *row, *rows, *offsets, *status;
+  int32_t *start, *length, *row, *rows, *offsets, *scratch, *status;
 };
 
 // strides in shared memory that put the 32 lanes' accesses to one column into different banks
@@ -64,25 +63,43 @@ __host__ __device__ inline SlotSmem slot_smem(int N, int sources, bool pairs, in
   return m;
 }
 
+// Zeroes the outputs of matrix b for matchings k0 .. k1 - 1, and what stands behind the last.
+__device__ void clear_schedule(const SlotArgs& a, size_t b, long long k0, long long k1) {
+  const int N = a.N, P = a.P;
+  for (size_t q = (size_t)k0 * N + threadIdx.x; q < (size_t)k1 * N; q += blockDim.x) {
+    const size_t g = b * a.K * N + q;
+    a.start[g] = a.length[g] = a.row[g] = 0;
+  }
+  for (int j = threadIdx.x; j < N; j += blockDim.x) {
+    if (k1 == a.K) a.rows[b * N + j] = 0;
+    if (a.offsets != nullptr) {
+      int32_t* to = a.offsets + (b * N + j) * ((size_t)a.K * P + 1);
+      for (size_t q = (size_t)k0 * P; q < (size_t)k1 * P + (k1 == a.K); ++q) to[q] = 0;
+    }
+  }
+}
+
 // SOURCES: start and length are computed (for the sources of this CTA's block); otherwise they are read back.
 // RECEIVERS: rows and offsets are computed (all sources in one CTA).
-// SPLIT: a cluster of CTAs shares the matchings (one CTA to an SM: a receiver's gathers are then fetched one receiver ahead; with
-// several CTAs to an SM that costs more than it hides, 138 in place of 123 us for 1024 x 64 ranks).
 // INSIDE: the choices by expert of a pair are fetched where its source is walked (32 destinations lie in the one or two KB of a source's
 // row, 32 sources of a receiver in as many rows) and the starts within the transfer left for the receiver in shared memory, where
-// that leaves room for two CTAs on an SM: 1024 x 64 ranks x 4 experts 104 us in place of 119.
-template <bool SOURCES, bool RECEIVERS, bool SPLIT, bool INSIDE>
+// that leaves room for two CTAs on an SM: 1024 x 64 ranks x 4 experts 104 us in place of 119 (98 with the pairs loaded four at a time).
+// PARTS: few matrices, long schedules. What a stretch of the matchings carries of each pair is walked first, for itself (without
+// RECEIVERS; into scratch[matrix][part][pair]); prefix_kernel turns that into what all stretches before it carry, min(D, sum), a cut
+// sum of cut sums; then every stretch is done as a schedule of its own that begins there. 4 x 128 ranks x 2304 matchings: 61 us; with
+// the stretches on the CTAs of a cluster, 16 at most, which exchange through shared memory, 119; in one CTA 1728.
+template <bool SOURCES, bool RECEIVERS, bool PARTS, bool INSIDE>
 __global__ void __launch_bounds__(1024) slots_kernel(const SlotArgs a) {
   extern __shared__ __align__(16) unsigned char smem[];
   const int N = a.N, P = a.P;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, threads = blockDim.x;
-  const int part = SPLIT ? blockIdx.x % a.CS : 0;   // stretch of the matchings
-  const size_t b = SPLIT ? blockIdx.x / a.CS : blockIdx.x;
-  const int i0 = SOURCES && !RECEIVERS ? blockIdx.y * SLOT_BLOCK : 0;
-  const int sources = SOURCES && !RECEIVERS ? min(SLOT_BLOCK, N - i0) : N;
-  const SlotSmem at = slot_smem(N, SOURCES && !RECEIVERS ? SLOT_BLOCK : N, SOURCES, RECEIVERS ? N : 0, blockDim.x >> 5,
+  const int part = PARTS ? blockIdx.x % a.parts : 0;   // stretch of the matchings
+  const size_t b = PARTS ? blockIdx.x / a.parts : blockIdx.x;
+  const int i0 = SOURCES && !RECEIVERS && !PARTS ? blockIdx.y * SLOT_BLOCK : 0;
+  const int sources = SOURCES && !RECEIVERS && !PARTS ? min(SLOT_BLOCK, N - i0) : N;
+  const SlotSmem at = slot_smem(N, SOURCES && !RECEIVERS && !PARTS ? SLOT_BLOCK : N, SOURCES, RECEIVERS ? N : 0, blockDim.x >> 5,
                                INSIDE ? 0 : slot_staged(P), INSIDE ? SLOT_CHUNK * P : 0);
-  const int IS = slot_int_stride(SOURCES && !RECEIVERS ? SLOT_BLOCK : N), BS = slot_byte_stride(N), PS = slot_int_stride(N);
+  const int IS = slot_int_stride(SOURCES && !RECEIVERS && !PARTS ? SLOT_BLOCK : N), BS = slot_byte_stride(N), PS = slot_int_stride(N);
   int2* pairs = reinterpret_cast<int2*>(smem + at.pairs);          // x used, y demand
   long long* received = reinterpret_cast<long long*>(smem + at.received);
   int* c_start = reinterpret_cast<int*>(smem + at.start);
@@ -101,11 +118,24 @@ __global__ void __launch_bounds__(1024) slots_kernel(const SlotArgs a) {
   const int count = bad ? 0 : count_in;
   if (threadIdx.x == 0) *bad_flag = 0;
   if constexpr (SOURCES) {
-    for (int i = warp; i < sources; i += warps) {
-      for (int j = lane; j < PS; j += 32) {
-        const int d = j < N ? D[(size_t)(i0 + i) * N + j] : 0;
-        bad |= d < 0;
-        pairs[i * PS + j] = make_int2(0, max(d, 0));
+    if (a.rows4) {
+#pragma unroll 4
+      for (int i = warp; i < sources; i += warps) {
+        for (int j = 4 * lane; j < N; j += 128) {
+          const int4 d = *reinterpret_cast<const int4*>(D + (size_t)(i0 + i) * N + j);
+          bad |= (d.x | d.y | d.z | d.w) < 0;
+          int2* to = pairs + i * PS + j;
+          to[0] = make_int2(0, max(d.x, 0)), to[1] = make_int2(0, max(d.y, 0));
+          to[2] = make_int2(0, max(d.z, 0)), to[3] = make_int2(0, max(d.w, 0));
+        }
+      }
+    } else {
+      for (int i = warp; i < sources; i += warps) {
+        for (int j = lane; j < N; j += 32) {
+          const int d = D[(size_t)(i0 + i) * N + j];
+          bad |= d < 0;
+          pairs[i * PS + j] = make_int2(0, max(d, 0));
+        }
       }
     }
   }
@@ -116,7 +146,7 @@ __global__ void __launch_bounds__(1024) slots_kernel(const SlotArgs a) {
   int* staged = reinterpret_cast<int*>(smem + at.staged) + warp * slot_staged(P);
   int* inside = reinterpret_cast<int*>(smem + at.inside);          // [receiver][matching][expert]
   const int chunks = (a.K - 1) / SLOT_CHUNK + 1;
-  const int c_begin = (int)((long long)chunks * part / a.CS), c_end = (int)((long long)chunks * (part + 1) / a.CS);
+  const int c_begin = (int)((long long)chunks * part / a.parts), c_end = (int)((long long)chunks * (part + 1) / a.parts);
 
   auto load_chunk = [&](int k0) {
     const int used_k = min(SLOT_CHUNK, count - k0);                // matchings of the chunk that count (may be negative)
@@ -215,41 +245,42 @@ __global__ void __launch_bounds__(1024) slots_kernel(const SlotArgs a) {
     }
   };
 
-  if constexpr (SPLIT) {
-    // What the stretches before this one have carried: every CTA first walks its own stretch alone, then adds up its
-    // predecessors' figures (used = min(D, sum): a cut sum of what was cut before is the cut sum).
-    __syncthreads();
-    for (int c = c_begin; c < c_end && c * SLOT_CHUNK < count && part + 1 < a.CS; ++c) {
-      load_chunk(c * SLOT_CHUNK);
+  if constexpr (PARTS) {
+    let_next_start();
+    int32_t* carried = a.scratch + (b * a.parts + part) * ((size_t)N * N);
+    if constexpr (!RECEIVERS) {
       __syncthreads();
-      walk_sources(c * SLOT_CHUNK, false);
-      __syncthreads();
-    }
-    cluster_sync_all();
-    // every CTA adds up its share of the pairs for all CTAs, two pairs at a time
-    const int quads = (N * PS + 1) / 2, q_begin = (int)((long long)quads * part / a.CS), q_end = (int)((long long)quads * (part + 1) / a.CS);
-    for (int q = q_begin + threadIdx.x; q < q_end; q += threads) {
-      unsigned lo = 0, hi = 0;
-      for (int c0 = 0; c0 < a.CS; c0 += 4) {
-        int4 v[4];
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-          if (c0 + c < a.CS) v[c] = *reinterpret_cast<const int4*>(map_to_cta(&pairs[2 * q].x, c0 + c));
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          if (c0 + c >= a.CS) break;
-          const unsigned more_lo = min(lo + (unsigned)v[c].x, (unsigned)v[c].y), more_hi = min(hi + (unsigned)v[c].z, (unsigned)v[c].w);
-          *reinterpret_cast<int4*>(map_to_cta(&pairs[2 * q].x, c0 + c)) = make_int4((int)lo, v[c].y, (int)hi, v[c].w);
-          lo = more_lo, hi = more_hi;
-        }
+      for (int c = c_begin; c < c_end && c * SLOT_CHUNK < count; ++c) {
+        load_chunk(c * SLOT_CHUNK);
+        __syncthreads();
+        walk_sources(c * SLOT_CHUNK, false);
+        __syncthreads();
       }
-    }
-    cluster_sync_all();
-    for (int q = threadIdx.x; q < N * (threads / N); q += threads) {
-      const int j = q % N, step = threads / N;
-      unsigned long long sum = 0;
-      for (int i = q / N; i < N; i += step) sum += (unsigned)pairs[i * PS + j].x;
-      atomicAdd(reinterpret_cast<unsigned long long*>(received + j), sum);
+      for (int i = warp; i < N; i += warps)
+        for (int j = lane; j < N; j += 32) carried[i * N + j] = pairs[i * PS + j].x;
+      return;                                                      // (what is wrong is found again)
+    } else {
+      wait_for_previous();
+      __syncthreads();
+      if (a.rows4) {
+#pragma unroll 4
+        for (int i = warp; i < N; i += warps)
+          if (4 * lane < N) {
+            const int4 u = *reinterpret_cast<const int4*>(carried + i * N + 4 * lane);
+            int2* to = pairs + i * PS + 4 * lane;
+            to[0].x = u.x, to[1].x = u.y, to[2].x = u.z, to[3].x = u.w;
+          }
+      } else {
+        for (int i = warp; i < N; i += warps)
+          for (int j = lane; j < N; j += 32) pairs[i * PS + j].x = carried[i * N + j];
+      }
+      __syncthreads();
+      for (int q = threadIdx.x; q < N * (threads / N); q += threads) {
+        const int j = q % N, step = threads / N;
+        unsigned long long sum = 0;
+        for (int i = q / N; i < N; i += step) sum += (unsigned)pairs[i * PS + j].x;
+        atomicAdd(reinterpret_cast<unsigned long long*>(received + j), sum);
+      }
     }
   }
 
@@ -294,10 +325,10 @@ __global__ void __launch_bounds__(1024) slots_kernel(const SlotArgs a) {
         return r;
       };
       Arrival next;
-      if constexpr (SPLIT) next = meet(warp);
+      if constexpr (PARTS) next = meet(warp);
       for (int j = warp; j < N; j += warps) {
         Arrival now;
-        if constexpr (SPLIT) now = next, next = meet(j + warps);
+        if constexpr (PARTS) now = next, next = meet(j + warps);
         else now = meet(j);
         const bool live = k < count && now.i >= 0;
         const int len = live ? c_begins[lane * IS + j] : 0, first = live ? c_start[lane * IS + now.i] : 0;
@@ -370,7 +401,7 @@ __global__ void __launch_bounds__(1024) slots_kernel(const SlotArgs a) {
   }
   if constexpr (RECEIVERS) {
     __syncthreads();
-    if (part + 1 == a.CS) {
+    if (part + 1 == a.parts) {
       for (int j = threadIdx.x; j < N; j += threads) {
         a.rows[b * N + j] = (int)received[j];
         if (a.offsets != nullptr) a.offsets[(b * N + j + 1) * ((size_t)a.K * P + 1) - 1] = (int)received[j];
@@ -379,82 +410,106 @@ __global__ void __launch_bounds__(1024) slots_kernel(const SlotArgs a) {
   }
   if (bad) *bad_flag = 1;
   __syncthreads();
-  if constexpr (!RECEIVERS) {
-    if (threadIdx.x == 0 && *bad_flag) a.status[b] = MOESCHED_ST_BAD_INPUT;   // (the receivers' kernel completes it)
-    return;
+  if constexpr (!RECEIVERS || PARTS) {
+    if (threadIdx.x == 0 && *bad_flag) a.status[b] = MOESCHED_ST_BAD_INPUT;   // (another kernel completes it)
   } else {
-    bool any = *bad_flag != 0;
-    if constexpr (SPLIT) {
-      cluster_sync_all();
-      for (int c = 0; c < a.CS; ++c) any |= *map_to_cta(bad_flag, c) != 0;
-      cluster_sync_all();                                          // nobody leaves while others read
-    }
-    if constexpr (!SOURCES) any |= a.status[b] != MOESCHED_ST_OK;
+    const bool any = *bad_flag != 0 || (!SOURCES && a.status[b] != MOESCHED_ST_OK);
     __syncthreads();
-    if (threadIdx.x == 0 && part == 0) a.status[b] = any ? MOESCHED_ST_BAD_INPUT : MOESCHED_ST_OK;
-    if (any) {                                                     // a rejected schedule moves nothing
-      const long long k0 = (long long)c_begin * SLOT_CHUNK, k1 = min((long long)a.K, (long long)c_end * SLOT_CHUNK);
-      for (size_t q = (size_t)k0 * N + threadIdx.x; q < (size_t)k1 * N; q += threads) {
-        const size_t g = b * a.K * N + q;
-        a.start[g] = a.length[g] = a.row[g] = 0;
-      }
-      for (int j = threadIdx.x; j < N; j += threads) {
-        if (part + 1 == a.CS) a.rows[b * N + j] = 0;
-        if (a.offsets != nullptr) {
-          int32_t* to = a.offsets + (b * N + j) * ((size_t)a.K * P + 1);
-          for (size_t q = (size_t)k0 * P; q < (size_t)k1 * P + (part + 1 == a.CS); ++q) to[q] = 0;
-        }
-      }
-    }
+    if (threadIdx.x == 0) a.status[b] = any ? MOESCHED_ST_BAD_INPUT : MOESCHED_ST_OK;
+    if (any) clear_schedule(a, b, 0, a.K);
   }
 }
 
-template <bool SOURCES, bool RECEIVERS, bool SPLIT, bool INSIDE>
-static cudaError_t launch_slots(const SlotArgs& a, dim3 grid, int warps, size_t smem, cudaStream_t stream) {
-  const auto kern = slots_kernel<SOURCES, RECEIVERS, SPLIT, INSIDE>;
+// See PARTS. A thread per pair; and the status that the stretches may then spoil.
+__global__ void __launch_bounds__(256) prefix_kernel(const SlotArgs a) {
+  let_next_start();
+  wait_for_previous();
+  const size_t b = blockIdx.x, pairs = (size_t)a.N * a.N;
+  const int q = blockIdx.y * 256 + threadIdx.x;
+  if (q == 0) a.status[b] = MOESCHED_ST_OK;
+  if (q >= (int)pairs) return;
+  const unsigned most = (unsigned)max(a.demand[b * pairs + q], 0);
+  int32_t* at = a.scratch + b * a.parts * pairs + q;
+  unsigned run = 0;
+  constexpr int AHEAD = 16;
+  for (int p0 = 0; p0 < a.parts; p0 += AHEAD) {
+    int v[AHEAD];
+#pragma unroll
+    for (int p = 0; p < AHEAD; ++p) v[p] = p0 + p < a.parts ? at[(p0 + p) * pairs] : 0;
+#pragma unroll
+    for (int p = 0; p < AHEAD; ++p) {
+      if (p0 + p < a.parts) at[(p0 + p) * pairs] = (int)run;
+      run = min(run + (unsigned)v[p], most);
+    }
+  }
+}
+// A rejected schedule moves nothing, whichever stretch was wrong.
+__global__ void __launch_bounds__(256) clear_kernel(const SlotArgs a) {
+  wait_for_previous();
+  const size_t b = blockIdx.x / a.parts;
+  const int part = blockIdx.x % a.parts;
+  if (a.status[b] != MOESCHED_ST_OK) clear_schedule(a, b, (long long)a.K * part / a.parts, (long long)a.K * (part + 1) / a.parts);
+}
+
+template <typename Kernel>
+static cudaError_t launch_slots(Kernel kern, const SlotArgs& a, dim3 grid, int threads, size_t smem, bool early, cudaStream_t stream) {
   if (cudaError_t e = permit_shared_memory(kern, smem); e != cudaSuccess) return e;
-  if (a.CS > 8)                                                    // beyond what every GPU of this kind must offer
-    if (cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1); e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
-  cfg.blockDim = dim3(32 * warps);
+  cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
-  if (SPLIT) {
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = a.CS;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-  }
+  cudaLaunchAttribute attr = start_early();
+  cfg.attrs = &attr;
+  cfg.numAttrs = early ? 1 : 0;
   return cudaLaunchKernelEx(&cfg, kern, a);
+}
+
+// Stretches of the matchings for a CTA each: with fewer matrices than half of the SMs and schedules of eight steps and more, as many
+// as fill the GPU once, of two steps at least. 1: a CTA does all of a schedule.
+static int slot_parts(int B, int N, int K) {
+  const long long chunks = (K - 1) / SLOT_CHUNK + 1, sms = sm_count();
+  if (N > SLOT_FUSED_N || chunks < 8 || B < 1 || 2LL * B > sms) return 1;
+  const long long fill = (sms + B - 1) / B;
+  return (int)(fill < chunks / 2 ? fill : chunks / 2);
+}
+size_t slots_scratch_bytes(int B, int N, int K) {
+  const int parts = slot_parts(B, N, K);
+  return parts > 1 ? (size_t)B * parts * N * N * sizeof(int32_t) : 0;
 }
 
 cudaError_t run_slots(int B, int N, const int32_t* demand, int K, const uint8_t* perm, const int32_t* dur, const int32_t* count,
                       int P, const int32_t* counts, int32_t* start, int32_t* length, int32_t* row, int32_t* rows,
-                      int32_t* offsets, int32_t* status, cudaStream_t stream) {
+                      int32_t* offsets, int32_t* scratch, int32_t* status, cudaStream_t stream) {
   if (offsets == nullptr) P = 0;
   SlotArgs a{N, K, P, 1, slot_reciprocal(N), slot_reciprocal(SLOT_BLOCK), P > 0 ? (65536u + P - 1) / P : 0, N % 4 == 0 && (reinterpret_cast<uintptr_t>(perm) & 3) == 0,
-             P % 4 == 0 && (reinterpret_cast<uintptr_t>(counts) & 15) == 0, demand, perm, dur, count, counts, start, length, row, rows,
-             offsets, status};
-  int warps = N >= 16 ? 16 : N < 4 ? 4 : N;
+             P % 4 == 0 && (reinterpret_cast<uintptr_t>(counts) & 15) == 0,
+             N % 4 == 0 && ((reinterpret_cast<uintptr_t>(demand) | reinterpret_cast<uintptr_t>(scratch)) & 15) == 0, demand, perm, dur, count, counts, start, length, row, rows,
+             offsets, scratch, status};
+  const int warps = N >= 16 ? 16 : N < 4 ? 4 : N;
+  cudaError_t e;
   if (N <= SLOT_FUSED_N) {
-    while (a.CS < SLOT_MAX_PARTS && (long long)B * a.CS * 2 <= sm_count() && K >= 2 * a.CS * SLOT_CHUNK) a.CS *= 2;
-    if (a.CS > 1 && N >= 32) warps = 32;
-    const size_t smem = slot_smem(N, N, true, N, warps, slot_staged(P), 0).bytes;
-    if (a.CS > 1) return launch_slots<true, true, true, false>(a, dim3((unsigned)(B * a.CS)), warps, smem, stream);
-    const size_t more = slot_smem(N, N, true, N, warps, 0, SLOT_CHUNK * P).bytes;
+    a.parts = scratch != nullptr ? slot_parts(B, N, K) : 1;
+    if (a.parts > 1) {
+      const int many = N >= 32 ? 32 : warps;
+      const dim3 grid((unsigned)(B * a.parts));
+      e = launch_slots(slots_kernel<true, false, true, false>, a, grid, 32 * many, slot_smem(N, N, true, 0, many, 0, 0).bytes, false, stream);
+      if (e == cudaSuccess) e = launch_slots(prefix_kernel, a, dim3((unsigned)B, (unsigned)((N * N + 255) / 256)), 256, 0, true, stream);
+      if (e == cudaSuccess)
+        e = launch_slots(slots_kernel<true, true, true, false>, a, grid, 32 * many, slot_smem(N, N, true, N, many, slot_staged(P), 0).bytes, true, stream);
+      return e == cudaSuccess ? launch_slots(clear_kernel, a, grid, 256, 0, true, stream) : e;
+    }
+    const size_t smem = slot_smem(N, N, true, N, warps, slot_staged(P), 0).bytes, more = slot_smem(N, N, true, N, warps, 0, SLOT_CHUNK * P).bytes;
     return P >= 1 && P <= SLOT_STAGED_P && 2 * (more + 1024) <= SMEM_LIMIT + 1024
-               ? launch_slots<true, true, false, true>(a, dim3((unsigned)B), warps, more, stream)
-               : launch_slots<true, true, false, false>(a, dim3((unsigned)B), warps, smem, stream);
+               ? launch_slots(slots_kernel<true, true, false, true>, a, dim3((unsigned)B), 32 * warps, more, false, stream)
+               : launch_slots(slots_kernel<true, true, false, false>, a, dim3((unsigned)B), 32 * warps, smem, false, stream);
   }
-  cudaError_t e = cudaMemsetAsync(status, 0, (size_t)B * sizeof(int32_t), stream);
+  if ((e = cudaMemsetAsync(status, 0, (size_t)B * sizeof(int32_t), stream)) != cudaSuccess) return e;
+  e = launch_slots(slots_kernel<true, false, false, false>, a, dim3((unsigned)B, (unsigned)((N + SLOT_BLOCK - 1) / SLOT_BLOCK)), 32 * warps,
+                   slot_smem(N, SLOT_BLOCK, true, 0, warps, 0, 0).bytes, false, stream);
   if (e != cudaSuccess) return e;
-  e = launch_slots<true, false, false, false>(a, dim3((unsigned)B, (unsigned)((N + SLOT_BLOCK - 1) / SLOT_BLOCK)), warps,
-                                slot_smem(N, SLOT_BLOCK, true, 0, warps, 0, 0).bytes, stream);
-  if (e != cudaSuccess) return e;
-  return launch_slots<false, true, false, false>(a, dim3((unsigned)B), warps, slot_smem(N, N, false, N, warps, slot_staged(P), 0).bytes, stream);
+  return launch_slots(slots_kernel<false, true, false, false>, a, dim3((unsigned)B), 32 * warps,
+                      slot_smem(N, N, false, N, warps, slot_staged(P), 0).bytes, false, stream);
 }
 
 }  // namespace moesched

@@ -31,16 +31,19 @@ def test_route_demand_checks_its_arguments(lib):
 
 def test_schedule_slots_checks_its_arguments(lib):
     def call(B=2, N=8, K=5, P=2, at=()):
-        p = A[:11]
+        p = A[:12]
         for k, v in dict(at).items():
             p[k] = v
-        return lib.moesched_schedule_slots(B, N, p[0], K, *p[1:4], P, *p[4:11], None)
+        return lib.moesched_schedule_slots(B, N, p[0], K, *p[1:4], P, *p[4:12], None)
 
     for bad in (dict(B=-1), dict(N=0), dict(N=257), dict(K=0), dict(P=0), dict(P=129)):
         assert call(**bad) == -1, bad
-    for k in range(11):
-        assert call(at={k: None}) == -1, k
+    for k in range(12):
+        assert k == 10 or call(at={k: None}) == -1, k             # (no scratch is needed)
         assert k == 1 or call(at={k: A[k] + 2}) == -1, k
+    assert lib.moesched_slots_scratch_bytes(2, 0, 5000) == lib.moesched_slots_scratch_bytes(-1, 8, 5000) == lib.moesched_slots_scratch_bytes(2, 8, 0) == 0
+    assert lib.moesched_slots_scratch_bytes(2, 8, 30) == lib.moesched_slots_scratch_bytes(500, 8, 3000) == lib.moesched_slots_scratch_bytes(2, 129, 3000) == 0
+    assert lib.moesched_slots_scratch_bytes(2, 8, 640) == 2 * 10 * 64 * 4
     assert call(B=0) == 0
     assert call(B=0, P=0, at={4: None, 9: None}) == 0
 
