@@ -38,7 +38,7 @@ constexpr int TURN_BYTES = 32 * 16 * 4;                    // of a warp that emp
 constexpr int RASTER_ROWS = 2048;                          // rows of row tiles that share a pass over the columns
 
 struct alignas(64) GemmArgs {
-  CUtensorMap a[3], b[3];
+  CUtensorMap a[3], b[3];                                  // (GLU: b[2] and a[1] are Wg and Wu in boxes of 32 rows)
   const int4* plan;                                        // {tiles, ok, -, -}, then {first row, rows, expert, -} of every tile
   const int32_t* offsets;
   int R, D, I, E, groups;
@@ -196,6 +196,7 @@ __global__ void __launch_bounds__(1024) plan_kernel(int R, int E, int groups, in
 struct Tile {
   int row, rows, e, n;      // first row of the result and rows, expert, first column
   int which;                // DWEIGHT: 0 gate, 1 up, 2 down
+  bool narrow;              // half of a tile's columns
 };
 // a tile of MODE is M rows high and N columns wide; GLU's are made of as many products again
 template <int MODE, bool PAIR>
@@ -214,10 +215,20 @@ __device__ __forceinline__ int tile_total(const GemmArgs& a, const int4 head) {
     return head.x * (int)div_up(MODE == GLU || MODE == DHIDDEN ? a.I : a.D, S::N);
   }
 }
+// Of `total` tiles for `step` CTAs or pairs, those of a last, or only, round that at most half of them would have are cut in two:
+// tiles up to `whole` are whole, the others come as halves. (DWEIGHT's tiles have short contractions, or many rounds.)
 template <int MODE, bool PAIR>
-__device__ __forceinline__ Tile tile_at(const GemmArgs& a, const int4 head, int t) {
+__device__ __forceinline__ int whole_tiles(int total, int step) {
+  const int last = total % step;
+  return MODE != DWEIGHT && 2 * last <= step ? total - last : total;
+}
+template <int MODE, bool PAIR>
+__device__ __forceinline__ Tile tile_at(const GemmArgs& a, const int4 head, int t, int whole) {
   using S = Shape<MODE, PAIR>;
   Tile w;
+  w.narrow = t >= whole;
+  const int second = w.narrow ? (t - whole) & 1 : 0;
+  if (w.narrow) t = whole + (t - whole) / 2;
   if constexpr (MODE == DWEIGHT) {
     const int gu = (int)(div_up(a.I, S::M) * div_up(a.D, S::N)), dn = (int)(div_up(a.D, S::M) * div_up(a.I, S::N));
     const int each = 2 * gu + dn;
@@ -235,7 +246,7 @@ __device__ __forceinline__ Tile tile_at(const GemmArgs& a, const int4 head, int 
     const int block = t / (RASTER * n_tiles), first = block * RASTER, high = min(RASTER, head.x - first);
     t -= first * n_tiles;
     const int4 row = a.plan[1 + first + t % high];
-    w.row = row.x, w.rows = row.y, w.e = row.z, w.n = t / high * S::N, w.which = 0;
+    w.row = row.x, w.rows = row.y, w.e = row.z, w.n = t / high * S::N + second * (S::N / 2), w.which = 0;
   }
   return w;
 }
@@ -323,7 +334,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
   const unsigned tmem = *reinterpret_cast<volatile unsigned*>(words + 1);
   wait_for_previous();                                     // nothing of other kernels is read, and nothing written, before
   const int4 head = a.plan[0];
-  const int total = tile_total<MODE, PAIR>(a, head);
+  const int tiles = tile_total<MODE, PAIR>(a, head), whole = whole_tiles<MODE, PAIR>(tiles, step), total = 2 * tiles - whole;
 
   if (warp == 0) {
     const bool elected = elect_lane();
@@ -331,14 +342,14 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
     unsigned phase = 0;
     bool ok = true;
     const unsigned lead_full = PAIR ? in_cta(full, 0) : full;
-    Tile next = first_tile < total ? tile_at<MODE, PAIR>(a, head, first_tile) : Tile{};
+    Tile next = first_tile < total ? tile_at<MODE, PAIR>(a, head, first_tile, whole) : Tile{};
     for (int t = first_tile; t < total && ok; t += step) {
       const Tile w = next;
       const int row = w.row + (int)rank * CTA_M, begun = issued;
       bool looked = false;                               // where the next tile is, while there is a wait anyway
       const auto look_ahead = [&]() {
         looked = true;
-        if (t + step < total) next = tile_at<MODE, PAIR>(a, head, t + step);
+        if (t + step < total) next = tile_at<MODE, PAIR>(a, head, t + step, whole);
       };
       ok = each_block<MODE>(a, w, spans, [&](int k, int held, int part) {
         if (issued == begun + 3) look_ahead();
@@ -349,7 +360,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
         const unsigned bar = own ? partly + 8 * stage : lead_full + 8 * stage;
         if (elected) {
           if (own) barrier_expect(bar, STAGE_BYTES);
-          else if (rank == 0) barrier_expect(full + 8 * stage, (PAIR ? 2 : 1) * STAGE_BYTES);
+          else if (rank == 0) barrier_expect(full + 8 * stage, (PAIR ? 2 : 1) * (w.narrow ? STAGE_BYTES - B_BYTES / 2 : STAGE_BYTES));
           const auto load = [&](unsigned dst, const CUtensorMap* map, int x, int y, int z) {
             if (PAIR && !own) tma_load_pair(dst, map, bar, x, y, z);
             else tma_load(dst, map, bar, x, y, z);
@@ -361,12 +372,19 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
           }
 #pragma unroll
           for (int q = 0; q < 2; ++q) {
+            if (q == 1 && w.narrow) break;
             const unsigned dst = tb + q * BOX_BYTES;
             if constexpr (MODE == GLU) {                   // a pair: a of the first CTA, u of the second
-              if constexpr (PAIR) load(dst, &a.b[rank], k, w.n + 64 * q, w.e);
-              else load(dst, &a.b[q], k, w.n, w.e);
+              if constexpr (PAIR) {
+                load(dst, &a.b[rank], k, w.n + 64 * q, w.e);
+              } else if (w.narrow) {
+                load(tb, &a.b[2], k, w.n, w.e);
+                load(tb + BOX_BYTES / 2, &a.a[1], k, w.n, w.e);
+              } else {
+                load(dst, &a.b[q], k, w.n, w.e);
+              }
             } else {
-              const int n = w.n + (int)rank * CTA_N + 64 * q;
+              const int n = w.n + (int)rank * (w.narrow ? CTA_N / 2 : CTA_N) + 64 * q;
               if constexpr (MODE == DOWN) load(dst, &a.b[0], k, n, w.e);
               else load(dst, &a.b[MODE == DHIDDEN ? 0 : part], n, k, MODE == DWEIGHT ? 0 : w.e);
             }
@@ -387,14 +405,14 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
       const bool elected = elect_lane();
       constexpr unsigned FORMAT = std::is_same_v<T, __half> ? 0 : 1;
       constexpr unsigned IDESC = 1u << 4 | FORMAT << 7 | FORMAT << 10 | (A_T ? 1u : 0u) << 15 | (B_T ? 1u : 0u) << 16 |
-                                 (S::SUMS / 8) << 17 | (S::M / 16) << 24;
+                                 (S::SUMS / 8) << 17 | (S::M / 16) << 24, NARROW = IDESC - ((S::SUMS / 16) << 17);
       int stage = 0, slot = 0;
       unsigned phase = 0, slot_phase = 0, fixed_phase = 0, full_phase = 0;
       bool ok = true;
       for (int t = first_tile; t < total && ok; t += step) {
-        const Tile w = tile_at<MODE, PAIR>(a, head, t);
+        const Tile w = tile_at<MODE, PAIR>(a, head, t, whole);
         bool first = true;
-        const unsigned d = tmem + slot * S::SUMS;
+        const unsigned d = tmem + slot * S::SUMS, idesc = w.narrow ? NARROW : IDESC;
         ok = each_block<MODE>(a, w, spans, [&](int, int held, int) {
           if (first && !warp_wait(free_ + 8 * slot, slot_phase ^ 1, failed)) return false;
           const bool partial = MODE == DWEIGHT && held < BK;
@@ -411,12 +429,12 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
           // 16 k: 32 bytes of a row, or 16 rows of 128 bytes
           constexpr int A_STEP = A_T ? 2048 >> 4 : 32 >> 4, B_STEP = B_T ? 2048 >> 4 : 32 >> 4;
           if (elected) {
-            mma_issue<PAIR>(d, da, db, IDESC, !first);
+            mma_issue<PAIR>(d, da, db, idesc, !first);
             if (!partial) {
 #pragma unroll
-              for (int s = 1; s < BK / 16; ++s) mma_issue<PAIR>(d, da + s * A_STEP, db + s * B_STEP, IDESC, true);
+              for (int s = 1; s < BK / 16; ++s) mma_issue<PAIR>(d, da + s * A_STEP, db + s * B_STEP, idesc, true);
             } else {
-              for (int s = 1; s < (held + 15) / 16; ++s) mma_issue<PAIR>(d, da + s * A_STEP, db + s * B_STEP, IDESC, true);
+              for (int s = 1; s < (held + 15) / 16; ++s) mma_issue<PAIR>(d, da + s * A_STEP, db + s * B_STEP, idesc, true);
             }
             mma_commit<PAIR>(empty + 8 * stage);
           }
@@ -443,7 +461,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
       bool ok = true;
       const unsigned lead_fixed = PAIR ? in_cta(fixed, 0) : fixed;
       for (int t = first_tile; t < total && ok; t += step) {
-        const Tile w = tile_at<MODE, PAIR>(a, head, t);
+        const Tile w = tile_at<MODE, PAIR>(a, head, t, whole);
         ok = each_block<MODE>(a, w, spans, [&](int, int held, int) {
           if (held < BK) {
             if (!__all_sync(FULL, barrier_wait(partly + 8 * stage, part_phase >> stage & 1, failed))) return false;
@@ -467,7 +485,6 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
     }
   } else if (warp >= 4) {
     const int quarter = warp & 3, half = (warp - 4) >> 2;  // lanes of tensor memory, and which half of the columns
-    const int c_begin = half * (S::N / 2), c_end = c_begin + S::N / 2;
     const unsigned mine = tmem + ((unsigned)quarter << 21);
     const unsigned lead_free = PAIR ? in_cta(free_, 0) : free_;
     float* turn = reinterpret_cast<float*>(smem + STAGES * STAGE_BYTES + (warp - 4) * TURN_BYTES);
@@ -476,10 +493,11 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
     int slot = 0;
     unsigned slot_phase = 0;
     for (int t = first_tile; t < total; t += step) {
-      const Tile w = tile_at<MODE, PAIR>(a, head, t);
+      const Tile w = tile_at<MODE, PAIR>(a, head, t, whole);
       const int row = w.row + (int)rank * CTA_M + quarter * 32 + t_row;       // of round 0
       const int rows = w.rows - ((int)rank * CTA_M + quarter * 32 + t_row);  // round q is inside if 8 q < rows
       const unsigned d = mine + slot * S::SUMS;
+      const int columns = w.narrow ? S::N / 2 : S::N, c_begin = half * (columns / 2), c_end = c_begin + columns / 2;
       bool any = true;
       if constexpr (MODE == DWEIGHT) {
         any = false;
@@ -498,7 +516,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
           float p[16], q[16];
           float4 gate[4];
           tmem_load16(d + c, p);
-          tmem_load16(d + S::N + c, q);
+          tmem_load16(d + columns + c, q);
           tmem_load_wait();
           __syncwarp();
 #pragma unroll
@@ -700,7 +718,8 @@ static cudaError_t launch_gemm(const GemmArgs& args, int act, cudaStream_t strea
     tiles = ((long long)args.R / S::M + (args.groups < args.R ? args.groups : args.R)) * div_up(MODE == GLU || MODE == DHIDDEN ? args.I : args.D, S::N);
   const long long most = PAIR ? sm_count() / 2 : sm_count();
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)((tiles < most ? tiles : most) * (PAIR ? 2 : 1)));
+  const long long units = MODE == DWEIGHT ? tiles : 2 * tiles;   // (halves)
+  cfg.gridDim = dim3((unsigned)((units < most ? units : most) * (PAIR ? 2 : 1)));
   cfg.blockDim = dim3(GEMM_THREADS);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
@@ -768,6 +787,10 @@ cudaError_t run_expert_ffn(int R, int D, int I, int E, int groups, int dtype, in
   map(&args[0].a[0], x, D, R, 1, CTA_M);
   map(&args[0].b[0], w_gate, D, I, E, 64);
   map(&args[0].b[1], w_up, D, I, E, 64);
+  if (!pair) {
+    map(&args[0].b[2], w_gate, D, I, E, 32);
+    map(&args[0].a[1], w_up, D, I, E, 32);
+  }
   args[0].out[0] = hidden, args[0].keep[0] = gate, args[0].keep[1] = up;
   map(&args[1].a[0], hidden, I, R, 1, CTA_M);
   map(&args[1].b[0], w_down, I, D, E, 64);

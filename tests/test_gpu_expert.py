@@ -150,7 +150,8 @@ def test_few_rows(R, D, I, lengths, E, dtype):
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
 @pytest.mark.parametrize("R,D,I,lengths,E", [
     (128, 64, 128, [128], 1), (129, 128, 256, [129], 1), (65, 8, 8, [65], 1), (200, 72, 40, [1, 127, 72], 3), (300, 200, 264, [0, 299, 0, 1], 4),
-    (257, 1000, 136, [100, 7, 0, 50, 93, 7], 2), (400, 264, 520, [63, 64, 65, 66, 17, 15, 16, 94], 4), (3001, 512, 384, [1500, 1, 0, 1500], 2)])
+    (257, 1000, 136, [100, 7, 0, 50, 93, 7], 2), (400, 264, 520, [63, 64, 65, 66, 17, 15, 16, 94], 4), (3001, 512, 384, [1500, 1, 0, 1500], 2),
+    (33, 1032, 1032, [0, 33], 2), (150, 2056, 712, [150], 1), (300, 1024, 520, [1, 128, 0, 171], 4), (100, 520, 1024, [60, 40], 1)])
 def test_row_tiles(R, D, I, lengths, E, dtype, kind):
     check(*inputs(R, D, I, E, TYPES[dtype], R + I), offsets_of(lengths), kind)
 
