@@ -59,8 +59,17 @@ __device__ __forceinline__ void barrier_expect(unsigned bar, unsigned bytes) {
 __device__ __forceinline__ void barrier_arrive(unsigned bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
-// Waits for the phase, but not for ever: false if it gave up, or if somebody else of the CTA has (a bug, never an input).
+// whether the phase is over: a look that does not wait
+__device__ __forceinline__ unsigned barrier_passed(unsigned bar, unsigned parity) {
+  unsigned done;
+  asm volatile("{\n.reg .pred p;\nmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+               : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+  return done;
+}
+// Waits for the phase, but not for ever: false if it gave up, or if somebody else of the CTA has (a bug, never an input). The look
+// comes first because a wait takes 200 cycles even where there is nothing to wait for, and the look 100.
 __device__ __forceinline__ bool barrier_wait(unsigned bar, unsigned parity, volatile int* failed) {
+  if (barrier_passed(bar, parity)) return true;
   for (int tries = 0; tries < (1 << 22); ++tries) {
     unsigned done;                                         // (waits for a microsecond at most)
     asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\nselp.u32 %0, 1, 0, p;\n}"
@@ -408,7 +417,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
                                  (S::SUMS / 8) << 17 | (S::M / 16) << 24, NARROW = IDESC - ((S::SUMS / 16) << 17);
       int stage = 0, slot = 0;
       unsigned phase = 0, slot_phase = 0, fixed_phase = 0, full_phase = 0;
-      bool ok = true;
+      bool ok = true, ready = false;                       // ready: the next block's operands have been seen there
       for (int t = first_tile; t < total && ok; t += step) {
         const Tile w = tile_at<MODE, PAIR>(a, head, t, whole);
         bool first = true;
@@ -420,10 +429,14 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
             if (!warp_wait(fixed + 8 * stage, fixed_phase >> stage & 1, failed)) return false;
             fixed_phase ^= 1u << stage;
           } else {                                          // (blocks that end within pass `full` by)
-            if (!warp_wait(full + 8 * stage, MODE == DWEIGHT ? full_phase >> stage & 1 : phase, failed)) return false;
+            if (!ready && !warp_wait(full + 8 * stage, MODE == DWEIGHT ? full_phase >> stage & 1 : phase, failed)) return false;
             full_phase ^= 1u << stage;
           }
           fence_after();
+          // the look at the next block's operands takes its 100 cycles while this block's products are issued, which with the
+          // waits is all that bounds a CTA's only tile (DWEIGHT's next block may be another warp's to finish first)
+          const int then = stage + 1 == STAGES ? 0 : stage + 1;
+          const unsigned seen = MODE == DWEIGHT ? 0 : barrier_passed(full + 8 * then, then ? phase : phase ^ 1);
           const unsigned at = ring + stage * STAGE_BYTES;
           const unsigned long long da = operand(at, A_T), db = operand(at + A_BYTES, B_T);
           // 16 k: 32 bytes of a row, or 16 rows of 128 bytes
@@ -439,6 +452,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
             mma_commit<PAIR>(empty + 8 * stage);
           }
           __syncwarp();
+          ready = __all_sync(FULL, seen);
           first = false;
           if (++stage == STAGES) stage = 0, phase ^= 1;
           return true;
