@@ -487,11 +487,14 @@ size_t moesched_slots_scratch_bytes(int B, int N, int k_stride);
  * time of an expert's feed-forward block against the tokens that it gets).
  *
  * Rows (tokens) lie by group: group g = rows d_offsets[g] .. d_offsets[g + 1] - 1 of the [R] rows, and belongs to expert g % E.
- * `groups` is a multiple of E: E for one batch, K * E for what K matchings brought (moesched_schedule_slots writes such offsets).
+ * `groups` is a multiple of E: E for one batch, K * E for what K matchings brought (moesched_schedule_slots writes such offsets);
+ * at most MOESCHED_MAX_GROUPS, and MOESCHED_MAX_ROWS rows. Outputs and scratch overlap neither one another nor an input.
  * Groups may be empty. Rows before the first and behind the last group are neither used nor written. Tensors are densely
  * packed, row major, 16-byte aligned, all of one type, MOESCHED_BF16 or MOESCHED_FP16; products are summed in 32 bits.
  * Values beyond the type's range become infinities.
  */
+#define MOESCHED_MAX_ROWS (1 << 30)
+#define MOESCHED_MAX_GROUPS (1 << 24)
 #define MOESCHED_BF16 0
 #define MOESCHED_FP16 1
 #define MOESCHED_ACT_SILU 0 /* a / (1 + exp(-a)) */

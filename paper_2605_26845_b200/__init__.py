@@ -445,6 +445,9 @@ except ImportError:
     _empty_strided_cuda = None
 
 
+_INT_MAX = 0x7fffffff                                    # (the binding of the C entry points cuts longer numbers off)
+
+
 def _allocator(device):
     """Function of (shape, strides, dtype) that makes a tensor on `device`. (torch.empty takes 2.3 us, torch.empty_strided 1.5 and the
     allocation underneath 0.8, which counts beside kernels of a few microseconds.)"""
@@ -470,6 +473,8 @@ def route_demand(experts, num_experts, out=None) -> dict:
         raise MoeschedError("experts must have shape [B, N, S]")
     B, N, S = experts.shape
     E, dev = int(num_experts), experts.device
+    if not N <= E <= 1024 or E % N != 0 or max(B, S) > _INT_MAX:
+        raise MoeschedError("num_experts must be a multiple of N and 1024 at most, B and S less than 2^31")
     if out is None:
         make, i32 = _allocator(dev), torch.int32
         out = {"demand": make((B, N, N), (N * N, N, 1), i32), "counts": make((B, N, E), (N * E, E, 1), i32),
@@ -496,6 +501,8 @@ def schedule_slots(demand, perm, dur, count, counts=None) -> dict:
     if perm.dim() != 3:
         raise MoeschedError("perm must be [B, k_stride, N]")
     K, P, dev = perm.shape[1], 0, demand.device
+    if max(B, K) > _INT_MAX:
+        raise MoeschedError("B and k_stride must be less than 2^31")
     if N < 1 or perm.shape != (B, K, N) or dur.shape != (B, K) or count.shape != (B,):
         raise MoeschedError("perm must be [B, k_stride, N], dur [B, k_stride] and count [B]")
     if counts is not None:
@@ -524,6 +531,7 @@ def schedule_slots(demand, perm, dur, count, counts=None) -> dict:
 
 
 _ACTS = {"silu": 0, "gelu": 1}
+_MAX_ROWS, _MAX_GROUPS = 1 << 30, 1 << 24
 _TYPES = {torch.bfloat16: 0, torch.float16: 1}
 
 
@@ -542,6 +550,8 @@ def _expert_rows(x, offsets, num_experts):
     groups = offsets.numel() - 1
     if x.dim() != 2 or offsets.dim() != 1 or num_experts < 1 or groups < 1 or groups % num_experts != 0:
         raise MoeschedError("x must be [R, width] and offsets [groups + 1], groups a multiple of the number of experts")
+    if x.shape[0] > _MAX_ROWS or groups > _MAX_GROUPS:
+        raise MoeschedError("at most 2^30 rows and 2^24 groups")
     return _TYPES[x.dtype], groups
 
 
@@ -590,7 +600,10 @@ def _expert_scratch(scratch, x, I, groups, backward):
 
 def expert_scratch_bytes(rows, width, groups, backward=False) -> int:
     """Working memory of expert_ffn (or its backward pass) for that many rows, a hidden width of `width` and `groups` groups."""
-    return int(load_library().moesched_expert_scratch_bytes(int(rows), int(width), int(groups), int(backward)))
+    rows, width, groups = int(rows), int(width), int(groups)
+    if max(rows, width, groups) > _INT_MAX:              # (the library answers the others)
+        return 0
+    return int(load_library().moesched_expert_scratch_bytes(rows, width, groups, int(backward)))
 
 
 def expert_ffn(x, w_gate, w_up, w_down, offsets, act="silu", save=False, out=None, scratch=None, status=None):
@@ -651,8 +664,8 @@ def expert_matvec4(x, weight, scale, offsets, weight_up=None, scale_up=None, act
     parts, dev = scale.shape[2], x.device
     if half == 0 or K != 2 * half or scale.shape[:2] != (E, N) or parts == 0 or K % parts != 0:
         raise MoeschedError("x must be [R, K], weight [E, N, K / 2] and scale [E, N, K / group]")
-    if E < 1 or groups % E != 0:
-        raise MoeschedError("the groups of offsets must be a multiple of the number of experts")
+    if E < 1 or groups % E != 0 or max(N, K) > 1 << 24:
+        raise MoeschedError("the groups of offsets must be a multiple of the number of experts, N and K 2^24 at most")
     if (weight_up is None) != (scale_up is None):
         raise MoeschedError("weight_up and scale_up go together")
     if weight.device != dev or scale.device != dev or offsets.device != dev:
@@ -680,8 +693,8 @@ def probe_expert(weights, tokens=(1, 16, 64, 256, 1024, 4096), act="silu", base=
     if not isinstance(first, torch.Tensor) or not first.is_cuda or first.dim() != 3:
         raise MoeschedError("weights must be CUDA tensors of three dimensions, or pairs of them")
     tokens = sorted({int(g) for g in tokens})
-    if not tokens or tokens[0] < 1:
-        raise MoeschedError("tokens must be counts of at least 1")
+    if not tokens or tokens[0] < 1 or reps < 1:
+        raise MoeschedError("tokens must be counts of at least 1, reps at least 1")
     E, dev = first.shape[0], first.device
     D = first.shape[2] * (2 if quantised else 1)
     gen = torch.Generator(dev)

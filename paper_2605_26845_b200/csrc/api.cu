@@ -75,7 +75,7 @@ static bool eval_pointers_ok(const void* demand, const void* perm, const void* d
 }
 
 static bool expert_sizes_ok(int R, int E, int groups, int dtype, int act) {
-  return R >= 0 && E >= 1 && E <= MOESCHED_MAX_EXPERTS && groups >= E && groups % E == 0 && groups <= (1 << 24) &&
+  return R >= 0 && R <= MOESCHED_MAX_ROWS && E >= 1 && E <= MOESCHED_MAX_EXPERTS && groups >= E && groups % E == 0 && groups <= MOESCHED_MAX_GROUPS &&
          (dtype == MOESCHED_BF16 || dtype == MOESCHED_FP16) && (act == MOESCHED_ACT_SILU || act == MOESCHED_ACT_GELU);
 }
 static bool ffn_width_ok(int v) { return v >= 8 && v <= 65536 && v % 8 == 0; }
@@ -381,7 +381,7 @@ int moesched_schedule_slots(int B, int N, const int32_t* d_demand, int k_stride,
 }
 
 size_t moesched_expert_scratch_bytes(int R, int I, int groups, int backward) {
-  if (R < 0 || !ffn_width_ok(I) || groups < 1 || groups > (1 << 24)) return 0;
+  if (R < 0 || R > MOESCHED_MAX_ROWS || !ffn_width_ok(I) || groups < 1 || groups > MOESCHED_MAX_GROUPS) return 0;
   return expert_scratch(R, I, groups, backward != 0).bytes;
 }
 

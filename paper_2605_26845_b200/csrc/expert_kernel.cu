@@ -68,9 +68,9 @@ __device__ __forceinline__ unsigned barrier_passed(unsigned bar, unsigned parity
 }
 // Waits for the phase, but not for ever: false if it gave up, or if somebody else of the CTA has (a bug, never an input). The look
 // comes first because a wait takes 200 cycles even where there is nothing to wait for, and the look 100.
-__device__ __forceinline__ bool barrier_wait(unsigned bar, unsigned parity, volatile int* failed) {
+__device__ __forceinline__ bool barrier_wait(unsigned bar, unsigned parity, volatile int* failed, int most) {
   if (barrier_passed(bar, parity)) return true;
-  for (int tries = 0; tries < (1 << 22); ++tries) {
+  for (int tries = 0; tries < most; ++tries) {
     unsigned done;                                         // (waits for a microsecond at most)
     asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\nselp.u32 %0, 1, 0, p;\n}"
                  : "=r"(done) : "r"(bar), "r"(parity), "r"(1000u) : "memory");
@@ -83,8 +83,8 @@ __device__ __forceinline__ bool barrier_wait(unsigned bar, unsigned parity, vola
 // For a whole warp: what follows is the same for all lanes, and the compiler sees it. (The descriptors of matrix instructions and
 // copies are read from the warp's common registers; out of a branch of one lane they were moved there one by one, which
 // took 80 to 130 cycles an instruction and was what bounded the products.)
-__device__ __forceinline__ bool warp_wait(unsigned bar, unsigned parity, volatile int* failed) {
-  return __all_sync(FULL, barrier_wait(bar, parity, failed)) != 0;
+__device__ __forceinline__ bool warp_wait(unsigned bar, unsigned parity, volatile int* failed, int most) {
+  return __all_sync(FULL, barrier_wait(bar, parity, failed, most)) != 0;
 }
 __device__ __forceinline__ bool elect_lane() {
   unsigned is;
@@ -306,6 +306,8 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
                  done = fixed + 8 * STAGES, free_ = done + 16, drain = free_ + 16;
   int* words = reinterpret_cast<int*>(bars + 4 * STAGES + 5);
   volatile int* failed = words;
+  // Looks at a barrier before a wait gives up: seconds. DWEIGHT's contractions are as long as an expert has rows and groups.
+  const int patience = (1 << 22) + (MODE == DWEIGHT ? 32 * (a.R / BK + a.groups) : 0);
   const int lane = threadIdx.x & 31, warp = __shfl_sync(FULL, (int)threadIdx.x >> 5, 0);
   const unsigned rank = PAIR ? cluster_ctarank() : 0;      // the first CTA of a pair issues
   const int first_tile = PAIR ? blockIdx.x / 2 : blockIdx.x, step = PAIR ? gridDim.x / 2 : gridDim.x;
@@ -362,7 +364,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
       };
       ok = each_block<MODE>(a, w, spans, [&](int k, int held, int part) {
         if (issued == begun + 3) look_ahead();
-        if (!warp_wait(empty + 8 * stage, phase ^ 1, failed)) return false;
+        if (!warp_wait(empty + 8 * stage, phase ^ 1, failed, patience)) return false;
         const unsigned to = ring + stage * STAGE_BYTES, tb = to + A_BYTES;
         // a block that ends within is counted by each CTA for itself, for the warp that zeroes its end
         const bool own = MODE == DWEIGHT && held < BK;
@@ -423,13 +425,13 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
         bool first = true;
         const unsigned d = tmem + slot * S::SUMS, idesc = w.narrow ? NARROW : IDESC;
         ok = each_block<MODE>(a, w, spans, [&](int, int held, int) {
-          if (first && !warp_wait(free_ + 8 * slot, slot_phase ^ 1, failed)) return false;
+          if (first && !warp_wait(free_ + 8 * slot, slot_phase ^ 1, failed, patience)) return false;
           const bool partial = MODE == DWEIGHT && held < BK;
           if (partial) {
-            if (!warp_wait(fixed + 8 * stage, fixed_phase >> stage & 1, failed)) return false;
+            if (!warp_wait(fixed + 8 * stage, fixed_phase >> stage & 1, failed, patience)) return false;
             fixed_phase ^= 1u << stage;
           } else {                                          // (blocks that end within pass `full` by)
-            if (!ready && !warp_wait(full + 8 * stage, MODE == DWEIGHT ? full_phase >> stage & 1 : phase, failed)) return false;
+            if (!ready && !warp_wait(full + 8 * stage, MODE == DWEIGHT ? full_phase >> stage & 1 : phase, failed, patience)) return false;
             full_phase ^= 1u << stage;
           }
           fence_after();
@@ -465,7 +467,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
       if (!ok) {
         if (elected) mma_commit<PAIR>(drain);
         int never = 0;
-        barrier_wait(drain, 0, &never);
+        barrier_wait(drain, 0, &never, 1 << 22);
       }
     }
   } else if (warp == 2) {
@@ -478,7 +480,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
         const Tile w = tile_at<MODE, PAIR>(a, head, t, whole);
         ok = each_block<MODE>(a, w, spans, [&](int, int held, int) {
           if (held < BK) {
-            if (!__all_sync(FULL, barrier_wait(partly + 8 * stage, part_phase >> stage & 1, failed))) return false;
+            if (!__all_sync(FULL, barrier_wait(partly + 8 * stage, part_phase >> stage & 1, failed, patience))) return false;
             part_phase ^= 1u << stage;
             const int to = (held + 15) / 16 * 16, bytes16 = (to - held) * 8;
             for (int q = lane; q < 4 * bytes16; q += 32) {
@@ -518,7 +520,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
         each_block<MODE>(a, w, spans, [&](int, int, int) { any = true; return false; });
       }
       const auto wait_sums = [&]() {
-        if (!__all_sync(FULL, barrier_wait(done + 8 * slot, slot_phase, failed))) return false;
+        if (!__all_sync(FULL, barrier_wait(done + 8 * slot, slot_phase, failed, patience))) return false;
         fence_after();
         return true;
       };

@@ -78,3 +78,25 @@ def test_the_binding_refuses_wrong_tensors(lib):
                  lambda: ms.expert_matvec4(x, w.byte(), w, o), lambda: ms.expert_matvec4(x, None, w, o)):
         with pytest.raises(ms.MoeschedError):
             call()
+
+
+def test_more_rows_and_groups_than_are_numbered(lib):
+    for rows, groups in (((1 << 30) + 1, 4), (1 << 31, 4), ((1 << 32) + 10, 4), (10, (1 << 24) + 4), (10, (1 << 32) + 4)):
+        assert ms.expert_scratch_bytes(rows, 64, groups) == 0, (rows, groups)
+    assert ms.expert_scratch_bytes(1 << 30, 8, 1 << 24) > 0
+
+    class Rows(torch.Tensor):                              # says that it is on a GPU; nothing is read
+        is_cuda = True
+
+    def rows(shape, dtype):                                # of that shape, and dense where it counts
+        t = torch.empty(0, dtype=dtype).as_subclass(Rows)
+        t.__class__ = type("Big", (Rows,), {"shape": torch.Size(shape), "dim": lambda s: len(shape), "is_contiguous": lambda s: True,
+                                            "numel": lambda s: torch.Size(shape).numel(), "dtype": dtype})
+        return t
+
+    offsets = rows((3,), torch.int32)
+    assert ms._expert_rows(rows((1 << 30, 8), torch.bfloat16), offsets, 2) == (0, 2)
+    for x, o in ((rows(((1 << 30) + 1, 8), torch.bfloat16), offsets), (rows(((1 << 32) + 5, 8), torch.bfloat16), offsets),
+                 (rows((5, 8), torch.bfloat16), rows(((1 << 32) + 3,), torch.int32))):
+        with pytest.raises(ms.MoeschedError, match="2\\^30"):
+            ms._expert_rows(x, o, 2)

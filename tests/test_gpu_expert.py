@@ -100,7 +100,8 @@ def close(got, want, err, what):
     assert (off <= 0).all(), (what, off.max().item(), (got.double() - want).abs().max().item())
 
 
-def check(x, wg, wu, wd, dy, offsets, kind, train=True):
+def check(x, wg, wu, wd, dy, offsets, kind, train=True, same_rows=None):
+    """same_rows: other offsets that give every expert the same rows, for the plain form."""
     E, dtype = wg.shape[0], x.dtype
     rnd = Rounded(dtype)
     R, D, I = x.shape[0], wg.shape[2], wg.shape[1]
@@ -115,7 +116,7 @@ def check(x, wg, wu, wd, dy, offsets, kind, train=True):
         assert status.item() == 0
         total = {k: torch.zeros((3,) + tuple(grads[k].shape), dtype=torch.float64, device="cuda") for k in ("dw_gate", "dw_up", "dw_down")}
     count = [0] * E
-    for e, s in spans(offsets, E):
+    for e, s in spans(offsets if same_rows is None else same_rows, E):
         rows[s] = True
         count[e] += s.stop - s.start
         args = [t.double() for t in (x[s], wg[e], wu[e], wd[e])]
@@ -162,6 +163,12 @@ def test_many_small_groups_of_many_experts():
     check(*inputs(sum(lengths), 96, 80, 40, torch.bfloat16, 5), offsets_of(lengths), "silu")
     lengths = torch.randint(0, 2, (3 * 700,), generator=g).tolist()       # over a thousand groups
     check(*inputs(sum(lengths), 64, 64, 3, torch.float16, 6), offsets_of(lengths), "gelu")
+
+
+def test_a_hundred_thousand_groups_of_one_expert():
+    lengths = torch.randint(0, 2, (100000,), generator=torch.Generator().manual_seed(2)).tolist()
+    R = sum(lengths)
+    check(*inputs(R, 64, 72, 1, torch.bfloat16, 7), offsets_of(lengths), "silu", same_rows=offsets_of([R]))
 
 
 @pytest.mark.parametrize("R", [40, 700])

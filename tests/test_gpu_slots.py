@@ -242,3 +242,10 @@ def test_a_batch_of_no_matrices():
     got = ms.schedule_slots(z, torch.zeros((0, 3, 4), dtype=torch.uint8, device="cuda"), torch.zeros((0, 3), dtype=torch.int32, device="cuda"),
                             torch.zeros(0, dtype=torch.int32, device="cuda"), torch.zeros((0, 4, 8), dtype=torch.int32, device="cuda"))
     assert got["offsets"].shape == (0, 4, 7)
+
+
+def test_numbers_of_experts_that_do_not_fit():
+    e = torch.zeros((1, 4, 9), dtype=torch.int32, device="cuda")
+    for experts in (-4, 0, 2, 6, 1028):
+        with pytest.raises(ms.MoeschedError):
+            ms.route_demand(e, experts)
