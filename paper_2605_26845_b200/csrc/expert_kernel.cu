@@ -763,7 +763,7 @@ static int plan_threads(int groups) { return groups >= 1024 ? 1024 : (groups + 3
 static bool few_rows(int R, int E) { return R <= 4LL * E + 8; }
 
 // Tiles of pairs or of single CTAs? A pair does some 1.4 times as much as its two SMs would alone, but its tiles are four times
-// as large. Single CTAs where their tiles of every product find an SM each (one expert, 4096 x 2048, 512 rows: 39 us, pairs 45;
+// as large. Single CTAs where their tiles of every product find an SM each (one expert, 4096 x 2048, 330 rows: 37 us, pairs 44;
 // 700 rows, two rounds: 64 and 47), or where groups have less than 128 rows on the average, more than half of a tile of 256
 // rows then being empty. (Each group is taken to fill half of its last tile.)
 static bool tiles_of_pairs(int R, int D, int I, int groups) {
