@@ -38,12 +38,33 @@ __device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
 __device__ __forceinline__ void put(__nv_bfloat16* to, float v) { *to = __float2bfloat16_rn(v); }
 __device__ __forceinline__ void put(__half* to, float v) { *to = __float2half_rn(v); }
 
+// The normal distribution F(a), and e = exp(-a^2 / 2) of its density f = e / sqrt(2 pi). F(-|a|) = e t P(t) with t = 1 / (1 + 0.33 |a|),
+// where P is the polynomial of degree 8 whose greatest relative error for |a| <= 14 is least (fitted for this; 5.5e-8, evaluated in
+// 32 bits 3.1e-7; beyond 14 e is nothing). In the tails it is as near, relatively, as around 0. With erfcf, and the
+// exponential once more, the epilogues bound short contractions: 8 experts, 1024 x 4096, 8192 rows in fp16, forward 217 us, so 188
+// (SiLU 175), backward 552 and 528.
+__device__ __forceinline__ float normal(float a, float& e) {
+  e = __expf(-0.5f * a * a);
+  const float t = __fdividef(1.0f, fmaf(0.33f, fabsf(a), 1.0f));
+  float p = fmaf(-0.0208072793f, t, 0.123078562f);
+  p = fmaf(p, t, -0.267183691f);
+  p = fmaf(p, t, 0.22462818f);
+  p = fmaf(p, t, -0.0565253757f);
+  p = fmaf(p, t, 0.121818744f);
+  p = fmaf(p, t, 0.111065961f);
+  p = fmaf(p, t, 0.132302776f);
+  p = fmaf(p, t, 0.131622165f);
+  const float below = e * t * p;
+  return a < 0.0f ? below : 1.0f - below;
+}
+
 // Activation of the gate and its slope. SiLU a s(a), slope s + a s (1 - s), s the logistic function; GELU a F(a), slope
 // F + a f(a), F and f the normal distribution and its density.
 template <int ACT>
 __device__ __forceinline__ float activation(float a) {
   if constexpr (ACT == MOESCHED_ACT_SILU) return __fdividef(a, 1.0f + __expf(-a));
-  return 0.5f * a * erfcf(a * -0.70710678118654752f);
+  float e;
+  return a * normal(a, e);
 }
 template <int ACT>
 __device__ __forceinline__ void activation_slope(float a, float& value, float& slope) {
@@ -52,9 +73,10 @@ __device__ __forceinline__ void activation_slope(float a, float& value, float& s
     value = a * s;
     slope = s + value * (1.0f - s);
   } else {
-    const float F = 0.5f * erfcf(a * -0.70710678118654752f);
+    float e;
+    const float F = normal(a, e);
     value = a * F;
-    slope = F + a * 0.39894228040143268f * __expf(-0.5f * a * a);
+    slope = fmaf(a * 0.39894228040143268f, e, F);
   }
 }
 

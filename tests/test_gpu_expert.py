@@ -205,6 +205,33 @@ def test_large_values_saturate_the_activation():
             check(x, wg, wu, wd, dy, offsets_of([150]), kind)
 
 
+@pytest.mark.parametrize("kind", ["silu", "gelu"])
+@pytest.mark.parametrize("R", [9, 400])
+def test_the_activations_tails_relative_to_themselves(R, kind):
+    """With unit weights y = act(a) and dx = act'(a) of the numbers in x, each rounded twice; in 32 bits exp(-v) is off by 2 + 1.2 v
+    steps of 2^-23, its argument by one, hence (2 + 2.2 * 41) * 2^-23 and a few more, below 2^-16."""
+    n = 64
+    a = torch.linspace(-9, 9, R * (n - 1), device="cuda").bfloat16().view(R, n - 1)
+    a = a[torch.randperm(R, generator=torch.Generator().manual_seed(0)).cuda()]
+    one = torch.ones((R, 1), dtype=torch.bfloat16, device="cuda")
+    x, eye = torch.cat([a, one], 1), torch.eye(n, dtype=torch.bfloat16, device="cuda")[None].contiguous()
+    wu = torch.zeros_like(eye)
+    wu[0, :, n - 1] = 1                                   # u = 1; the last column of dx has the sums of du
+    y, saved = ms.expert_ffn(x, eye, wu, eye, offsets_of([R]), act=kind, save=True)
+    grads = ms.expert_ffn_backward(torch.ones_like(x), x, eye, wu, eye, offsets_of([R]), saved, act=kind)
+    v = a.double()
+    if kind == "gelu":                                    # (erfc: ndtr is 1 + erf, of which nothing is left in the tail)
+        part = torch.special.erfc(-v / math.sqrt(2)) / 2, v * torch.exp(-v * v / 2) / math.sqrt(2 * math.pi)
+        f, s = v * part[0], part[0] + part[1]
+    else:
+        part = torch.sigmoid(v), v * torch.sigmoid(v) * torch.sigmoid(-v)
+        f, s = v * part[0], part[0] + part[1]
+    twice = 2 * (torch.finfo(torch.bfloat16).eps / 2) * 1.01 + 2.0 ** -16
+    assert ((y[:, :-1].double() - f).abs() <= twice * f.abs()).all()
+    # (the slope is a sum of two parts, each as near as that)
+    assert ((grads["dx"][:, :-1].double() - s).abs() <= twice * s.abs() + 2.0 ** -16 * (part[0].abs() + part[1].abs())).all()
+
+
 @pytest.mark.parametrize("R", [20, 300])
 def test_offsets_out_of_order_are_reported(R):
     x, wg, wu, wd, dy = inputs(R, 64, 64, 2, torch.bfloat16, 11)
