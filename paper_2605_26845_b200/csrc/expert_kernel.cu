@@ -483,10 +483,10 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
             if (!__all_sync(FULL, barrier_wait(partly + 8 * stage, part_phase >> stage & 1, failed, patience))) return false;
             part_phase ^= 1u << stage;
             const int to = (held + 15) / 16 * 16, bytes16 = (to - held) * 8;
-            for (int q = lane; q < 4 * bytes16; q += 32) {
-              const int box = q / bytes16, at = q - box * bytes16;
-              *reinterpret_cast<uint4*>(smem + stage * STAGE_BYTES + box * BOX_BYTES + held * 128 + at * 16) = make_uint4(0, 0, 0, 0);
-            }
+            unsigned char* from = smem + stage * STAGE_BYTES + held * 128;
+            for (int at = lane; at < bytes16; at += 32)
+#pragma unroll
+              for (int box = 0; box < 4; ++box) *reinterpret_cast<uint4*>(from + box * BOX_BYTES + at * 16) = make_uint4(0, 0, 0, 0);
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
             if (lane == 0) {
