@@ -607,13 +607,14 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
         };
         Held even, odd;
         fetch(c_begin, even);
+        fetch(c_begin + 16, odd);
         if (!wait_sums()) break;
 #pragma unroll 1
         for (int c = c_begin; c < c_end; c += 32) {
-          fetch(c + 16, odd);
           work(c, even);
           fetch(c + 32, even);
           work(c + 16, odd);
+          fetch(c + 48, odd);
         }
       } else {
         if (any && !wait_sums()) break;
