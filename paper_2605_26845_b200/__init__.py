@@ -128,7 +128,7 @@ def _call(name, device, *args):
     index = device.index
     stream = torch._C._cuda_getCurrentRawStream(index)
     fn = getattr(load_library(), name)
-    if torch.cuda.current_device() == index:
+    if torch._C._cuda_getDevice() == index:
         rc = fn(*args, stream)
     else:
         with torch.cuda.device(device):
@@ -507,9 +507,10 @@ def schedule_slots(demand, perm, dur, count, counts=None) -> dict:
         raise MoeschedError("perm must be [B, k_stride, N], dur [B, k_stride] and count [B]")
     if counts is not None:
         counts = _dev(counts, torch.int32, "counts")
-        if counts.dim() != 3 or counts.shape[:2] != (B, N) or counts.shape[2] % N != 0:
+        wide = counts.shape
+        if len(wide) != 3 or wide[0] != B or wide[1] != N or wide[2] % N != 0:
             raise MoeschedError("counts must be [B, N, N * experts per rank]")
-        P = counts.shape[2] // N
+        P = wide[2] // N
     if perm.device != dev or dur.device != dev or count.device != dev or (counts is not None and counts.device != dev):
         raise MoeschedError("all tensors must be on one device")
     make, i32, shape, strides = _allocator(dev), torch.int32, (B, K, N), (K * N, N, 1)
