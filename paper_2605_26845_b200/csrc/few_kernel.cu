@@ -191,11 +191,23 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, 1) few_kernel(const FewArgs a)
 
   // this warp's units
   const int teams = gridDim.x * (FEW_WARPS / split), team = blockIdx.x * (FEW_WARPS / split) + warp / split;
-  const long long first = units * team / teams, mine = units * (team + 1) / teams - first;
+  // (divisions of 64 bits take a microsecond here, together; those of 32 are for all but calls that take long anyway)
+  const bool few = units * teams < 1LL << 32;
+  const auto share = [&](int q) {
+    return few ? (long long)((unsigned)units * (unsigned)q / (unsigned)teams) : units * q / teams;
+  };
+  const long long first = share(team), mine = share(team + 1) - first;
   // rows of the expert, and of them the one of this lane's token in eight number `pass`
   const auto find_rows = [&](FewCursor& c) {
     const int e = busy[c.expert], skip = c.pass * FEW_ROWS;
     c.row = -1;
+    if (a.groups == a.E) {                                // one group each: nothing to look for, which is a microsecond less
+      const int2 span = rows_of_group(a.offsets, e, R);
+      c.rows = span.y - span.x;
+      c.passes = (c.rows + FEW_ROWS - 1) / FEW_ROWS;
+      if (skip + gr < c.rows) c.row = span.x + skip + gr;
+      return;
+    }
     long long seen = 0;
     for (long long g0 = e; g0 < a.groups; g0 += 32LL * a.E) {
       const long long g = g0 + (long long)lane * a.E;
@@ -230,8 +242,14 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, 1) few_kernel(const FewArgs a)
     get.expert = lo;
     const long long begin = lo > 0 ? unit_end[lo - 1] : 0;
     find_rows(get);
-    get.tile = (int)((first - begin) / get.passes);
-    get.pass = (int)((first - begin) % get.passes);
+    const long long into = first - begin;
+    if (few) {
+      get.tile = (int)((unsigned)into / (unsigned)get.passes);
+      get.pass = (int)into - get.tile * get.passes;
+    } else {
+      get.tile = (int)(into / get.passes);
+      get.pass = (int)(into % get.passes);
+    }
     if (get.pass > 0) find_rows(get);
   }
   __syncthreads();                                        // the rings are the warps' own from here on
