@@ -208,26 +208,28 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, 1) few_kernel(const FewArgs a)
       if (skip + gr < c.rows) c.row = span.x + skip + gr;
       return;
     }
-    long long seen = 0;
+    // Sums stop at 2^30, which the rows of groups in order do not pass (R does not); others may give any row, but one of R.
+    constexpr unsigned MOST = MOESCHED_MAX_ROWS;
+    unsigned seen = 0;
     for (long long g0 = e; g0 < a.groups; g0 += 32LL * a.E) {
       const long long g = g0 + (long long)lane * a.E;
       const int2 span = g < a.groups ? rows_of_group(a.offsets, (int)g, R) : make_int2(0, 0);
-      const int len = span.y - span.x;
-      long long incl = len;
+      unsigned incl = span.y - span.x;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
-        const long long v = __shfl_up_sync(FULL, incl, o);
-        if (lane >= o) incl += v;
+        const unsigned v = __shfl_up_sync(FULL, incl, o);
+        if (lane >= o) incl = min(incl + v, MOST);
       }
-      const long long at = skip - (seen + incl - len);    // of the first token in this lane's group
-      for (int q = 0; q < FEW_ROWS; ++q) {
-        const unsigned has = __ballot_sync(FULL, at + q >= 0 && at + q < len);
-        const int row = __shfl_sync(FULL, (int)(span.x + at + q), has != 0 ? __ffs(has) - 1 : 0);
-        if (has != 0 && q == gr) c.row = row;
-      }
-      seen += __shfl_sync(FULL, incl, 31);
+      const int token = skip + gr - (int)seen;            // of this lane, from this round's first row on
+      int at = 0;                                         // groups that end before it
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1)
+        if ((int)__shfl_sync(FULL, incl, at + o - 1) <= token) at += o;
+      const int end = (int)__shfl_sync(FULL, incl, at), row = __shfl_sync(FULL, span.y, at) - (end - token);
+      if (token >= 0 && token < end && row >= 0) c.row = row;
+      seen = min(seen + __shfl_sync(FULL, incl, 31), MOST);
     }
-    c.rows = (int)min(seen, (long long)R);
+    c.rows = (int)min(seen, (unsigned)R);
     c.passes = (c.rows + FEW_ROWS - 1) / FEW_ROWS;
   };
   FewCursor get = {};                                     // of the copies; `put_` of the products
