@@ -127,6 +127,8 @@ __device__ __forceinline__ void mma_commit(unsigned bar) {
   else
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
+// Loads from tensor memory are instructions of a whole warp (.aligned): where lanes may have gone different ways before, as at the
+// ragged ends of rows and columns, __syncwarp() brings them together first.
 __device__ __forceinline__ void tmem_load16(unsigned addr, float (&v)[16]) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
@@ -531,6 +533,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
         for (int c = c_begin; c < c_end; c += 16) {
           float p[16], q[16];
           float4 gate[4];
+          __syncwarp();                                    // (see tmem_load16)
           tmem_load16(d + c, p);
           tmem_load16(d + columns + c, q);
           tmem_load_wait();
@@ -579,6 +582,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
         };
         const auto work = [&](int c, const Held& h) {
           float p[16];
+          __syncwarp();                                    // (see tmem_load16)
           tmem_load16(d + c, p);
           tmem_load_wait();
           __syncwarp();
@@ -625,6 +629,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
         for (int c = c_begin; c < c_end; c += 32) {
           if (any) {
             float p[32];
+            __syncwarp();                                  // (see tmem_load16)
             tmem_load32(d + c, p);
             tmem_load_wait();
             __syncwarp();
