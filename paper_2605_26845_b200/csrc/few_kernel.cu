@@ -478,7 +478,10 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, 1) few_kernel(const FewArgs a)
     next_unit(use);
     // the sums are read before they are written again: with two sets, by the barrier of the next unit
     if constexpr (Shape::SUM_SETS == 2) set ^= 1;
-    else if (split > 1) asm volatile("bar.sync %0, %1;" ::"r"(team_bar), "r"(team_threads) : "memory");
+    else if (split > 1) {
+      __syncwarp();                                       // (lanes without a row to store may be ahead; a barrier is for whole warps)
+      asm volatile("bar.sync %0, %1;" ::"r"(team_bar), "r"(team_threads) : "memory");
+    }
     __syncwarp();
   }
   asm volatile("cp.async.wait_group 0;" ::: "memory");
