@@ -65,6 +65,7 @@ __global__ void __launch_bounds__(32 * WARPS) route_kernel(int N, int S, int E, 
       own[x] = total;
     }
     if (threadIdx.x == 0) own[E] = bad;
+    __syncwarp();                                           // (a cluster's barrier is for whole warps)
     cluster_sync_all();
   }
   // totals, first slots: thread t has the experts t, t + threads, ... in rounds, with the sum of the rounds before
@@ -122,6 +123,7 @@ __global__ void __launch_bounds__(32 * WARPS) route_kernel(int N, int S, int E, 
       status[src] = bad ? MOESCHED_ST_BAD_INPUT : MOESCHED_ST_OK;
     }
   }
+  __syncwarp();
   if (CS > 1) cluster_sync_all();                           // (nobody leaves while others read)
   else __syncthreads();                                     // (warp 0 moves its first slots on)
   const unsigned below = (1u << lane) - 1;

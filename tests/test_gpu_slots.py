@@ -249,3 +249,19 @@ def test_numbers_of_experts_that_do_not_fit():
     for experts in (-4, 0, 2, 6, 1028):
         with pytest.raises(ms.MoeschedError):
             ms.route_demand(e, experts)
+
+
+@pytest.mark.parametrize("B,N,S,P", [(1, 1, 262_145, 37), (1, 2, 70_001, 3), (3, 5, 40_000, 1)])
+def test_a_choice_out_of_range_marks_its_source_wherever_it_is(B, N, S, P):
+    """Few sources with many choices are counted by several CTAs each; the choice that is wrong is in the share of a later one."""
+    E = N * P
+    experts = np.random.default_rng(S).integers(-1, E, (B, N, S)).astype(np.int32)
+    for at, value in ((S - 1, E), (S // 2 + 5, -2), (0, 2 ** 31 - 1)):
+        wrong = experts.copy()
+        wrong[B - 1, N - 1, at] = value
+        r = ms.route_demand(dev(wrong), E)
+        wrong[B - 1, N - 1, at] = -1
+        status = r["status"].cpu().numpy()
+        assert status[B - 1, N - 1] == ms.ST_BAD_INPUT and (status.reshape(-1)[:-1] == 0).all()
+        for k, v in zip(("demand", "counts", "slot"), plain_route(wrong, E)):
+            assert (r[k].cpu().numpy() == v).all(), k
