@@ -512,8 +512,8 @@ size_t moesched_slots_scratch_bytes(int B, int N, int k_stride);
  *   d_gate, d_up  out  [R][I] float: a and u for the backward pass (in 32 bits: in 16 the gradients of the weights would be
  *                   half as far again from exact ones); both may be NULL
  *   d_scratch  tmp  moesched_expert_scratch_bytes(R, I, groups, 0) bytes, 256-byte aligned; calls that overlap need their own
- *   d_status   out  [1] int32: OK, or BAD_INPUT where the offsets are not in order or not within 0 .. R: the outputs then
- *                   hold nothing of use
+ *   d_status   out  [1] int32: OK, or BAD_INPUT where the offsets are not in order or not within 0 .. R: all of the outputs are then
+ *                   NaN, so that it shows without the status (INTERNAL, which no input leads to: NaN at least where they would be wrong)
  */
 size_t moesched_expert_scratch_bytes(int R, int I, int groups, int backward);
 int moesched_expert_ffn(int R, int D, int I, int E, int groups, int dtype, int act, const void* d_x, const void* d_w_gate,

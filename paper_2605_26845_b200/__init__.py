@@ -612,8 +612,9 @@ def expert_ffn(x, w_gate, w_up, w_down, offsets, act="silu", save=False, out=Non
     x [R, D] is rows offsets[g] .. offsets[g+1]-1 and belongs to expert g % E. w_gate, w_up [E, I, D], w_down [E, D, I], bfloat16
     or float16; offsets [groups + 1] int32, groups a multiple of E (schedule_slots' offsets of a rank, or the part of them for one matching).
     Returns y [R, D]; rows outside the groups are left as they were (undefined in a tensor made here). With save=True
-    returns (y, saved) for expert_ffn_backward. `status` [1] int32 takes the outcome (ST_BAD_INPUT: offsets out of order);
-    `scratch` is working memory of expert_scratch_bytes(R, I, groups)."""
+    returns (y, saved) for expert_ffn_backward. `status` [1] int32 takes the outcome; where it is not
+    ST_OK (ST_BAD_INPUT: offsets out of order) the results are NaN, with or without a status. `scratch` is working memory of
+    expert_scratch_bytes(R, I, groups)."""
     E, I, D = _expert_weights(x, w_gate, w_up, w_down)
     dtype, groups = _expert_rows(x, offsets, E)
     if offsets.device != x.device:
@@ -629,7 +630,8 @@ def expert_ffn(x, w_gate, w_up, w_down, offsets, act="silu", save=False, out=Non
 
 def expert_ffn_backward(dy, x, w_gate, w_up, w_down, offsets, saved, act="silu", out=None, scratch=None, status=None) -> dict:
     """Gradients of expert_ffn: 'dx' [R, D], 'dw_gate', 'dw_up' [E, I, D] and 'dw_down' [E, D, I] (0 for an expert without rows)
-    from dy [R, D], the inputs of the forward call and what it saved. `out` may hand back the dict of an earlier
+    from dy [R, D], the inputs of the forward call and what it saved. Rows of dx outside the groups are left as they were (undefined in a
+    tensor made here); NaN throughout, as in expert_ffn, if the offsets are out of order. `out` may hand back the dict of an earlier
     call for reuse; `scratch` is working memory of expert_scratch_bytes(R, I, groups, True)."""
     E, I, D = _expert_weights(x, w_gate, w_up, w_down)
     dtype, groups = _expert_rows(x, offsets, E)
@@ -654,7 +656,8 @@ def expert_ffn_backward(dy, x, w_gate, w_up, w_down, offsets, saved, act="silu",
 def expert_matvec4(x, weight, scale, offsets, weight_up=None, scale_up=None, act="silu", out=None, status=None):
     """Products of a few rows with their experts' 4-bit weights: y[r, n] = sum_k (q - 8) scale[e, n, k // group] x[r, k], the q of
     k = 2m in the low half of byte m of weight [E, N, K / 2] uint8, scale [E, N, K / group] in the type of x (bfloat16
-    or float16), group 32, 64 or 128. With weight_up and scale_up, act(x W^T) * (x W_up^T). Rows lie by group as in expert_ffn."""
+    or float16), group 32, 64 or 128. With weight_up and scale_up, act(x W^T) * (x W_up^T). Rows lie by group as in expert_ffn, and
+    the result is NaN, whether or not `status` [1] int32 is there to take the outcome, if the offsets are out of order."""
     dtype, groups = _expert_rows(x, offsets, 1)
     weight = _dev(weight, torch.uint8, "weight")
     scale = _dev(scale, x.dtype, "scale")

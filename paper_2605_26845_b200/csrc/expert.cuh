@@ -81,9 +81,21 @@ __device__ __forceinline__ void activation_slope(float a, float& value, float& s
 }
 
 // Rows of group g, or none where the offsets are not in order: no offsets make a kernel leave its tensors.
+__device__ __forceinline__ bool rows_in_order(int2 span, int R) { return span.x >= 0 && span.x <= span.y && span.y <= R; }
 __device__ __forceinline__ int2 rows_of_group(const int32_t* offsets, int g, int R) {
-  const int begin = offsets[g], end = offsets[g + 1];
-  return begin >= 0 && begin <= end && end <= R ? make_int2(begin, end) : make_int2(0, 0);
+  const int2 span = make_int2(offsets[g], offsets[g + 1]);
+  return rows_in_order(span, R) ? span : make_int2(0, 0);
+}
+
+// A call that fails leaves NaN in its outputs, so that it shows without its status, which nobody may have asked for. This is one in 32 bits,
+// and twice one in either type of 16.
+constexpr unsigned NANS = 0x7fff7fffu;
+// `value` all over a tensor (16-byte aligned, an even number of bytes): share `part` of `parts`, by all threads of a CTA
+static __device__ __noinline__ void fill(void* to, size_t bytes, unsigned value, unsigned part, unsigned parts) {
+  const size_t whole = bytes / 16;
+  for (size_t q = (size_t)part * blockDim.x + threadIdx.x; q < whole; q += (size_t)parts * blockDim.x)
+    static_cast<uint4*>(to)[q] = make_uint4(value, value, value, value);
+  if (part == 0 && threadIdx.x < bytes % 16 / 2) static_cast<unsigned short*>(to)[whole * 8 + threadIdx.x] = (unsigned short)value;
 }
 
 }  // namespace moesched

@@ -39,7 +39,7 @@ constexpr int RASTER_ROWS = 2048;                          // rows of row tiles 
 
 struct alignas(64) GemmArgs {
   CUtensorMap a[3], b[3];                                  // (GLU: b[2] and a[1] are Wg and Wu in boxes of 32 rows)
-  const int4* plan;                                        // {tiles, ok, -, -}, then {first row, rows, expert, -} of every tile
+  int4* plan;                                              // {tiles, ok, the first products failed, -}, then {first row, rows, expert, -} of every tile
   const int32_t* offsets;
   int R, D, I, E, groups;
   void* out[3];
@@ -202,6 +202,14 @@ __global__ void __launch_bounds__(1024) plan_kernel(int R, int E, int groups, in
   }
 }
 
+// Gradients of the weights where there are no rows: 0, or NaN where the offsets name some.
+__global__ void __launch_bounds__(1024) no_rows_kernel(const int4* plan, void* dw_gate, void* dw_up, void* dw_down, size_t bytes) {
+  const unsigned value = plan[0].y ? 0 : NANS;
+  fill(dw_gate, bytes, value, blockIdx.x, gridDim.x);
+  fill(dw_up, bytes, value, blockIdx.x, gridDim.x);
+  fill(dw_down, bytes, value, blockIdx.x, gridDim.x);
+}
+
 // ---- the products ---------------------------------------------------------------------------------------
 
 struct Tile {
@@ -221,7 +229,7 @@ __device__ __forceinline__ int tile_total(const GemmArgs& a, const int4 head) {
   using S = Shape<MODE, PAIR>;
   if constexpr (MODE == DWEIGHT) {
     const int gu = (int)(div_up(a.I, S::M) * div_up(a.D, S::N)), dn = (int)(div_up(a.D, S::M) * div_up(a.I, S::N));
-    return head.y ? a.E * (2 * gu + dn) : 0;
+    return a.E * (2 * gu + dn);
   } else {
     return head.x * (int)div_up(MODE == GLU || MODE == DHIDDEN ? a.I : a.D, S::N);
   }
@@ -266,6 +274,18 @@ __device__ __forceinline__ Tile tile_at(const GemmArgs& a, const int4 head, int 
 struct Spans {
   int expert = -1, begin = 0, end = 0;
 };
+// NaN in all outputs of a product (hidden rows and their gradients are nobody's)
+template <int MODE>
+__device__ __forceinline__ void spoil(const GemmArgs& a, unsigned part, unsigned parts) {
+  if constexpr (MODE == GLU) {
+    for (int q = 0; q < 2 && a.keep[0] != nullptr; ++q) fill(a.keep[q], (size_t)a.R * a.I * 4, NANS, part, parts);
+  } else if constexpr (MODE == DWEIGHT) {
+    for (int q = 0; q < 3; ++q) fill(a.out[q], (size_t)a.E * a.I * a.D * 2, NANS, part, parts);
+  } else if constexpr (MODE != DHIDDEN) {
+    fill(a.out[0], (size_t)a.R * a.D * 2, NANS, part, parts);
+  }
+}
+
 // calls f(k-block's first row or column, what it holds (64 or less), which operands) for every block of the contraction
 template <int MODE, typename F>
 __device__ __forceinline__ bool each_block(const GemmArgs& a, const Tile& w, Spans& kept, F&& f) {
@@ -347,7 +367,11 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
   const unsigned tmem = *reinterpret_cast<volatile unsigned*>(words + 1);
   wait_for_previous();                                     // nothing of other kernels is read, and nothing written, before
   const int4 head = a.plan[0];
-  const int tiles = tile_total<MODE, PAIR>(a, head), whole = whole_tiles<MODE, PAIR>(tiles, step), total = 2 * tiles - whole;
+  // (head.z, that GLU or DHIDDEN gave up, is the same for all CTAs of the products that follow; those two do not look at it)
+  constexpr bool FIRST = MODE == GLU || MODE == DHIDDEN;
+  const bool lost = !head.y || (!FIRST && head.z);
+  if (lost) spoil<MODE>(a, blockIdx.x, gridDim.x);
+  const int tiles = lost ? 0 : tile_total<MODE, PAIR>(a, head), whole = whole_tiles<MODE, PAIR>(tiles, step), total = 2 * tiles - whole;
 
   if (warp == 0) {
     const bool elected = elect_lane();
@@ -666,7 +690,13 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
   }
   fence_before();
   __syncthreads();
-  if (threadIdx.x == 0 && *failed) *a.status = MOESCHED_ST_INTERNAL;
+  if (*failed) {                                           // (what other CTAs still write does not reach this one's tiles)
+    if (threadIdx.x == 0) {
+      *a.status = MOESCHED_ST_INTERNAL;
+      if (FIRST) a.plan[0].z = 1;
+    }
+    spoil<MODE>(a, 0, 1);
+  }
   __syncwarp();
   if constexpr (PAIR) cluster_sync_all();                  // the other CTA may still use our barriers and operands
   if (warp == 1) {
@@ -832,10 +862,10 @@ cudaError_t run_expert_backward(int R, int D, int I, int E, int groups, int dtyp
   const size_t weights = (size_t)E * I * D * 2;
   const bool pair = tiles_of_pairs(R, D, I, groups);
   if (R == 0) {                                             // no rows: no tensor maps, and gradients of nothing
-    if ((e = cudaMemsetAsync(dw_gate, 0, weights, stream)) != cudaSuccess) return e;
-    if ((e = cudaMemsetAsync(dw_up, 0, weights, stream)) != cudaSuccess) return e;
-    if ((e = cudaMemsetAsync(dw_down, 0, weights, stream)) != cudaSuccess) return e;
-    plan_kernel<<<1, plan_threads(groups), 0, stream>>>(R, E, groups, CTA_M, offsets, static_cast<int4*>(scratch), status);
+    int4* plan = static_cast<int4*>(scratch);
+    plan_kernel<<<1, plan_threads(groups), 0, stream>>>(R, E, groups, CTA_M, offsets, plan, status);
+    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    no_rows_kernel<<<sm_count(), 1024, 0, stream>>>(plan, dw_gate, dw_up, dw_down, weights);
     return cudaGetLastError();
   }
   const ExpertScratch at = expert_scratch(R, I, groups, true);

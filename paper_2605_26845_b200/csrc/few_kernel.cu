@@ -144,13 +144,6 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, 1) few_kernel(const FewArgs a)
   let_next_start();
   // experts with rows, and the units up to the end of each
   bool bad = false;
-  if (blockIdx.x == 0) {                                  // one CTA looks at all offsets
-    for (int g = threadIdx.x; g <= a.groups; g += 32 * FEW_WARPS) {
-      const int v = a.offsets[g];
-      bad |= v < 0 || v > R || (g > 0 && a.offsets[g - 1] > v);
-    }
-    bad = __syncthreads_or(bad);
-  }
   int experts = 0;
   long long units = 0;
   for (int e0 = 0; e0 < a.E; e0 += 32 * FEW_WARPS) {
@@ -158,10 +151,10 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, 1) few_kernel(const FewArgs a)
     long long have = 0;
     if (e < a.E)
       for (long long g = e; g < a.groups; g += a.E) {
-        const int2 span = rows_of_group(a.offsets, (int)g, R);
-        have += span.y - span.x;
+        const int2 span = make_int2(a.offsets[g], a.offsets[g + 1]);
+        if (rows_in_order(span, R)) have += span.y - span.x;
+        else bad = true;
       }
-    have = min(have, (long long)R);                       // (offsets out of order may name more rows than there are)
     // units in the upper bits, experts in the lower ten and one
     long long incl = have > 0 ? ((have + FEW_ROWS - 1) / FEW_ROWS * tiles) << 11 | 1 : 0;
     const long long own = incl;
@@ -187,7 +180,16 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, 1) few_kernel(const FewArgs a)
     experts += (int)(all & 2047);
     units += all >> 11;
   }
-  __syncthreads();
+  if (__syncthreads_or(bad)) {                            // (every CTA looks at all groups)
+    wait_for_previous();
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = MOESCHED_ST_BAD_INPUT;
+    fill(a.y, (size_t)R * N * 2, NANS, blockIdx.x, gridDim.x);
+    if (a.sum[0] != nullptr) {
+      fill(a.sum[0], (size_t)R * N * 4, NANS, blockIdx.x, gridDim.x);
+      fill(a.sum[1], (size_t)R * N * 4, NANS, blockIdx.x, gridDim.x);
+    }
+    return;
+  }
 
   // this warp's units
   const int teams = gridDim.x * (FEW_WARPS / split), team = blockIdx.x * (FEW_WARPS / split) + warp / split;
@@ -208,8 +210,7 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, 1) few_kernel(const FewArgs a)
       if (skip + gr < c.rows) c.row = span.x + skip + gr;
       return;
     }
-    // Sums stop at 2^30, which the rows of groups in order do not pass (R does not); others may give any row, but one of R.
-    constexpr unsigned MOST = MOESCHED_MAX_ROWS;
+    // (the groups are in order: no sum passes R, which is 2^30 at most)
     unsigned seen = 0;
     for (long long g0 = e; g0 < a.groups; g0 += 32LL * a.E) {
       const long long g = g0 + (long long)lane * a.E;
@@ -218,7 +219,7 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, 1) few_kernel(const FewArgs a)
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
         const unsigned v = __shfl_up_sync(FULL, incl, o);
-        if (lane >= o) incl = min(incl + v, MOST);
+        if (lane >= o) incl += v;
       }
       const int token = skip + gr - (int)seen;            // of this lane, from this round's first row on
       int at = 0;                                         // groups that end before it
@@ -226,10 +227,10 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, 1) few_kernel(const FewArgs a)
       for (int o = 16; o > 0; o >>= 1)
         if ((int)__shfl_sync(FULL, incl, at + o - 1) <= token) at += o;
       const int end = (int)__shfl_sync(FULL, incl, at), row = __shfl_sync(FULL, span.y, at) - (end - token);
-      if (token >= 0 && token < end && row >= 0) c.row = row;
-      seen = min(seen + __shfl_sync(FULL, incl, 31), MOST);
+      if (token >= 0 && token < end) c.row = row;
+      seen += __shfl_sync(FULL, incl, 31);
     }
-    c.rows = (int)min(seen, (unsigned)R);
+    c.rows = (int)seen;
     c.passes = (c.rows + FEW_ROWS - 1) / FEW_ROWS;
   };
   FewCursor get = {};                                     // of the copies; `put_` of the products
@@ -256,7 +257,7 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, 1) few_kernel(const FewArgs a)
   }
   __syncthreads();                                        // the rings are the warps' own from here on
   wait_for_previous();                                    // x may come from the kernel before this one
-  if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = bad ? MOESCHED_ST_BAD_INPUT : MOESCHED_ST_OK;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = MOESCHED_ST_OK;
   if (mine <= 0) return;
   const auto next_unit = [&](FewCursor& c) {
     --c.left;
