@@ -542,6 +542,16 @@ def _act(act):
     return _ACTS[act]
 
 
+def _no_graph(what, *tensors):
+    """Refuses tensors that want a gradient where autograd records: the experts' calls are not recorded, and the gradient would be lost
+    without a sign."""
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if isinstance(t, torch.Tensor) and t.requires_grad:
+                raise MoeschedError(f"{what} is not recorded by autograd, but an argument requires a gradient: call it under torch.no_grad() "
+                                    "(gradients come from expert_ffn_backward), or detach the argument")
+
+
 def _expert_rows(x, offsets, num_experts):
     """Element type of x [R, width] and number of groups of offsets; both checked."""
     if not isinstance(x, torch.Tensor) or x.dtype not in _TYPES:
@@ -614,7 +624,9 @@ def expert_ffn(x, w_gate, w_up, w_down, offsets, act="silu", save=False, out=Non
     Returns y [R, D]; rows outside the groups are left as they were (undefined in a tensor made here). With save=True
     returns (y, saved) for expert_ffn_backward. `status` [1] int32 takes the outcome; where it is not
     ST_OK (ST_BAD_INPUT: offsets out of order) the results are NaN, with or without a status. `scratch` is working memory of
-    expert_scratch_bytes(R, I, groups)."""
+    expert_scratch_bytes(R, I, groups). Autograd does not record the call: tensors that require gradients are refused unless it is off
+    (torch.no_grad(), or within an autograd function); the gradients come from expert_ffn_backward."""
+    _no_graph("expert_ffn", x, w_gate, w_up, w_down, out)
     E, I, D = _expert_weights(x, w_gate, w_up, w_down)
     dtype, groups = _expert_rows(x, offsets, E)
     if offsets.device != x.device:
@@ -632,7 +644,8 @@ def expert_ffn_backward(dy, x, w_gate, w_up, w_down, offsets, saved, act="silu",
     """Gradients of expert_ffn: 'dx' [R, D], 'dw_gate', 'dw_up' [E, I, D] and 'dw_down' [E, D, I] (0 for an expert without rows)
     from dy [R, D], the inputs of the forward call and what it saved. Rows of dx outside the groups are left as they were (undefined in a
     tensor made here); NaN throughout, as in expert_ffn, if the offsets are out of order. `out` may hand back the dict of an earlier
-    call for reuse; `scratch` is working memory of expert_scratch_bytes(R, I, groups, True)."""
+    call for reuse; `scratch` is working memory of expert_scratch_bytes(R, I, groups, True). Not recorded by autograd, like expert_ffn."""
+    _no_graph("expert_ffn_backward", dy, x, w_gate, w_up, w_down)
     E, I, D = _expert_weights(x, w_gate, w_up, w_down)
     dtype, groups = _expert_rows(x, offsets, E)
     R, dev = x.shape[0], x.device
@@ -657,7 +670,9 @@ def expert_matvec4(x, weight, scale, offsets, weight_up=None, scale_up=None, act
     """Products of a few rows with their experts' 4-bit weights: y[r, n] = sum_k (q - 8) scale[e, n, k // group] x[r, k], the q of
     k = 2m in the low half of byte m of weight [E, N, K / 2] uint8, scale [E, N, K / group] in the type of x (bfloat16
     or float16), group 32, 64 or 128. With weight_up and scale_up, act(x W^T) * (x W_up^T). Rows lie by group as in expert_ffn, and
-    the result is NaN, whether or not `status` [1] int32 is there to take the outcome, if the offsets are out of order."""
+    the result is NaN, whether or not `status` [1] int32 is there to take the outcome, if the offsets are out of order.
+    Not recorded by autograd, like expert_ffn."""
+    _no_graph("expert_matvec4", x, scale, scale_up, out)
     dtype, groups = _expert_rows(x, offsets, 1)
     weight = _dev(weight, torch.uint8, "weight")
     scale = _dev(scale, x.dtype, "scale")
@@ -704,7 +719,7 @@ def probe_expert(weights, tokens=(1, 16, 64, 256, 1024, 4096), act="silu", base=
     gen = torch.Generator(dev)
     gen.manual_seed(0)
     times = []
-    with torch.cuda.device(dev):
+    with torch.cuda.device(dev), torch.no_grad():
         for g in tokens:
             x = torch.randn((g, D), generator=gen, device=dev).to(typed.dtype)
             offsets = torch.tensor([g * e // E for e in range(E + 1)], dtype=torch.int32, device=dev)

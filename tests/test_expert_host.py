@@ -100,3 +100,26 @@ def test_more_rows_and_groups_than_are_numbered(lib):
                  (rows((5, 8), torch.bfloat16), rows(((1 << 32) + 3,), torch.int32))):
         with pytest.raises(ms.MoeschedError, match="2\\^30"):
             ms._expert_rows(x, o, 2)
+
+
+def test_tensors_that_want_a_gradient_are_refused_where_autograd_records():
+    x, w = torch.zeros((4, 8), dtype=torch.bfloat16), torch.zeros((1, 8, 8), dtype=torch.bfloat16)
+    o, q = torch.zeros(2, dtype=torch.int32), torch.zeros((1, 8, 4), dtype=torch.uint8)
+
+    def calls(x, w, dy, s):
+        return (lambda: ms.expert_ffn(x, w, w.detach(), w.detach(), o), lambda: ms.expert_ffn_backward(dy, x, w.detach(), w, w.detach(), o, {}),
+                lambda: ms.expert_matvec4(x, q, s, o), lambda: ms.expert_matvec4(x, q, s.detach(), o, q, s))
+
+    want, wide = (t.clone().requires_grad_() for t in (x, w))
+    for call in calls(want, w, x, w) + calls(x, wide, x, wide):
+        with pytest.raises(ms.MoeschedError, match="no_grad"):
+            call()
+        with torch.no_grad(), pytest.raises(ms.MoeschedError, match="CUDA tensor"):       # (the next check)
+            call()
+    for call in calls(x, w, x, w):
+        with pytest.raises(ms.MoeschedError, match="CUDA tensor"):
+            call()
+    with pytest.raises(ms.MoeschedError, match="no_grad"):
+        ms.expert_ffn(x, w, w, w, o, out=want)
+    with pytest.raises(ms.MoeschedError, match="no_grad"):
+        ms.expert_ffn_backward(want, x, w, w, w, o, {})
