@@ -450,8 +450,10 @@ _INT_MAX = 0x7fffffff                                    # (the binding of the C
 
 def _allocator(device):
     """Function of (shape, strides, dtype) that makes a tensor on `device`. (torch.empty takes 2.3 us, torch.empty_strided 1.5 and the
-    allocation underneath 0.8, which counts beside kernels of a few microseconds.)"""
-    if _empty_strided_cuda is not None and device.index == torch._C._cuda_getDevice():
+    allocation underneath 0.8, which counts beside kernels of a few microseconds.) Not the one underneath where the dispatcher has something to
+    do: fill uninitialised memory (deterministic algorithms), or tell a dispatch mode."""
+    if (_empty_strided_cuda is not None and device.index == torch._C._cuda_getDevice() and not torch._C._get_deterministic_algorithms()
+            and not torch._C._len_torch_dispatch_stack()):
         return _empty_strided_cuda
     return lambda shape, strides, dtype: torch.empty_strided(shape, strides, dtype=dtype, device=device)
 

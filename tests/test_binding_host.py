@@ -118,3 +118,28 @@ def test_a_path_uses_the_buffers_that_it_has_at_the_time_of_the_call(calls, path
             check()
     path.mw.work = path.bvn.work = None
     check()
+
+
+def test_allocations_pass_the_dispatcher_by_only_where_it_has_nothing_to_do(monkeypatch):
+    from torch.utils._python_dispatch import TorchDispatchMode
+
+    class Watching(TorchDispatchMode):
+        def __torch_dispatch__(self, func, types, args=(), kwargs=None):
+            return func(*args, **(kwargs or {}))
+
+    def short(shape, strides, dtype):
+        raise AssertionError("not called")
+
+    monkeypatch.setattr(ms, "_empty_strided_cuda", short)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0)
+    device = torch.device("cuda", 0)
+    assert ms._allocator(device) is short and ms._allocator(torch.device("cuda", 1)) is not short
+    with Watching():
+        assert ms._allocator(device) is not short
+    before = torch.are_deterministic_algorithms_enabled()
+    torch.use_deterministic_algorithms(True)
+    try:
+        assert ms._allocator(device) is not short
+    finally:
+        torch.use_deterministic_algorithms(before)
+    assert ms._allocator(device) is short

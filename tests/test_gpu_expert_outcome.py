@@ -75,3 +75,31 @@ def test_4_bit_products_with_offsets_out_of_order(R, K, N, E, groups, dtype):
             out = beyond[:R * N].view(R, N)
             ms.expert_matvec4(x, q, scale, offsets, *second, out=out)
             assert lost([out]) and (beyond[R * N:] == 7.0).all(), offsets
+
+
+def test_results_are_seen_by_deterministic_mode_and_by_dispatch_modes():
+    """Rows that no group has are undefined in a tensor made by the call; deterministic mode fills them (with NaN), and a dispatch mode sees
+    the allocations."""
+    from torch.utils._python_dispatch import TorchDispatchMode
+
+    seen = []
+
+    class Watching(TorchDispatchMode):
+        def __torch_dispatch__(self, func, types, args=(), kwargs=None):
+            seen.append(func)
+            return func(*args, **(kwargs or {}))
+
+    x, wg, wu, wd, _ = inputs(40, 64, 72, 1, torch.bfloat16, 5)
+    offsets = offsets_of([20], first=7)
+    want = ms.expert_ffn(x, wg, wu, wd, offsets)[7:27]
+    held = [torch.full_like(x, 3.0) for _ in range(4)]
+    del held                                              # (what the next allocations of that size find)
+    torch.use_deterministic_algorithms(True)
+    try:
+        y = ms.expert_ffn(x, wg, wu, wd, offsets)
+    finally:
+        torch.use_deterministic_algorithms(False)
+    assert torch.isnan(y[:7]).all() and torch.isnan(y[27:]).all() and torch.equal(y[7:27], want)
+    with Watching():
+        y = ms.expert_ffn(x, wg, wu, wd, offsets)
+    assert torch.ops.aten.empty_strided.default in seen and torch.equal(y[7:27], want)
