@@ -22,6 +22,8 @@
 // clock is at 1.45 to 1.55 GHz then: what bounds the large products is the power.
 #include <cuda.h>
 
+#include <atomic>
+
 #include "expert.cuh"
 
 namespace moesched {
@@ -713,7 +715,8 @@ using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, voi
                               CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
 static cudaError_t encoder(EncodeFn* fn) {
-  static EncodeFn found = nullptr;      // (every thread finds the same)
+  static std::atomic<EncodeFn> kept{nullptr};              // (every thread finds the same)
+  EncodeFn found = kept.load(std::memory_order_relaxed);
   if (found == nullptr) {
     void* p = nullptr;
     cudaDriverEntryPointQueryResult how;
@@ -721,6 +724,7 @@ static cudaError_t encoder(EncodeFn* fn) {
     if (e != cudaSuccess) return e;
     if (how != cudaDriverEntryPointSuccess || p == nullptr) return cudaErrorNotSupported;
     found = reinterpret_cast<EncodeFn>(p);
+    kept.store(found, std::memory_order_relaxed);
   }
   *fn = found;
   return cudaSuccess;
