@@ -707,7 +707,9 @@ def probe_expert(weights, tokens=(1, 16, 64, 256, 1024, 4096), act="silu", base=
     are timed for every count in `tokens`, spread evenly over the experts, and the model's curve is laid through the times: a fixed cost up
     to a knee, linear beyond. weights = (w_gate, w_up, w_down) as expert_ffn takes them, or three (weight, scale) pairs in 4
     bits, timed with expert_matvec4. Returns 'model' (base, or DEFAULT_MODEL, with the experts' three numbers and the bytes of a token,
-    as schedule_eval, Path and the others take it), 'tokens' and 'ns'. Synchronises: a measurement, not for a serving loop."""
+    as schedule_eval, Path and the others take it), 'tokens' and 'ns'. A time is that of the GPU alone: batches are replayed from a graph, behind
+    work that keeps the GPU busy until they are queued, and find the weights in memory, not in the L2 (another layer's were there
+    before). Synchronises: a measurement, not for a serving loop."""
     quantised = isinstance(weights[0], (tuple, list))
     first = weights[0][0] if quantised else weights[0]
     typed = weights[0][1] if quantised else weights[0]
@@ -722,6 +724,7 @@ def probe_expert(weights, tokens=(1, 16, 64, 256, 1024, 4096), act="silu", base=
     gen.manual_seed(0)
     times = []
     with torch.cuda.device(dev), torch.no_grad():
+        other = torch.zeros(torch.cuda.get_device_properties(dev).L2_cache_size, dtype=torch.float32, device=dev)     # (four times the L2)
         for g in tokens:
             x = torch.randn((g, D), generator=gen, device=dev).to(typed.dtype)
             offsets = torch.tensor([g * e // E for e in range(E + 1)], dtype=torch.int32, device=dev)
@@ -735,10 +738,14 @@ def probe_expert(weights, tokens=(1, 16, 64, 256, 1024, 4096), act="silu", base=
                     return expert_ffn(x, *weights, offsets, act=act)
             for _ in range(3):
                 batch()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=torch.cuda.Stream(dev), capture_error_mode="thread_local"):
+                batch()
             events = [(torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)) for _ in range(reps)]
             for start, end in events:
+                other.sum()                              # (read, not written: nothing is left to be written back)
                 start.record()
-                batch()
+                graph.replay()
                 end.record()
             torch.cuda.current_stream(dev).synchronize()
             times.append(sorted(s.elapsed_time(e) for s, e in events)[reps // 2] * 1e6)

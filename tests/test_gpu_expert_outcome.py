@@ -1,5 +1,7 @@
 """What a call of the experts leaves behind when its offsets are out of order: NaN in every output, whether or not anybody asked for the
 status. So nothing that was there before, or comes from uninitialised memory, passes for a result."""
+import time
+
 import pytest
 import torch
 
@@ -103,3 +105,22 @@ def test_results_are_seen_by_deterministic_mode_and_by_dispatch_modes():
     with Watching():
         y = ms.expert_ffn(x, wg, wu, wd, offsets)
     assert torch.ops.aten.empty_strided.default in seen and torch.equal(y[7:27], want)
+
+
+def test_a_probe_times_the_gpu_and_not_the_host(monkeypatch):
+    """Calls that take the host two milliseconds each leave the times of batches as they are; weights that are parameters are taken."""
+    E, D, I = 2, 256, 128
+    _, wg, wu, wd, _ = inputs(1, D, I, E, torch.bfloat16, 30)
+    pairs = [quantised(E, n, k, 64, torch.bfloat16, n)[:2] for n, k in ((I, D), (I, D), (D, I))]
+    call = ms._call
+
+    def slow(name, *args):
+        time.sleep(0.002)
+        return call(name, *args)
+
+    monkeypatch.setattr(ms, "_call", slow)
+    before = torch.cuda.memory_allocated()
+    for weights in ([torch.nn.Parameter(w) for w in (wg, wu, wd)], pairs):
+        ns = ms.probe_expert(weights, tokens=(1, 8, 300), reps=5)["ns"]
+        assert all(0 < t < 1e6 for t in ns), ns
+    assert torch.cuda.memory_allocated() - before < 1 << 20
