@@ -9,6 +9,7 @@ a missing library or a non-CUDA tensor raises.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 from dataclasses import dataclass
 
@@ -702,6 +703,21 @@ def expert_matvec4(x, weight, scale, offsets, weight_up=None, scale_up=None, act
     return out
 
 
+def _expert_curve(tokens, times):
+    """Fixed cost, slope and knee of the curve that is nearest to the times, of those with one of the counts as the knee. Near is a ratio, so
+    that half of a time is as far off as twice (a difference relative to the time would put curves below)."""
+    best = None
+    for knee in tokens:
+        flat = [ns for g, ns in zip(tokens, times) if g <= knee]
+        fixed = sum(flat) / len(flat)
+        beyond = [(g - knee, ns - fixed) for g, ns in zip(tokens, times) if g > knee]
+        slope = max(0.0, sum(g * ns for g, ns in beyond) / sum(g * g for g, _ in beyond)) if beyond else 0.0
+        off = sum(math.log((fixed + max(0, g - knee) * slope) / ns) ** 2 for g, ns in zip(tokens, times))
+        if best is None or off < best[0]:
+            best = off, fixed, slope, knee
+    return best[1:]
+
+
 def probe_expert(weights, tokens=(1, 16, 64, 256, 1024, 4096), act="silu", base=None, reps=20) -> dict:
     """Compute model of the experts of one rank, measured (the paper profiles its experts, Fig. 1): the batches of expert_ffn
     are timed for every count in `tokens`, spread evenly over the experts, and the model's curve is laid through the times: a fixed cost up
@@ -749,17 +765,7 @@ def probe_expert(weights, tokens=(1, 16, 64, 256, 1024, 4096), act="silu", base=
                 end.record()
             torch.cuda.current_stream(dev).synchronize()
             times.append(sorted(s.elapsed_time(e) for s, e in events)[reps // 2] * 1e6)
-    # of all counts as the knee the one whose curve is nearest to the times, relative to them
-    best = None
-    for knee in tokens:
-        flat = [ns for g, ns in zip(tokens, times) if g <= knee]
-        fixed = sum(flat) / len(flat)
-        beyond = [(g - knee, ns - fixed) for g, ns in zip(tokens, times) if g > knee]
-        slope = max(0.0, sum(g * ns for g, ns in beyond) / sum(g * g for g, _ in beyond)) if beyond else 0.0
-        off = sum(((fixed + max(0, g - knee) * slope) / ns - 1) ** 2 for g, ns in zip(tokens, times))
-        if best is None or off < best[0]:
-            best = off, fixed, slope, knee
-    _, fixed, slope, knee = best
+    fixed, slope, knee = _expert_curve(tokens, times)
     model = dict(base or DEFAULT_MODEL, bytes_per_token=2 * D, expert_fixed_ns=round(fixed), expert_knee_tokens=knee,
                  expert_ps_per_token=round(slope * 1000))
     return {"model": model, "tokens": tokens, "ns": times}

@@ -123,3 +123,15 @@ def test_tensors_that_want_a_gradient_are_refused_where_autograd_records():
         ms.expert_ffn(x, w, w, w, o, out=want)
     with pytest.raises(ms.MoeschedError, match="no_grad"):
         ms.expert_ffn_backward(want, x, w, w, w, o, {})
+
+
+def test_the_curve_through_measured_times():
+    tokens = [1, 16, 64, 256, 1024, 4096]
+    for fixed, slope, knee in ((100.0, 0.25, 64), (7.5, 0.0, 4096), (31.0, 3.0, 1)):          # its own curve is found again
+        times = [fixed + max(0, g - knee) * slope for g in tokens]
+        got = ms._expert_curve(tokens, times)
+        assert all(abs(got[0] + max(0, g - got[2]) * got[1] - t) <= 1e-9 * t for g, t in zip(tokens, times)), got
+    # four experts, of which one token meets only one: the curve is not laid through that one, with the others at a third of their times
+    times = [24.8, 69.6, 70.3, 72.5, 84.0, 227.5]
+    fixed, slope, knee = ms._expert_curve(tokens, times)
+    assert all(0.5 <= (fixed + max(0, g - knee) * slope) / t <= 2 for g, t in zip(tokens, times))
