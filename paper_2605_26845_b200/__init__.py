@@ -476,8 +476,8 @@ def route_demand(experts, num_experts, out=None) -> dict:
         raise MoeschedError("experts must have shape [B, N, S]")
     B, N, S = experts.shape
     E, dev = int(num_experts), experts.device
-    if not N <= E <= 1024 or E % N != 0 or max(B, S) > _INT_MAX:
-        raise MoeschedError("num_experts must be a multiple of N and 1024 at most, B and S less than 2^31")
+    if not 1 <= N <= E <= MAX_EXPERTS or E % N != 0 or max(B, S) > _INT_MAX:
+        raise MoeschedError(f"num_experts must be a multiple of N and {MAX_EXPERTS} at most, B and S less than 2^31")
     if out is None:
         make, i32 = _allocator(dev), torch.int32
         out = {"demand": make((B, N, N), (N * N, N, 1), i32), "counts": make((B, N, E), (N * E, E, 1), i32),
@@ -511,8 +511,8 @@ def schedule_slots(demand, perm, dur, count, counts=None) -> dict:
     if counts is not None:
         counts = _dev(counts, torch.int32, "counts")
         wide = counts.shape
-        if len(wide) != 3 or wide[0] != B or wide[1] != N or wide[2] % N != 0:
-            raise MoeschedError("counts must be [B, N, N * experts per rank]")
+        if len(wide) != 3 or wide[0] != B or wide[1] != N or wide[2] % N != 0 or not N <= wide[2] <= MAX_EXPERTS:
+            raise MoeschedError(f"counts must be [B, N, N * experts per rank], {MAX_EXPERTS} experts at most")
         P = wide[2] // N
     if perm.device != dev or dur.device != dev or count.device != dev or (counts is not None and counts.device != dev):
         raise MoeschedError("all tensors must be on one device")
@@ -535,7 +535,7 @@ def schedule_slots(demand, perm, dur, count, counts=None) -> dict:
 
 
 _ACTS = {"silu": 0, "gelu": 1}
-_MAX_ROWS, _MAX_GROUPS = 1 << 30, 1 << 24
+_MAX_ROWS, _MAX_GROUPS, _MAX_WIDTH = 1 << 30, 1 << 24, 65536
 _TYPES = {torch.bfloat16: 0, torch.float16: 1}
 
 
@@ -589,6 +589,8 @@ def _expert_weights(x, w_gate, w_up, w_down):
             raise MoeschedError(f"{what} must have shape {shape}, on the device of x")
     if x.shape[1] != D:
         raise MoeschedError("x must be [R, D] with the D of the weights")
+    if max(D, I) > _MAX_WIDTH or E > MAX_EXPERTS:
+        raise MoeschedError(f"D and I must be {_MAX_WIDTH} at most, and there may be {MAX_EXPERTS} experts")
     return E, I, D
 
 
@@ -615,7 +617,7 @@ def _expert_scratch(scratch, x, I, groups, backward):
 def expert_scratch_bytes(rows, width, groups, backward=False) -> int:
     """Working memory of expert_ffn (or its backward pass) for that many rows, a hidden width of `width` and `groups` groups."""
     rows, width, groups = int(rows), int(width), int(groups)
-    if max(rows, width, groups) > _INT_MAX:              # (the library answers the others)
+    if max(rows, width, groups) > _INT_MAX or min(rows, width, groups) < 0:              # (the library answers the others)
         return 0
     return int(load_library().moesched_expert_scratch_bytes(rows, width, groups, int(backward)))
 

@@ -143,3 +143,31 @@ def test_allocations_pass_the_dispatcher_by_only_where_it_has_nothing_to_do(monk
     finally:
         torch.use_deterministic_algorithms(before)
     assert ms._allocator(device) is short
+
+
+def test_sizes_that_an_int_does_not_hold_are_refused(calls):
+    """The library numbers in 32 bits, and ctypes cuts what is longer: 2^32 + 8 columns would be 8."""
+    big = (1 << 32) + 8
+
+    def t(*shape, dtype=torch.bfloat16):
+        return torch.empty(shape, dtype=dtype, device="meta")       # (a shape, and no memory)
+
+    def ints(*shape):
+        return t(*shape, dtype=torch.int32)
+
+    refused = [
+        lambda: ms.route_demand(ints(1, 0, 5), 0), lambda: ms.route_demand(ints(1, 0, 5), 8), lambda: ms.route_demand(ints(1, 4, 5), big),
+        lambda: ms.schedule_slots(ints(1, 1, 1), t(1, 3, 1, dtype=torch.uint8), ints(1, 3), ints(1), ints(1, 1, (1 << 32) + 4)),
+        lambda: ms.schedule_slots(ints(1, 1, 1), t(1, 3, 1, dtype=torch.uint8), ints(1, 3), ints(1), ints(1, 1, 0)),
+        lambda: ms.expert_ffn(t(4, 8), t(1, big, 8), t(1, big, 8), t(1, 8, big), ints(2)),
+        lambda: ms.expert_ffn(t(0, big), t(1, 8, big), t(1, 8, big), t(1, big, 8), ints(2)),
+        lambda: ms.expert_ffn(t(4, 8), t(big, 8, 8), t(big, 8, 8), t(big, 8, 8), ints(big + 1)),
+        lambda: ms.expert_ffn_backward(t(4, 8), t(4, 8), t(1, big, 8), t(1, big, 8), t(1, 8, big), ints(2), dict(gate=t(4, big), up=t(4, big))),
+        lambda: ms.expert_matvec4(t(4, 64), t(1, big, 32, dtype=torch.uint8), t(1, big, 2), ints(2)),
+        lambda: ms.expert_matvec4(t(4, big), t(1, 8, big // 2, dtype=torch.uint8), t(1, 8, big // 8), ints(2)),
+    ]
+    for n, call in enumerate(refused):
+        with pytest.raises(ms.MoeschedError):
+            call()
+        assert not calls, n
+    assert ms.expert_scratch_bytes(10 - (1 << 32), 64, 4) == ms.expert_scratch_bytes(10, 64 - (1 << 32), 4) == ms.expert_scratch_bytes(10, 64, 4 - (1 << 32)) == 0
