@@ -595,6 +595,8 @@ def _expert_weights(x, w_gate, w_up, w_down):
 
 
 def _status_of(status, device):
+    """The caller's, or a new one, which the call has to hold on to until it has launched: memory that is free again another
+    thread may be given on the same stream, for work that is launched earlier."""
     if status is None:
         return _empty(torch.int32, device, 1)
     _dev(status, torch.int32, "status")
@@ -639,9 +641,9 @@ def expert_ffn(x, w_gate, w_up, w_down, offsets, act="silu", save=False, out=Non
     R, dev = x.shape[0], x.device
     out = _like(out, x, (R, D), "out")
     saved = {k: _empty(torch.float32, dev, R, I) for k in ("gate", "up")} if save else {}
-    scratch = _expert_scratch(scratch, x, I, groups, 0)
+    scratch, status = _expert_scratch(scratch, x, I, groups, 0), _status_of(status, dev)
     _call("moesched_expert_ffn", dev, R, D, I, E, groups, dtype, _act(act), _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(w_down),
-          _ptr(offsets), _ptr(out), _ptr(saved.get("gate")), _ptr(saved.get("up")), _ptr(scratch), _ptr(_status_of(status, dev)))
+          _ptr(offsets), _ptr(out), _ptr(saved.get("gate")), _ptr(saved.get("up")), _ptr(scratch), _ptr(status))
     return (out, saved) if save else out
 
 
@@ -664,10 +666,10 @@ def expert_ffn_backward(dy, x, w_gate, w_up, w_down, offsets, saved, act="silu",
             raise MoeschedError(f"saved['{k}'] must be [R, I], on the device of x")
     shapes = dict(dx=(R, D), dw_gate=(E, I, D), dw_up=(E, I, D), dw_down=(E, D, I))
     grads = {k: _like(None if out is None else out[k], x, v, k) for k, v in shapes.items()}
-    scratch = _expert_scratch(scratch, x, I, groups, 1)
+    scratch, status = _expert_scratch(scratch, x, I, groups, 1), _status_of(status, dev)
     _call("moesched_expert_ffn_backward", dev, R, D, I, E, groups, dtype, _act(act), _ptr(dy), _ptr(x), _ptr(w_gate), _ptr(w_up),
           _ptr(w_down), _ptr(offsets), _ptr(saved["gate"]), _ptr(saved["up"]), *(_ptr(grads[k]) for k in shapes), _ptr(scratch),
-          _ptr(_status_of(status, dev)))
+          _ptr(status))
     return grads
 
 
@@ -699,9 +701,9 @@ def expert_matvec4(x, weight, scale, offsets, weight_up=None, scale_up=None, act
             raise MoeschedError("weight_up must be like weight, on the device of x")
         if _dev(scale_up, x.dtype, "scale_up").shape != scale.shape or scale_up.device != dev:
             raise MoeschedError("scale_up must be like scale, on the device of x")
-    out = _like(out, x, (R, N), "out")
+    out, status = _like(out, x, (R, N), "out"), _status_of(status, dev)
     _call("moesched_expert_matvec4", dev, R, K, N, E, groups, K // parts, dtype, _act(act), x.data_ptr(), weight.data_ptr(),
-          scale.data_ptr(), _ptr(weight_up), _ptr(scale_up), offsets.data_ptr(), out.data_ptr(), _status_of(status, dev).data_ptr())
+          scale.data_ptr(), _ptr(weight_up), _ptr(scale_up), offsets.data_ptr(), out.data_ptr(), status.data_ptr())
     return out
 
 

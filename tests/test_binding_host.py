@@ -171,3 +171,35 @@ def test_sizes_that_an_int_does_not_hold_are_refused(calls):
             call()
         assert not calls, n
     assert ms.expert_scratch_bytes(10 - (1 << 32), 64, 4) == ms.expert_scratch_bytes(10, 64 - (1 << 32), 4) == ms.expert_scratch_bytes(10, 64, 4 - (1 << 32)) == 0
+
+
+def test_what_a_call_allocates_lives_until_it_is_launched(monkeypatch):
+    """Memory that is free again may be another thread's, on the same stream and in front of this call, before it is launched."""
+    import gc
+    import weakref
+
+    made, launched = {}, []
+
+    def empty(dtype, device, *shape):
+        t = torch.empty(shape, dtype=dtype)
+        made[t.data_ptr()] = weakref.ref(t)
+        return t
+
+    def call(name, device, *args):
+        gc.collect()
+        used = [made[a] for a in args if isinstance(a, int) and a in made]
+        launched.append(name)
+        assert len(used) == len(made) and all(r() is not None for r in used), name
+
+    monkeypatch.setattr(ms, "_dev", lambda t, dtype, what: t)
+    monkeypatch.setattr(ms, "_empty", empty)
+    monkeypatch.setattr(ms, "_call", call)
+    monkeypatch.setattr(ms, "load_library", lambda: type("Library", (), {"moesched_expert_scratch_bytes": lambda self, *a: 4096})())
+    x, w, q = torch.ones((4, 8), dtype=torch.bfloat16), torch.ones((1, 8, 8), dtype=torch.bfloat16), torch.ones((1, 8, 4), dtype=torch.uint8)
+    offsets, kept = torch.zeros(2, dtype=torch.int32), dict(gate=torch.ones((4, 8)), up=torch.ones((4, 8)))
+    ms.expert_ffn(x, w, w, w, offsets, save=True)
+    made.clear()
+    ms.expert_ffn_backward(x, x, w, w, w, offsets, kept)
+    made.clear()
+    ms.expert_matvec4(x, q, w[:, :, :1].contiguous(), offsets)
+    assert launched == ["moesched_expert_ffn", "moesched_expert_ffn_backward", "moesched_expert_matvec4"]
