@@ -491,7 +491,9 @@ size_t moesched_slots_scratch_bytes(int B, int N, int k_stride);
  * at most MOESCHED_MAX_GROUPS, and MOESCHED_MAX_ROWS rows. Outputs and scratch overlap neither one another nor an input.
  * Groups may be empty. Rows before the first and behind the last group are neither used nor written. Tensors are densely
  * packed, row major, 16-byte aligned, all of one type, MOESCHED_BF16 or MOESCHED_FP16; products are summed in 32 bits.
- * Values beyond the type's range become infinities.
+ * Values beyond the type's range become infinities, and that includes h, da and du below, which are rounded to the type on the way: in
+ * FP16 an h beyond 65504 makes y infinite where it need not be, and a da or du below 6e-5 loses digits, below 3e-8 is 0 (BF16 has
+ * the range of 32 bits).
  */
 #define MOESCHED_MAX_ROWS (1 << 30)
 #define MOESCHED_MAX_GROUPS (1 << 24)

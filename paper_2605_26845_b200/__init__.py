@@ -628,6 +628,7 @@ def expert_ffn(x, w_gate, w_up, w_down, offsets, act="silu", save=False, out=Non
     """Gated feed-forward block of the experts, y = (act(x Wg^T) * (x Wu^T)) Wd^T, on rows grouped by expert: group g of
     x [R, D] is rows offsets[g] .. offsets[g+1]-1 and belongs to expert g % E. w_gate, w_up [E, I, D], w_down [E, D, I], bfloat16
     or float16; offsets [groups + 1] int32, groups a multiple of E (schedule_slots' offsets of a rank, or the part of them for one matching).
+    act(x Wg^T) * (x Wu^T) is rounded to the type before the second product: in float16, infinite beyond 65504.
     Returns y [R, D]; rows outside the groups are left as they were (undefined in a tensor made here). With save=True
     returns (y, saved) for expert_ffn_backward. `status` [1] int32 takes the outcome; where it is not
     ST_OK (ST_BAD_INPUT: offsets out of order) the results are NaN, with or without a status. `scratch` is working memory of
@@ -649,7 +650,8 @@ def expert_ffn(x, w_gate, w_up, w_down, offsets, act="silu", save=False, out=Non
 
 def expert_ffn_backward(dy, x, w_gate, w_up, w_down, offsets, saved, act="silu", out=None, scratch=None, status=None) -> dict:
     """Gradients of expert_ffn: 'dx' [R, D], 'dw_gate', 'dw_up' [E, I, D] and 'dw_down' [E, D, I] (0 for an expert without rows)
-    from dy [R, D], the inputs of the forward call and what it saved. Rows of dx outside the groups are left as they were (undefined in a
+    from dy [R, D], the inputs of the forward call and what it saved. (The gradients of x Wg^T and x Wu^T are rounded to the type on the way:
+    in float16, fewer digits below 6e-5 and 0 below 3e-8.) Rows of dx outside the groups are left as they were (undefined in a
     tensor made here); NaN throughout, as in expert_ffn, if the offsets are out of order. `out` may hand back the dict of an earlier
     call for reuse; `scratch` is working memory of expert_scratch_bytes(R, I, groups, True). Not recorded by autograd, like expert_ffn."""
     _no_graph("expert_ffn_backward", dy, x, w_gate, w_up, w_down)

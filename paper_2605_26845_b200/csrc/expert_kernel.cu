@@ -17,9 +17,9 @@
 // Row tiles of the groups are laid out by a small kernel first (plan_kernel): a tile never spans two groups, what lies behind its
 // group's last row is computed and not stored. In DWEIGHT the rows are the contraction: there the rows behind
 // a group's last, up to the next multiple of 16, are zeroed in shared memory (0 x NaN would not be nothing).
-// Measured with eight experts, 4096 x 2048, 16384 rows: GLU 393 us (1.40 PFLOP/s, tensor cores busy 87 % of the cycles), DOWN 185,
-// DHIDDEN 262 (60 %: it moves 1.05 GB beside its product, a and u in 32 bits among them), DINPUT 374 (89 %), DWEIGHT 601 (77 %). The
-// clock is at 1.45 to 1.55 GHz then: what bounds the large products is the power.
+// Single launches of eight experts, 4096 x 2048, 16384 rows: GLU 361 us (1.52 PFLOP/s, tensor cores busy 89 % of the cycles), DOWN 161,
+// DHIDDEN 244 (60 %: it moves 1.0 GB beside its product, a and u in 32 bits among them), DINPUT 339 (93 %), DWEIGHT 563 (81 %), 1670 in all;
+// back to back they take 1960 to 2300 a pass, as the clock falls to 1.3 to 1.5 GHz: what bounds the large products is the power.
 #include <cuda.h>
 
 #include <atomic>

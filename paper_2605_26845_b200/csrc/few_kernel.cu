@@ -9,7 +9,8 @@
 // weight is unpacked once for all eight. Which k a lane holds is free as long as both operands agree on it: a lane takes
 // neighbouring k. In 4 bits an instruction never mixes the groups of scales: the sum over one group is made in 32 bits of
 // (q - 8) x, which 16-bit operands hold exactly, and scaled when it is added up.
-// 16 bits: bound by the memory (16 rows of four experts of 7168 x 2048: 58 us for gate, up and down, 353 MB, 6.1 TB/s). 4 bits: bound by
+// 16 bits: bound by the memory (16 rows of four experts of 7168 x 2048: 58 us for gate, up and down from a graph, 353 MB, 6.1 TB/s; 64 to 71
+// call by call, other rows and weights every time). 4 bits: bound by
 // the instructions that unpack, 5 (half) or 7 (bfloat16) for eight weights in the unit that shifts and masks, which issues every
 // second cycle (61 rows of 32 experts, 2048 to 7168: 67 us, 3.7 TB/s).
 #include "expert.cuh"
@@ -518,7 +519,7 @@ cudaError_t run_few(int R, int K, int N, int E, int groups, int group, int dtype
   FewArgs a{R, K, N, E, groups, 1, x, {w, w_up}, {scale, scale_up}, offsets, y, {sum, sum_up}, status};
   const bool gated = w_up != nullptr;
   // Warps share the k of an output only until half of the GPU's warps have a unit: every sharing costs a barrier and a sum (four
-  // experts of 7168 x 2048 in 16 bits, 16 rows: 60 us; until all have one 64, four each 73, a quarter of them 69).
+  // experts of 7168 x 2048 in 16 bits, 16 rows, from a graph: 60 us then, 58 now; until all have one 64, four each 73, a quarter of them 69).
   const long long units = (long long)(E < R ? E : R) * ((N + (gated ? 15 : 31)) / (gated ? 16 : 32));
   while (a.split < FEW_WARPS && 2 * units * a.split < (long long)FEW_WARPS * sm_count()) a.split *= 2;
   if (dtype == MOESCHED_BF16) {
