@@ -9,7 +9,7 @@
 // weight is unpacked once for all eight. Which k a lane holds is free as long as both operands agree on it: a lane takes
 // neighbouring k. In 4 bits an instruction never mixes the groups of scales: the sum over one group is made in 32 bits of
 // (q - 8) x, which 16-bit operands hold exactly, and scaled when it is added up.
-// 16 bits: bound by the memory (16 rows of four experts of 7168 x 2048: 58 us for gate, up and down from a graph, 353 MB, 6.1 TB/s; 64 to 71
+// 16 bits: bound by the memory (16 rows of four experts of 7168 x 2048: 58 us for gate, up and down from a graph, 353 MB, 6.1 TB/s; 61 to 71
 // call by call, other rows and weights every time). 4 bits: bound by
 // the instructions that unpack, 5 (half) or 7 (bfloat16) for eight weights in the unit that shifts and masks, which issues every
 // second cycle (61 rows of 32 experts, 2048 to 7168: 67 us, 3.7 TB/s).
