@@ -555,6 +555,110 @@ int moesched_expert_matvec4(int R, int K, int N, int E, int groups, int group, i
                             const int32_t* d_offsets, void* d_y, int32_t* d_status, void* stream);
 
 /*
+ * Tokens on their way to the send buffers and back: what surrounds the choices of moesched_route_demand (paper Sec. 2.1). Tensors are
+ * densely packed, row major, 16-byte aligned, of type MOESCHED_BF16, MOESCHED_FP16 or MOESCHED_FP32; D is a multiple of 8, 8 .. 65536.
+ * Sums and statistics are in 32 bits, outputs are rounded once. An output may take the place of an input only where that is said.
+ */
+#define MOESCHED_FP32 2
+#define MOESCHED_MAX_TOP_K 32
+
+/*
+ * Root-mean-square norm of every token, with the residual's addition before it and an output in 8 bits behind it:
+ *   h = x + r rounded to the type (without d_residual h = x),  c = 1 / sqrt(sum h^2 / D + eps),  y = h c w,
+ *   q = y / scale in e4m3 (rounded to nearest, at most 448),  scale = the greatest |y| of a group of columns / 448, 2^-126 at least.
+ * y is the norm of h as it is kept, in the type. q is rounded from y in 32 bits. (With 8 bits and a scale for every 128 columns a token is
+ * D + 4 ceil(D / 128) bytes on a link in place of 2 D: bytes_per_token of the model.) A NaN or an infinity in a row makes its y NaN,
+ * and the scales and what they stand for.
+ *
+ *   rows       in   0 .. MOESCHED_MAX_ROWS;  eps >= 0, finite
+ *   d_x        in   [rows][D];  d_residual  in  [rows][D] or NULL;  d_weight  in  [D]
+ *   d_sum      out  [rows][D]: h; NULL if and only if d_residual is. May be d_x or d_residual
+ *   d_y        out  [rows][D], may be d_x; may be NULL where d_q is given
+ *   d_q        out  [rows][D] e4m3 bytes, or NULL: `group` is not looked at then, and is 32, 64 or 128 otherwise
+ *   d_scale    out  [rows][ceil(D / group)] float; NULL if and only if d_q is
+ *   d_rstd     out  [rows] float: c, for the backward pass; may be NULL
+ */
+int moesched_rms_norm(int rows, int D, int dtype, float eps, int group, const void* d_x, const void* d_residual,
+                      const void* d_weight, void* d_sum, void* d_y, uint8_t* d_q, float* d_scale, float* d_rstd, void* stream);
+
+/*
+ * Its gradients, with g = dy w:  dx = c (g - h c^2 sum(g h) / D) + dsum (the residual's gradient is the same),  dw = sum over the rows of
+ * dy h c. The sum has a fixed order: results are the same bit for bit, call after call.
+ *
+ *   d_dy       in   [rows][D];  d_h  in  [rows][D]: d_sum of the forward call, or d_x;  d_rstd  in  [rows]
+ *   d_dsum     in   [rows][D]: the gradient that h has from elsewhere (the residual stream goes on), or NULL
+ *   d_dx       out  [rows][D], may be d_dy or d_dsum;  d_dweight  out  [D], 0 without rows: written, not added to
+ *   d_scratch  tmp  moesched_norm_scratch_bytes(rows, D) bytes. Contents are undefined afterwards; calls that overlap need their own
+ */
+size_t moesched_norm_scratch_bytes(int rows, int D);
+int moesched_rms_norm_backward(int rows, int D, int dtype, const void* d_dy, const void* d_h, const void* d_weight,
+                               const float* d_rstd, const void* d_dsum, void* d_dx, void* d_dweight, float* d_scratch, void* stream);
+
+/*
+ * The router's choice: for every token the k experts with the greatest score + bias and their weights. Scores are the softmax of the token's
+ * logits over the experts, or their logistic function. Experts come in falling order, the lowest first among equal ones (compared
+ * as in 64 bits; without a bias by the logits themselves). An expert whose logit (or score + bias) is -infinity or NaN is not chosen; a
+ * token that runs out of experts has -1 and weight 0 for the rest: choices that are not sent. Weights are scores times `factor`, without
+ * the bias; with `normalise`, scores over the sum of the chosen ones, times `factor`. A NaN among a token's logits makes its weights NaN.
+ *
+ *   rows       in   tokens, 0 .. MOESCHED_MAX_ROWS;  1 <= E <= MOESCHED_MAX_EXPERTS;  1 <= k <= min(E, MOESCHED_MAX_TOP_K)
+ *   factor     in   finite
+ *   d_logits   in   [rows][E], aligned to its type;  d_bias  in  [E] float, or NULL
+ *   d_experts  out  [rows][k] int32, as moesched_route_demand takes them;  d_weights  out  [rows][k] float
+ */
+#define MOESCHED_SCORE_SOFTMAX 0
+#define MOESCHED_SCORE_SIGMOID 1
+int moesched_route_choose(int rows, int E, int k, int dtype, int score, int normalise, float factor, const void* d_logits,
+                          const float* d_bias, int32_t* d_experts, float* d_weights, void* stream);
+
+/*
+ * Gradient of the logits from that of the weights (the choice itself has none, nor has the bias). d_experts as the forward call wrote them;
+ * entries outside 0 .. E-1 were not chosen. A token's experts are different ones.
+ *   d_dweights  in  [rows][k] float;  d_dlogits  out  [rows][E], written throughout
+ */
+int moesched_route_choose_backward(int rows, int E, int k, int dtype, int score, int normalise, float factor,
+                                   const float* d_dweights, const void* d_logits, const int32_t* d_experts, void* d_dlogits,
+                                   void* stream);
+
+/*
+ * Tokens to the rows of their send buffers, by expert: rows[g][slot[g][t k + j]] = x[g][t] for every choice j of token t. d_slot is
+ * moesched_route_demand's, the G sources being its B * N ranks (or one rank alone); a slot that is not one of the T * k rows is not sent.
+ * Rows that no slot names are left as they were. The slots of a source are distinct; of two choices with one slot, which is a caller's
+ * mistake, either's row stays, or parts of both.
+ *
+ *   G, T, k    in   G, T >= 0, G * T <= MOESCHED_MAX_ROWS, 1 <= k <= MOESCHED_MAX_TOP_K, T * k <= 2^31-1
+ *   row_bytes  in   of a token: a multiple of 8, 8 .. 2^18
+ *   scales     in   floats that go with a token (those of its 8-bit groups): 0 .. 65536; d_scale and d_row_scale are NULL if and only if 0
+ *   d_x        in   [G][T] rows;  d_scale  in  [G][T][scales];  d_slot  in  [G][T * k] int32
+ *   d_rows     out  [G][T * k] rows;  d_row_scale  out  [G][T * k][scales]
+ */
+int moesched_tokens_to_rows(int G, int T, int k, int row_bytes, int scales, const void* d_x, const float* d_scale,
+                            const int32_t* d_slot, void* d_rows, float* d_row_scale, void* stream);
+
+/*
+ * And back: y[g][t] = add[g][t] + sum over j of weight[g][t k + j] * rows[g][slot[g][t k + j]], in the order of j. A choice that was not sent
+ * adds nothing, whatever its weight. Without weights it is the sum of the rows: the gradient of moesched_tokens_to_rows.
+ *
+ *   d_rows     in   [G][T * k][D];  d_slot  in  [G][T * k];  d_weights  in  [G][T * k] float, or NULL: all 1
+ *   d_add      in   [G][T][D], or NULL;  d_y  out  [G][T][D], may be d_add
+ */
+int moesched_rows_to_tokens(int G, int T, int k, int D, int dtype, const void* d_rows, const int32_t* d_slot,
+                            const float* d_weights, const void* d_add, void* d_y, void* stream);
+
+/*
+ * Its gradients: drows[g][slot] = weight * dy[g][t],  dweights[g][t k + j] = <dy[g][t], rows[g][slot]>, 0 for a choice that was not sent.
+ * (That of d_add is dy.) Rows that no slot names are left as they were. d_drows may be d_rows.
+ */
+int moesched_rows_to_tokens_backward(int G, int T, int k, int D, int dtype, const void* d_dy, const void* d_rows,
+                                     const int32_t* d_slot, const float* d_weights, void* d_drows, float* d_dweights, void* stream);
+
+/*
+ * Rows in 8 bits, as they arrive, to rows of a type: y = q scale.
+ *   d_q  in  [R][D] e4m3 bytes;  d_scale  in  [R][ceil(D / group)] float, group 32, 64 or 128;  d_y  out  [R][D];  R <= MOESCHED_MAX_ROWS
+ */
+int moesched_rows_widen(int R, int D, int group, int dtype, const uint8_t* d_q, const float* d_scale, void* d_y, void* stream);
+
+/*
  * Measurement aid (no counterpart in the paper): enqueue a kernel of `blocks` CTAs of 256
  * threads, each thread running 8 independent chains of add / min / xor for `iters`
  * iterations, and return the number of integer lane-operations it executes

@@ -1,4 +1,5 @@
 // C ABI of the library: argument checks, launch geometry, error reporting.
+#include <cfloat>
 #include <vector>
 
 #include "common.cuh"
@@ -79,6 +80,20 @@ static bool expert_sizes_ok(int R, int E, int groups, int dtype, int act) {
          (dtype == MOESCHED_BF16 || dtype == MOESCHED_FP16) && (act == MOESCHED_ACT_SILU || act == MOESCHED_ACT_GELU);
 }
 static bool ffn_width_ok(int v) { return v >= 8 && v <= 65536 && v % 8 == 0; }
+
+static bool aligned_to(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+static bool token_type_ok(int dtype) { return dtype == MOESCHED_BF16 || dtype == MOESCHED_FP16 || dtype == MOESCHED_FP32; }
+static bool token_sizes_ok(int rows, int D, int dtype) {
+  return rows >= 0 && rows <= MOESCHED_MAX_ROWS && ffn_width_ok(D) && token_type_ok(dtype);
+}
+static bool group_ok(int group) { return group == 32 || group == 64 || group == 128; }
+static bool choose_sizes_ok(int rows, int E, int k, int dtype, int score, float factor) {
+  return rows >= 0 && rows <= MOESCHED_MAX_ROWS && E >= 1 && E <= MOESCHED_MAX_EXPERTS && k >= 1 && k <= E && k <= MOESCHED_MAX_TOP_K &&
+         token_type_ok(dtype) && (score == MOESCHED_SCORE_SOFTMAX || score == MOESCHED_SCORE_SIGMOID) && factor >= -FLT_MAX && factor <= FLT_MAX;
+}
+static bool rows_sizes_ok(int G, int T, int k) {
+  return G >= 0 && T >= 0 && (int64_t)G * T <= MOESCHED_MAX_ROWS && k >= 1 && k <= MOESCHED_MAX_TOP_K && (int64_t)T * k <= 0x7fffffff;
+}
 
 }  // namespace moesched
 
@@ -431,6 +446,108 @@ int moesched_expert_matvec4(int R, int K, int N, int E, int groups, int group, i
   if (!aligned16(d_w_up) || !aligned16(d_scale_up)) return MOESCHED_EINVAL;
   cudaError_t e = run_few(R, K, N, E, groups, group, dtype, act, d_x, d_w, d_scale, d_w_up, d_scale_up, d_offsets, d_y, nullptr,
                           nullptr, d_status, false, static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? MOESCHED_OK : fail_cuda(e);
+}
+
+int moesched_rms_norm(int rows, int D, int dtype, float eps, int group, const void* d_x, const void* d_residual,
+                      const void* d_weight, void* d_sum, void* d_y, uint8_t* d_q, float* d_scale, float* d_rstd, void* stream) {
+  if (!token_sizes_ok(rows, D, dtype) || !(eps >= 0.0f && eps <= FLT_MAX)) return MOESCHED_EINVAL;
+  if (d_q != nullptr && !group_ok(group)) return MOESCHED_EINVAL;
+  if (rows == 0) return MOESCHED_OK;
+  if (!d_x || !d_weight || (!d_y && !d_q) || (d_residual == nullptr) != (d_sum == nullptr) || (d_q == nullptr) != (d_scale == nullptr))
+    return MOESCHED_EINVAL;
+  const void* pointers[] = {d_x, d_residual, d_weight, d_sum, d_y, d_q, d_scale};
+  for (const void* p : pointers)
+    if (!aligned16(p)) return MOESCHED_EINVAL;
+  if (!aligned4(d_rstd)) return MOESCHED_EINVAL;
+  cudaError_t e = run_norm(rows, D, dtype, eps, group, d_x, d_residual, d_weight, d_sum, d_y, d_q, d_scale, d_rstd,
+                           static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? MOESCHED_OK : fail_cuda(e);
+}
+
+size_t moesched_norm_scratch_bytes(int rows, int D) { return token_sizes_ok(rows, D, MOESCHED_FP32) ? norm_scratch_bytes(rows, D) : 0; }
+
+int moesched_rms_norm_backward(int rows, int D, int dtype, const void* d_dy, const void* d_h, const void* d_weight,
+                               const float* d_rstd, const void* d_dsum, void* d_dx, void* d_dweight, float* d_scratch, void* stream) {
+  if (!token_sizes_ok(rows, D, dtype) || !d_dweight || !aligned16(d_dweight)) return MOESCHED_EINVAL;
+  const void* pointers[] = {d_dy, d_h, d_weight, d_dx, d_scratch};
+  for (const void* p : pointers)
+    if ((rows > 0 && p == nullptr) || !aligned16(p)) return MOESCHED_EINVAL;
+  if ((rows > 0 && !d_rstd) || !aligned4(d_rstd) || !aligned16(d_dsum)) return MOESCHED_EINVAL;
+  cudaError_t e = run_norm_backward(rows, D, dtype, d_dy, d_h, d_weight, d_rstd, d_dsum, d_dx, d_dweight, d_scratch,
+                                    static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? MOESCHED_OK : fail_cuda(e);
+}
+
+int moesched_route_choose(int rows, int E, int k, int dtype, int score, int normalise, float factor, const void* d_logits,
+                          const float* d_bias, int32_t* d_experts, float* d_weights, void* stream) {
+  if (!choose_sizes_ok(rows, E, k, dtype, score, factor)) return MOESCHED_EINVAL;
+  if (rows == 0) return MOESCHED_OK;
+  if (!d_logits || !d_experts || !d_weights || !aligned_to(d_logits, dtype == MOESCHED_FP32 ? 4 : 2) || !aligned4(d_bias) ||
+      !aligned4(d_experts) || !aligned4(d_weights))
+    return MOESCHED_EINVAL;
+  cudaError_t e = run_choose(rows, E, k, dtype, score, normalise != 0, factor, d_logits, d_bias, d_experts, d_weights,
+                             static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? MOESCHED_OK : fail_cuda(e);
+}
+
+int moesched_route_choose_backward(int rows, int E, int k, int dtype, int score, int normalise, float factor,
+                                   const float* d_dweights, const void* d_logits, const int32_t* d_experts, void* d_dlogits,
+                                   void* stream) {
+  if (!choose_sizes_ok(rows, E, k, dtype, score, factor)) return MOESCHED_EINVAL;
+  if (rows == 0) return MOESCHED_OK;
+  const size_t size = dtype == MOESCHED_FP32 ? 4 : 2;
+  if (!d_dweights || !d_logits || !d_experts || !d_dlogits || !aligned_to(d_logits, size) || !aligned_to(d_dlogits, size) ||
+      !aligned4(d_dweights) || !aligned4(d_experts))
+    return MOESCHED_EINVAL;
+  cudaError_t e = run_choose_backward(rows, E, k, dtype, score, normalise != 0, factor, d_dweights, d_logits, d_experts, d_dlogits,
+                                      static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? MOESCHED_OK : fail_cuda(e);
+}
+
+int moesched_tokens_to_rows(int G, int T, int k, int row_bytes, int scales, const void* d_x, const float* d_scale,
+                            const int32_t* d_slot, void* d_rows, float* d_row_scale, void* stream) {
+  if (!rows_sizes_ok(G, T, k) || row_bytes < 8 || row_bytes > (1 << 18) || row_bytes % 8 != 0 || scales < 0 || scales > 65536)
+    return MOESCHED_EINVAL;
+  if (G == 0 || T == 0) return MOESCHED_OK;
+  if (!d_x || !d_slot || !d_rows || (scales == 0) != (d_scale == nullptr) || (scales == 0) != (d_row_scale == nullptr))
+    return MOESCHED_EINVAL;
+  const void* pointers[] = {d_x, d_scale, d_rows, d_row_scale};
+  for (const void* p : pointers)
+    if (!aligned16(p)) return MOESCHED_EINVAL;
+  if (!aligned4(d_slot)) return MOESCHED_EINVAL;
+  cudaError_t e = run_tokens_to_rows(G, T, k, row_bytes, scales, d_x, d_scale, d_slot, d_rows, d_row_scale,
+                                     static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? MOESCHED_OK : fail_cuda(e);
+}
+
+int moesched_rows_to_tokens(int G, int T, int k, int D, int dtype, const void* d_rows, const int32_t* d_slot,
+                            const float* d_weights, const void* d_add, void* d_y, void* stream) {
+  if (!rows_sizes_ok(G, T, k) || !token_sizes_ok(0, D, dtype)) return MOESCHED_EINVAL;
+  if (G == 0 || T == 0) return MOESCHED_OK;
+  if (!d_rows || !d_slot || !d_y || !aligned16(d_rows) || !aligned16(d_add) || !aligned16(d_y) || !aligned4(d_slot) || !aligned4(d_weights))
+    return MOESCHED_EINVAL;
+  cudaError_t e = run_rows_to_tokens(G, T, k, D, dtype, d_rows, d_slot, d_weights, d_add, d_y, static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? MOESCHED_OK : fail_cuda(e);
+}
+
+int moesched_rows_to_tokens_backward(int G, int T, int k, int D, int dtype, const void* d_dy, const void* d_rows,
+                                     const int32_t* d_slot, const float* d_weights, void* d_drows, float* d_dweights, void* stream) {
+  if (!rows_sizes_ok(G, T, k) || !token_sizes_ok(0, D, dtype)) return MOESCHED_EINVAL;
+  if (G == 0 || T == 0) return MOESCHED_OK;
+  if (!d_dy || !d_rows || !d_slot || !d_weights || !d_drows || !d_dweights || !aligned16(d_dy) || !aligned16(d_rows) ||
+      !aligned16(d_drows) || !aligned4(d_slot) || !aligned4(d_weights) || !aligned4(d_dweights))
+    return MOESCHED_EINVAL;
+  cudaError_t e = run_rows_to_tokens_backward(G, T, k, D, dtype, d_dy, d_rows, d_slot, d_weights, d_drows, d_dweights,
+                                              static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? MOESCHED_OK : fail_cuda(e);
+}
+
+int moesched_rows_widen(int R, int D, int group, int dtype, const uint8_t* d_q, const float* d_scale, void* d_y, void* stream) {
+  if (!token_sizes_ok(R, D, dtype) || !group_ok(group)) return MOESCHED_EINVAL;
+  if (R == 0) return MOESCHED_OK;
+  if (!d_q || !d_scale || !d_y || !aligned16(d_q) || !aligned16(d_scale) || !aligned16(d_y)) return MOESCHED_EINVAL;
+  cudaError_t e = run_rows_widen(R, D, group, dtype, d_q, d_scale, d_y, static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? MOESCHED_OK : fail_cuda(e);
 }
 

@@ -277,6 +277,24 @@ cudaError_t run_expert_backward(int R, int D, int I, int E, int groups, int dtyp
                                 const float* gate, const float* up, void* dx, void* dw_gate, void* dw_up, void* dw_down,
                                 void* scratch, int32_t* status, cudaStream_t stream);
 
+// norm of tokens (norm_kernel.cu), the router's choice (choose_kernel.cu), tokens to rows and back (rows_kernel.cu)
+cudaError_t run_norm(int rows, int D, int dtype, float eps, int group, const void* x, const void* residual, const void* weight,
+                     void* sum, void* y, uint8_t* q, float* scale, float* rstd, cudaStream_t stream);
+size_t norm_scratch_bytes(int rows, int D);
+cudaError_t run_norm_backward(int rows, int D, int dtype, const void* dy, const void* h, const void* weight, const float* rstd,
+                              const void* dsum, void* dx, void* dweight, float* scratch, cudaStream_t stream);
+cudaError_t run_choose(int rows, int E, int k, int dtype, int score, int normalise, float factor, const void* logits, const float* bias,
+                       int32_t* experts, float* weights, cudaStream_t stream);
+cudaError_t run_choose_backward(int rows, int E, int k, int dtype, int score, int normalise, float factor, const float* dweights,
+                                const void* logits, const int32_t* experts, void* dlogits, cudaStream_t stream);
+cudaError_t run_tokens_to_rows(int G, int T, int k, int row_bytes, int scales, const void* x, const float* scale, const int32_t* slot,
+                               void* rows, float* row_scale, cudaStream_t stream);
+cudaError_t run_rows_to_tokens(int G, int T, int k, int D, int dtype, const void* rows, const int32_t* slot, const float* weights,
+                               const void* add, void* y, cudaStream_t stream);
+cudaError_t run_rows_to_tokens_backward(int G, int T, int k, int D, int dtype, const void* dy, const void* rows, const int32_t* slot,
+                                        const float* weights, void* drows, float* dweights, cudaStream_t stream);
+cudaError_t run_rows_widen(int R, int D, int group, int dtype, const uint8_t* q, const float* scale, void* y, cudaStream_t stream);
+
 // All of an SM's memory that can be shared memory is, while the kernel runs there. (A preference: failing is harmless.)
 template <typename Kernel>
 void prefer_shared_memory(Kernel kern) {
