@@ -6,7 +6,10 @@
 // Weights come from the logits of the chosen alone where they are normalised:
 //   softmax   w = e^(l - m) / sum e^(l - m),  m the greatest of them
 //   logistic  w = t / sum t,  t = e^(l - m) / (1 + e^l),  m = min(0, the greatest): it has no common factor left that could underflow
-// One warp has a token, lane i the experts i, i + 32, ...; the greatest is found with two reductions over the warp (value, then lowest expert).
+// One warp has a token, lane i the experts i J .. i J + J - 1. It finds a bound that no wanted key is below, gathers what is left (10 of 256 usually) one a
+// lane, and each counts the keys before its own. Instructions bound it, 300 to 400 a token.
+#include <cfloat>
+
 #include "token.cuh"
 
 namespace moesched {
@@ -19,7 +22,6 @@ __device__ __forceinline__ unsigned ordered(float v) {
   const unsigned u = __float_as_uint(v + 0.0f);                  // (-0 and 0 are equal)
   return (u & 0x80000000u) != 0u ? ~u : u | 0x80000000u;
 }
-__device__ __forceinline__ float unordered(unsigned u) { return __uint_as_float((u & 0x80000000u) != 0u ? u ^ 0x80000000u : ~u); }
 __device__ __forceinline__ unsigned long long ordered(double v) {
   if (!(v > -INFINITY)) return 0ull;
   const unsigned long long u = (unsigned long long)__double_as_longlong(v + 0.0);
@@ -32,45 +34,120 @@ __device__ __forceinline__ unsigned long long warp_most(unsigned long long v) {
   return (unsigned long long)hi << 32 | lo;
 }
 __device__ __forceinline__ float warp_most(float v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(FULL, v, o));
+  asm volatile("redux.sync.max.f32 %0, %0, 0xffffffff;" : "+f"(v));
   return v;
 }
 
-// Lane i gets the expert of the i-th greatest key, -1 where no key is left; `between(a, b)` sees each key and the next, as many as `count` + 1
-template <int J, typename Key, typename Between>
-__device__ __forceinline__ int greatest(Key (&key)[J], int count, Between between) {
+// Lane i gets the expert of the i-th greatest key, -1 where no key is left, `count` of them in falling order
+template <int J, typename Key>
+__device__ __forceinline__ int greatest(Key (&key)[J], int count) {
   const int lane = threadIdx.x & 31;
   int mine = -1;
-  Key before = 0;
-  for (int r = 0;; ++r) {
-    Key best = 0;
+  for (int r = 0; r < count; ++r) {
+    Key best = key[0];
     int at = 0;
 #pragma unroll
-    for (int j = 0; j < J; ++j) {
+    for (int j = 1; j < J; ++j) {
       at = key[j] > best ? j : at;
       best = key[j] > best ? key[j] : best;
     }
     const Key most = warp_most(best);
-    if (r > 0) between(before, most);
-    if (r == count || most == 0) break;
-    const int expert = (int)__reduce_min_sync(FULL, best == most ? 32u * at + lane : 0xffffffffu);
+    if (most == 0) break;
+    const int expert = (int)__reduce_min_sync(FULL, best == most ? (unsigned)(lane * J + at) : 0xffffffffu);
     if (lane == r) mine = expert;
 #pragma unroll
-    for (int j = 0; j < J; ++j) key[j] = 32 * j + lane == expert ? Key(0) : key[j];
-    before = most;
+    for (int j = 0; j < J; ++j) key[j] = lane * J + j == expert ? Key(0) : key[j];
   }
   return mine;
 }
 
-template <typename T, int J>
-__device__ __forceinline__ void load_logits(const T* logits, int E, float (&l)[J]) {
+// The keys that may be among the `count` greatest, in falling order, the lowest expert first among equal ones: lane i gets the i-th. The count-th greatest of
+// the lanes' own greatest keys has `count` keys at or above it, so that nothing below it is wanted; spare(key) is the lowest key that has to be looked at
+// all the same. Returns how many there are: with more than 32, nothing else holds. -infinity and NaN are no keys. list: [64], of the warp.
+template <int J, typename Spare>
+__device__ __forceinline__ int candidates(const float (&key)[J], int count, uint2* list, Spare spare, float& own, int& expert) {
+  const int lane = threadIdx.x & 31;
+  float best = fmaxf(key[0], -INFINITY);
 #pragma unroll
-  for (int j = 0; j < J; ++j) {
-    const int e = 32 * j + (threadIdx.x & 31);
-    l[j] = e < E ? to_float(logits[e]) : -INFINITY;
+  for (int j = 1; j < J; ++j) best = fmaxf(best, key[j]);
+  float bound = -INFINITY;
+  for (int r = 0; r < count; ++r) {                             // (equal ones go together: the bound is only lower for it)
+    bound = warp_most(best);
+    best = best == bound ? -INFINITY : best;
+  }
+  bound = fmaxf(spare(bound), -FLT_MAX);
+  int at = 0, found = 0;
+  if constexpr (J <= 4) {
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      const unsigned who = __ballot_sync(FULL, key[j] >= bound);
+      at += __popc(who & ((1u << lane) - 1u));
+      found += __popc(who);
+    }
+  } else {
+    int mine = 0;
+#pragma unroll
+    for (int j = 0; j < J; ++j) mine += key[j] >= bound;
+    at = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(FULL, at, o);
+      if (lane >= o) at += v;
+    }
+    found = __shfl_sync(FULL, at, 31);
+    at -= mine;
+  }
+  if (found > 32) return found;
+#pragma unroll
+  for (int j = 0; j < J; ++j)
+    if (key[j] >= bound) list[at++] = make_uint2(__float_as_uint(key[j]), lane * J + j);
+  __syncwarp();
+  const uint2 entry = lane < found ? list[lane] : make_uint2(0xff800000u, 0u);
+  const unsigned mine = ordered(__uint_as_float(entry.x));
+  int place = 0;
+#pragma unroll 4
+  for (int i = 0; i < found; ++i) {
+    const unsigned other = __shfl_sync(FULL, mine, i);
+    place += other + (i < lane) > mine;                         // (no key is the greatest number)
+  }
+  if (lane < found) list[32 + place] = entry;
+  __syncwarp();
+  const uint2 sorted = lane < found ? list[32 + lane] : make_uint2(0xff800000u, 0xffffffffu);
+  own = __uint_as_float(sorted.x);
+  expert = (int)sorted.y;
+  return found;
+}
+
+// How near two scores with their biases, in 32 bits, may be to one another without their order being known. A score is at most 1 and off by 2^-18 at most (its
+// exponential by 2 steps of 2^-23 and by those of its argument, at most x 2^-23 with x e^-x < 0.4; the sum of up to 32 on a lane and over 32 lanes by 37 half
+// steps; the quotient by 2 steps), the sum with the bias by half a step of its own.
+__device__ __forceinline__ float apart(float u, float v) { return 0x1p-17f + 0x1p-23f * (fabsf(u) + fabsf(v)); }
+
+// The lane's logits, -infinity where there is no expert. WIDE: as many as 16 bytes hold at a time
+template <typename T, int J, bool WIDE>
+__device__ __forceinline__ void load_logits(const T* logits, int E, float (&l)[J]) {
+  constexpr int COUNT = Vec<T>::COUNT;
+  const int first = (threadIdx.x & 31) * J;
+  if constexpr (WIDE && J % COUNT == 0) {
+#pragma unroll
+    for (int j = 0; j < J; j += COUNT) {
+      float f[COUNT];
+      uint4 v = make_uint4(0u, 0u, 0u, 0u);
+      const bool in = first + j < E;
+      if (in) v = __ldg(reinterpret_cast<const uint4*>(logits + first + j));
+      Vec<T>::unpack(v, f);
+#pragma unroll
+      for (int q = 0; q < COUNT; ++q) l[j + q] = in ? f[q] : -INFINITY;
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < J; ++j) l[j] = first + j < E ? to_float(logits[first + j]) : -INFINITY;
   }
 }
+
+// e^v; the quotients below are of numbers between 2^-126 and 2^126, or have no meaning
+__device__ __forceinline__ float exponential(float v) { return __expf(v); }
+__device__ __forceinline__ float logistic(float v) { return __fdividef(1.0f, 1.0f + exponential(-v)); }
 
 // greatest logit of the row, and the sum of e^(l - m); the sum of a row without a logit is 0
 template <int J>
@@ -82,8 +159,17 @@ __device__ __forceinline__ void softmax_of(const float (&l)[J], float& m, float&
   sum = 0.0f;
   if (m == -INFINITY) return;
 #pragma unroll
-  for (int j = 0; j < J; ++j) sum += expf(l[j] - m);
+  for (int j = 0; j < J; ++j) sum += exponential(l[j] - m);
   sum = warp_sum(sum);
+}
+
+// Normalised scores of the chosen, a lane's from its logit: see above
+template <bool SOFTMAX>
+__device__ __forceinline__ float normalised(float l, bool there) {
+  const float most = warp_most(l), m = SOFTMAX ? most : fminf(most, 0.0f);
+  float w = SOFTMAX ? exponential(l - m) : l > 0.0f ? logistic(l) : __fdividef(exponential(l - m), 1.0f + exponential(l));
+  w = there ? w : 0.0f;
+  return __fdividef(w, warp_sum(w));
 }
 
 __device__ __noinline__ double exp64(double v) { return exp(v); }
@@ -91,7 +177,7 @@ __device__ __noinline__ double exp64(double v) { return exp(v); }
 // Scores and choices in 64 bits
 template <int J, int SCORE>
 __device__ __noinline__ int choose64(const float (&l)[J], const float* bias, int E, int k, float top) {
-  const int lane = threadIdx.x & 31;
+  const int first = (threadIdx.x & 31) * J;
   double sum = 0.0;
   unsigned long long key[J];
   if constexpr (SCORE == MOESCHED_SCORE_SOFTMAX) {
@@ -102,68 +188,63 @@ __device__ __noinline__ int choose64(const float (&l)[J], const float* bias, int
   }
 #pragma unroll
   for (int j = 0; j < J; ++j) {
-    const int e = 32 * j + lane;
     key[j] = 0ull;
-    if (e >= E || !(l[j] > -INFINITY)) continue;
+    if (first + j >= E || !(l[j] > -INFINITY)) continue;
     const double s = SCORE == MOESCHED_SCORE_SOFTMAX ? exp64((double)l[j] - (double)top) / sum : 1.0 / (1.0 + exp64(-(double)l[j]));
-    key[j] = ordered(s + (double)bias[e]);
+    key[j] = ordered(s + (double)bias[first + j]);
   }
-  return greatest(key, k, [](unsigned long long, unsigned long long) {});
+  return greatest(key, k);
 }
 
-template <typename T, int J, int SCORE>
+template <typename T, int J, int SCORE, bool WIDE>
 __global__ void __launch_bounds__(32 * CHOOSE_WARPS) choose_kernel(int rows, int E, int k, int normalise, float factor,
                                                                    const T* __restrict__ logits, const float* __restrict__ bias,
                                                                    int32_t* __restrict__ experts, float* __restrict__ weights) {
   constexpr bool SOFTMAX = SCORE == MOESCHED_SCORE_SOFTMAX;
+  __shared__ uint2 lists[CHOOSE_WARPS][64];
+  uint2* list = lists[threadIdx.x >> 5];
   const int lane = threadIdx.x & 31;
   const long long row = (long long)blockIdx.x * CHOOSE_WARPS + (threadIdx.x >> 5);
   if (row >= rows) return;
   const T* own = logits + row * E;
   float l[J], top = 0.0f, sum = 0.0f;
-  load_logits(own, E, l);
-  bool lost = false;
+  load_logits<T, J, WIDE>(own, E, l);
+  float most = l[0];                                             // NaN if one of them is
 #pragma unroll
-  for (int j = 0; j < J; ++j) lost |= isnan(l[j]);
-  lost = __any_sync(FULL, lost);
+  for (int j = 1; j < J; ++j) asm("max.NaN.f32 %0, %0, %1;" : "+f"(most) : "f"(l[j]));
+  const bool lost = __any_sync(FULL, isnan(most));
   if (SOFTMAX && (bias != nullptr || !normalise)) softmax_of(l, top, sum);
-  unsigned key[J];
-  int expert;
+  float mine;
+  int expert, found;
   if (bias == nullptr) {
+    found = candidates(l, k, list, [](float b) { return b; }, mine, expert);
+    if (found > 32) {
+      unsigned key[J];
 #pragma unroll
-    for (int j = 0; j < J; ++j) key[j] = ordered(l[j]);
-    expert = greatest(key, k, [](unsigned, unsigned) {});
+      for (int j = 0; j < J; ++j) key[j] = ordered(l[j]);
+      expert = greatest(key, k);
+      mine = expert >= 0 ? to_float(own[expert]) : -INFINITY;
+    }
   } else {
-    bool near = false;
+    float key[J];
+    const float share = SOFTMAX ? __fdividef(1.0f, sum) : 0.0f;
 #pragma unroll
     for (int j = 0; j < J; ++j) {
-      const int e = 32 * j + lane;
-      const float s = SOFTMAX ? expf(l[j] - top) / sum : 1.0f / (1.0f + expf(-l[j]));
-      key[j] = e < E && l[j] > -INFINITY ? ordered(s + bias[e]) : 0u;
+      const int e = lane * J + j;
+      const float s = SOFTMAX ? exponential(l[j] - top) * share : logistic(l[j]);
+      key[j] = e < E && l[j] > -INFINITY ? s + __ldg(bias + e) : -INFINITY;
     }
-    // A score is at most 1 and off by 2^-18 at most (its exponential by 2 steps of 2^-23 and by that of its argument, which is x 2^-24 with x e^-x < 0.4;
-    // the sum of up to 32 on a lane and over 32 lanes by 37 half steps; the quotient), the sum with the bias by half a step of its own.
-    expert = greatest(key, k, [&](unsigned a, unsigned b) {
-      if (b == 0u) return;
-      const float u = unordered(a), v = unordered(b);
-      near |= !(u - v > 0x1p-17f + 0x1p-23f * (fabsf(u) + fabsf(v)));
-    });
-    if (near) expert = choose64<J, SCORE>(l, bias, E, k, top);
+    found = candidates(key, k, list, [](float b) { return b - 2.0f * apart(b, b); }, mine, expert);
+    const float next = __shfl_down_sync(FULL, mine, 1);
+    const bool near = lane < k && lane + 1 < found && !(mine - next > apart(mine, next));
+    if (found > 32 || __any_sync(FULL, near)) expert = choose64<J, SCORE>(l, bias, E, k, top);
+    mine = expert >= 0 ? to_float(own[expert]) : -INFINITY;
   }
-  const bool there = expert >= 0;
-  const float mine = there ? to_float(own[expert]) : -INFINITY;
-  float w;
-  if (normalise) {
-    const float most = warp_most(mine), m = SOFTMAX ? most : fminf(most, 0.0f);
-    if (SOFTMAX) w = expf(mine - m);
-    else w = mine > 0.0f ? 1.0f / (1.0f + expf(-mine)) : expf(mine - m) / (1.0f + expf(mine));
-    w = there ? w : 0.0f;
-    w = w / warp_sum(w);
-  } else {
-    w = SOFTMAX ? expf(mine - top) / sum : 1.0f / (1.0f + expf(-mine));
-  }
+  const bool there = lane < k && expert >= 0;
+  if (!there) mine = -INFINITY;
+  const float w = normalise ? normalised<SOFTMAX>(mine, there) : SOFTMAX ? __fdividef(exponential(mine - top), sum) : logistic(mine);
   if (lane < k) {
-    experts[row * k + lane] = expert;
+    experts[row * k + lane] = there ? expert : -1;
     weights[row * k + lane] = lost ? NAN : there ? w * factor : 0.0f;
   }
 }
@@ -172,49 +253,60 @@ __global__ void __launch_bounds__(32 * CHOOSE_WARPS) choose_kernel(int rows, int
 //   softmax             p (a [chosen] - sum a p)      over all experts
 //   softmax, normalised q (a - sum a q)               over the chosen, 0 for the others
 //   logistic            a s (1 - s);  normalised  q (a - sum a q) (1 - s)
-template <typename T, int J, int SCORE>
+template <typename T, int J, int SCORE, bool WIDE>
 __global__ void __launch_bounds__(32 * CHOOSE_WARPS) choose_backward_kernel(int rows, int E, int k, int normalise, float factor,
                                                                             const float* __restrict__ dweights,
                                                                             const T* __restrict__ logits,
                                                                             const int32_t* __restrict__ experts, T* dlogits) {
   constexpr bool SOFTMAX = SCORE == MOESCHED_SCORE_SOFTMAX;
+  constexpr int COUNT = Vec<T>::COUNT;
   const int lane = threadIdx.x & 31;
   const long long row = (long long)blockIdx.x * CHOOSE_WARPS + (threadIdx.x >> 5);
   if (row >= rows) return;
   const T* own = logits + row * E;
   T* out = dlogits + row * E;
   int expert = lane < k ? experts[row * k + lane] : -1;
+  float a = lane < k ? dweights[row * k + lane] * factor : 0.0f;
+  const bool all = SOFTMAX && !normalise;
+  if (!all) {                                                    // zeros, while the choices are on their way
+    if (WIDE)
+      for (int e = lane * COUNT; e < E; e += 32 * COUNT) *reinterpret_cast<uint4*>(out + e) = make_uint4(0u, 0u, 0u, 0u);
+    else
+      for (int e = lane; e < E; e += 32) put(out + e, 0.0f);
+  }
   if ((unsigned)expert >= (unsigned)E) expert = -1;
   const bool there = expert >= 0;
   const float mine = there ? to_float(own[expert]) : -INFINITY;
-  const float a = there ? dweights[row * k + lane] * factor : 0.0f;
-  float d, dot = 0.0f;
-  if (normalise) {
-    const float most = warp_most(mine), m = SOFTMAX ? most : fminf(most, 0.0f);
-    float q;
-    if (SOFTMAX) q = expf(mine - m);
-    else q = mine > 0.0f ? 1.0f / (1.0f + expf(-mine)) : expf(mine - m) / (1.0f + expf(mine));
-    q = there ? q : 0.0f;
-    q = q / warp_sum(q);
-    dot = warp_sum(there ? a * q : 0.0f);
-    d = q * (a - dot);
-    if (!SOFTMAX) d /= 1.0f + expf(mine);                        // 1 - s
-  } else if (SOFTMAX) {
+  a = there ? a : 0.0f;
+  float d;
+  if (all) {
     float l[J], top, sum;
-    load_logits(own, E, l);
+    load_logits<T, J, WIDE>(own, E, l);
     softmax_of(l, top, sum);
-    const float p = there ? expf(mine - top) / sum : 0.0f;
-    dot = warp_sum(a * p);
+    const float share = __fdividef(1.0f, sum), p = there ? exponential(mine - top) * share : 0.0f, dot = warp_sum(a * p);
     d = p * (a - dot);
 #pragma unroll
-    for (int j = 0; j < J; ++j)
-      if (32 * j + lane < E) put(out + 32 * j + lane, l[j] == -INFINITY ? 0.0f : expf(l[j] - top) / sum * -dot);
+    for (int j = 0; j < J; ++j) l[j] = l[j] == -INFINITY ? 0.0f : exponential(l[j] - top) * share * -dot;
+    if constexpr (WIDE && J % COUNT == 0) {
+#pragma unroll
+      for (int j = 0; j < J; j += COUNT) {
+        float f[COUNT];
+#pragma unroll
+        for (int q = 0; q < COUNT; ++q) f[q] = l[j + q];
+        if (lane * J + j < E) *reinterpret_cast<uint4*>(out + lane * J + j) = Vec<T>::pack(f);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < J; ++j)
+        if (lane * J + j < E) put(out + lane * J + j, l[j]);
+    }
+  } else if (normalise) {
+    const float q = normalised<SOFTMAX>(mine, there), dot = warp_sum(there ? a * q : 0.0f);
+    d = q * (a - dot);
+    if (!SOFTMAX) d = __fdividef(d, 1.0f + exponential(mine));   // 1 - s
   } else {
-    const float s = 1.0f / (1.0f + expf(-mine));
-    d = a * s / (1.0f + expf(mine));
+    d = __fdividef(a * logistic(mine), 1.0f + exponential(mine));
   }
-  if (!SOFTMAX || normalise)
-    for (int e = lane; e < E; e += 32) put(out + e, 0.0f);
   __syncwarp();                                                  // the chosen after all of them
   if (there) put(out + expert, d);
 }
@@ -229,31 +321,41 @@ static cudaError_t with_experts(int E, Call call) {
   return call(std::integral_constant<int, 32>());
 }
 
+// Rows of logits start and end on 16 bytes
+template <typename T>
+static bool wide_rows(int E, const void* p, const void* q) {
+  return E % Vec<T>::COUNT == 0 && (reinterpret_cast<uintptr_t>(p) | reinterpret_cast<uintptr_t>(q)) % 16 == 0;
+}
+
 cudaError_t run_choose(int rows, int E, int k, int dtype, int score, int normalise, float factor, const void* logits, const float* bias,
                        int32_t* experts, float* weights, cudaStream_t stream) {
-  if (rows == 0) return cudaSuccess;
   return with_type(dtype, [&](auto type) {
     using T = decltype(type);
     return with_experts(E, [&](auto count) {
       constexpr int J = decltype(count)::value;
-      const auto kern = score == MOESCHED_SCORE_SOFTMAX ? choose_kernel<T, J, MOESCHED_SCORE_SOFTMAX> : choose_kernel<T, J, MOESCHED_SCORE_SIGMOID>;
-      return launch(kern, (rows + CHOOSE_WARPS - 1) / CHOOSE_WARPS, 32 * CHOOSE_WARPS, 0, stream, rows, E, k, normalise, factor,
-                    static_cast<const T*>(logits), bias, experts, weights);
+      const bool wide = wide_rows<T>(E, logits, nullptr);
+      const auto kern = score == MOESCHED_SCORE_SOFTMAX
+                            ? (wide ? choose_kernel<T, J, MOESCHED_SCORE_SOFTMAX, true> : choose_kernel<T, J, MOESCHED_SCORE_SOFTMAX, false>)
+                            : (wide ? choose_kernel<T, J, MOESCHED_SCORE_SIGMOID, true> : choose_kernel<T, J, MOESCHED_SCORE_SIGMOID, false>);
+      return launch(kern, dim3((rows + CHOOSE_WARPS - 1) / CHOOSE_WARPS), dim3(32 * CHOOSE_WARPS), 0, false, stream, rows, E, k, normalise,
+                    factor, static_cast<const T*>(logits), bias, experts, weights);
     });
   });
 }
 
 cudaError_t run_choose_backward(int rows, int E, int k, int dtype, int score, int normalise, float factor, const float* dweights,
                                 const void* logits, const int32_t* experts, void* dlogits, cudaStream_t stream) {
-  if (rows == 0) return cudaSuccess;
   return with_type(dtype, [&](auto type) {
     using T = decltype(type);
     return with_experts(E, [&](auto count) {
       constexpr int J = decltype(count)::value;
-      const auto kern = score == MOESCHED_SCORE_SOFTMAX ? choose_backward_kernel<T, J, MOESCHED_SCORE_SOFTMAX>
-                                                        : choose_backward_kernel<T, J, MOESCHED_SCORE_SIGMOID>;
-      return launch(kern, (rows + CHOOSE_WARPS - 1) / CHOOSE_WARPS, 32 * CHOOSE_WARPS, 0, stream, rows, E, k, normalise, factor, dweights,
-                    static_cast<const T*>(logits), experts, static_cast<T*>(dlogits));
+      const bool wide = wide_rows<T>(E, logits, dlogits);
+      const auto kern =
+          score == MOESCHED_SCORE_SOFTMAX
+              ? (wide ? choose_backward_kernel<T, J, MOESCHED_SCORE_SOFTMAX, true> : choose_backward_kernel<T, J, MOESCHED_SCORE_SOFTMAX, false>)
+              : (wide ? choose_backward_kernel<T, J, MOESCHED_SCORE_SIGMOID, true> : choose_backward_kernel<T, J, MOESCHED_SCORE_SIGMOID, false>);
+      return launch(kern, dim3((rows + CHOOSE_WARPS - 1) / CHOOSE_WARPS), dim3(32 * CHOOSE_WARPS), 0, false, stream, rows, E, k, normalise,
+                    factor, dweights, static_cast<const T*>(logits), experts, static_cast<T*>(dlogits));
     });
   });
 }

@@ -3,222 +3,396 @@
 //   h = x + r, rounded to the type: the residual stream as it is kept, so that the gradients are those of the values that were normed
 //   c = 1 / sqrt(sum h^2 / D + eps),  y = h c w
 //   q = y / scale in e4m3, scale = max |y| of a group of columns / 448, from y in 32 bits
-// A team of threads has a row in registers, from one read to the outputs: TEAM threads with V vectors of 16 bytes each. The
-// greatest of a group is found among the neighbouring lanes that hold it.
+// A team of warps has a row in registers, from one read to the outputs: V vectors of 16 bytes a thread. The greatest of a group is
+// found among the neighbouring lanes that hold it. Memory bounds all of it.
 #include <cuda_fp8.h>
 
 #include "token.cuh"
 
 namespace moesched {
 
-constexpr int NORM_THREADS = 1024;
+constexpr int NORM_THREADS = 512;                               // of a CTA
+// Rows on their way, as many as fit: a thread has 16 V bytes for each of `tensors`
+constexpr int NORM_PARTS_VECTORS = 2 * NORM_THREADS / 32 / 4;      // sums of warps, in front of them
+__host__ __device__ constexpr int norm_stages(int V, int tensors) { return V * tensors <= 6 ? 3 : 2; }
 
-// Sum over a team of whole warps, in a fixed order; `part` has a float for every warp of the CTA. Teams of one warp need no barrier.
-__device__ __forceinline__ float team_sum(float v, float* part, int team, int warps) {
+// Sum over a team of whole warps, in a fixed order. `part` has a float for every warp of the team, and is not written again before the team has
+// met once more. `meet` is the barrier, of the team or of all teams.
+template <typename Meet>
+__device__ __forceinline__ float team_sum(float v, float* part, int warps, int warp_of_team, Meet meet) {
   v = warp_sum(v);
   if (warps == 1) return v;
-  const int warp = threadIdx.x >> 5;
-  if ((threadIdx.x & 31) == 0) part[warp] = v;
-  __syncthreads();
+  if ((threadIdx.x & 31) == 0) part[warp_of_team] = v;
+  __syncwarp();
+  meet();
   v = 0.0f;
-  for (int w = 0; w < warps; ++w) v += part[team * warps + w];
+#pragma unroll 4
+  for (int w = 0; w < warps; ++w) v += part[w];
   return v;
 }
 
-template <typename T, int V, bool QUANT>
-__global__ void __launch_bounds__(NORM_THREADS) norm_kernel(int rows, int D, int team_warps, int group, float eps, const T* x,
-                                                            const T* residual, const T* __restrict__ weight, T* sum, T* y,
-                                                            uint8_t* q, float* scale, float* rstd) {
+struct NormArgs {
+  int rows, D, team_warps, group_shift, groups;                 // 2^group_shift vectors in each of the groups of a row
+  float eps;
+  const void *x, *residual, *weight;
+  void *sum, *y;
+  uint8_t* q;
+  float *scale, *rstd;
+};
+
+__device__ __forceinline__ float most_or_nan(float a, float b) {
+  float v;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(v) : "f"(a), "f"(fabsf(b)));
+  return v;
+}
+
+// Vector i of a row: h, of which y and q are made, and where they go. All lanes of a warp come here, those without a vector with zeros.
+template <typename T, bool QUANT>
+__device__ __forceinline__ void norm_out(const NormArgs& a, const uint4& h, const uint4& w, float c, bool in, size_t row, int i) {
   constexpr int COUNT = Vec<T>::COUNT;
+  Two x[COUNT / 2], u[COUNT / 2];
+  pairs_of<T>(h, x);
+  pairs_of<T>(w, u);
+  float f[COUNT];
+#pragma unroll
+  for (int e = 0; e < COUNT / 2; ++e) {
+    const float2 y = apart_of(mul2(mul2(x[e], two(c, c)), u[e]));
+    f[2 * e] = y.x;
+    f[2 * e + 1] = y.y;
+  }
+  const size_t at = row * a.D + (size_t)i * COUNT;
+  if (a.y != nullptr && in) *reinterpret_cast<uint4*>(static_cast<T*>(a.y) + at) = Vec<T>::pack(f);
+  if constexpr (QUANT) {
+    float most = fabsf(f[0]);                                   // a NaN stays
+#pragma unroll
+    for (int e = 1; e < COUNT; ++e) most = most_or_nan(most, f[e]);
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1)
+      if (o >> a.group_shift == 0) most = most_or_nan(most, __shfl_xor_sync(FULL, most, o));
+    // not below the smallest normal number, whose reciprocal is finite: groups of zeros, or of hardly more
+    const float s = most < 448.0f * 0x1p-126f ? 0x1p-126f : most * (1.0f / 448.0f), inverse = __fdividef(1.0f, s);
+    if (in) {
+      unsigned packed[COUNT / 4];
+#pragma unroll
+      for (int e = 0; e < COUNT; e += 4) {
+        const unsigned lo = __nv_cvt_float2_to_fp8x2(make_float2(f[e] * inverse, f[e + 1] * inverse), __NV_SATFINITE, __NV_E4M3);
+        const unsigned hi = __nv_cvt_float2_to_fp8x2(make_float2(f[e + 2] * inverse, f[e + 3] * inverse), __NV_SATFINITE, __NV_E4M3);
+        packed[e / 4] = lo | hi << 16;
+      }
+      if constexpr (COUNT == 8) *reinterpret_cast<uint2*>(a.q + at) = make_uint2(packed[0], packed[1]);
+      else *reinterpret_cast<unsigned*>(a.q + at) = packed[0];
+      if ((i & ((1 << a.group_shift) - 1)) == 0) a.scale[row * a.groups + (i >> a.group_shift)] = s;
+    }
+  }
+}
+
+// Vector of h, and what it adds to the sum of squares
+template <typename T>
+__device__ __forceinline__ uint4 norm_in(const uint4& x, const uint4& r, bool residual, float& total) {
+  constexpr int COUNT = Vec<T>::COUNT;
+  uint4 h = x;
+  float f[COUNT];
+  Vec<T>::unpack(x, f);
+  if (residual) {
+    float g[COUNT];
+    Vec<T>::unpack(r, g);
+#pragma unroll
+    for (int e = 0; e < COUNT; ++e) f[e] += g[e];
+    h = Vec<T>::pack(f);
+    Vec<T>::unpack(h, f);
+  }
+#pragma unroll
+  for (int e = 0; e < COUNT; ++e) total = fmaf(f[e], f[e], total);
+  return h;
+}
+
+template <typename T, int V, bool ADDED, bool QUANT>
+__global__ void __launch_bounds__(V == 4 ? NORM_THREADS : 256, V == 4 ? 2 : 4) norm_kernel(NormArgs a) {
   __shared__ float part[NORM_THREADS / 32];
-  const int vectors = D / COUNT, threads = 32 * team_warps;
-  const int team = threadIdx.x / threads, at = threadIdx.x % threads;
-  const long long row = (long long)blockIdx.x * (blockDim.x / threads) + team;
-  const bool active = row < rows;
-  const size_t first = (size_t)(active ? row : 0) * D;
-  uint4 h[V], w[V];
+  const int vectors = a.D / Vec<T>::COUNT, warps = a.team_warps, threads = 32 * warps;
+  const int team = threadIdx.x / threads, at = threadIdx.x - team * threads;
+  const long long mine = (long long)blockIdx.x * (blockDim.x / threads) + team;
+  const bool active = mine < a.rows;
+  const size_t row = active ? (size_t)mine : 0, first = row * vectors;
+  const uint4 *x = static_cast<const uint4*>(a.x) + first, *residual = static_cast<const uint4*>(a.residual) + first, zero = make_uint4(0u, 0u, 0u, 0u);
+  uint4 h[V], r[V], w[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    const int i = at + v * threads;
+    const bool in = active && i < vectors;
+    h[v] = in ? load_once(x + i) : zero;
+    r[v] = ADDED && in ? load_once(residual + i) : zero;
+  }
   float total = 0.0f;
 #pragma unroll
   for (int v = 0; v < V; ++v) {
     const int i = at + v * threads;
-    const bool in = active && i < vectors;
-    h[v] = in ? load_once(x + first + (size_t)i * COUNT) : make_uint4(0u, 0u, 0u, 0u);
-    if (residual != nullptr) w[v] = in ? load_once(residual + first + (size_t)i * COUNT) : make_uint4(0u, 0u, 0u, 0u);
+    h[v] = norm_in<T>(h[v], r[v], ADDED, total);
+    if (ADDED && active && i < vectors) static_cast<uint4*>(a.sum)[first + i] = h[v];
+    w[v] = i < vectors ? __ldg(static_cast<const uint4*>(a.weight) + i) : zero;
   }
+  total = team_sum(total, part + team * warps, warps, at >> 5, [] { __syncthreads(); });
+  const float c = rsqrtf(total / (float)a.D + a.eps);
+  if (a.rstd != nullptr && active && at == 0) a.rstd[row] = c;
 #pragma unroll
   for (int v = 0; v < V; ++v) {
     const int i = at + v * threads;
-    float f[COUNT];
-    Vec<T>::unpack(h[v], f);
-    if (residual != nullptr) {
-      float r[COUNT];
-      Vec<T>::unpack(w[v], r);
-#pragma unroll
-      for (int e = 0; e < COUNT; ++e) f[e] += r[e];
-      h[v] = Vec<T>::pack(f);
-      Vec<T>::unpack(h[v], f);
-      if (active && i < vectors) *reinterpret_cast<uint4*>(sum + first + (size_t)i * COUNT) = h[v];
-    }
-#pragma unroll
-    for (int e = 0; e < COUNT; ++e) total = fmaf(f[e], f[e], total);
-  }
-#pragma unroll
-  for (int v = 0; v < V; ++v) {
-    const int i = at + v * threads;
-    w[v] = i < vectors ? __ldg(reinterpret_cast<const uint4*>(weight) + i) : make_uint4(0u, 0u, 0u, 0u);
-  }
-  total = team_sum(total, part, team, team_warps);
-  const float c = rsqrtf(total / (float)D + eps);
-  if (rstd != nullptr && active && at == 0) rstd[row] = c;
-#pragma unroll
-  for (int v = 0; v < V; ++v) {
-    const int i = at + v * threads;
-    const bool in = active && i < vectors;
-    float f[COUNT], g[COUNT];
-    Vec<T>::unpack(h[v], f);
-    Vec<T>::unpack(w[v], g);
-#pragma unroll
-    for (int e = 0; e < COUNT; ++e) f[e] = f[e] * c * g[e];
-    if (y != nullptr && in) *reinterpret_cast<uint4*>(y + first + (size_t)i * COUNT) = Vec<T>::pack(f);
-    if constexpr (QUANT) {
-      unsigned most = 0u;                                       // (of the magnitudes' bits: a NaN is above infinity, and stays)
-#pragma unroll
-      for (int e = 0; e < COUNT; ++e) most = max(most, __float_as_uint(f[e]) & 0x7fffffffu);
-      for (int o = group / COUNT / 2; o > 0; o >>= 1) most = max(most, __shfl_xor_sync(FULL, most, o));
-      // not below the smallest normal number, whose reciprocal is finite: groups of zeros, or of hardly more
-      const float top = __uint_as_float(most), s = top < 448.0f * 0x1p-126f ? 0x1p-126f : top / 448.0f, inverse = 1.0f / s;
-      if (in) {
-        unsigned packed[COUNT / 4];
-#pragma unroll
-        for (int e = 0; e < COUNT; e += 4) {
-          const unsigned lo = __nv_cvt_float2_to_fp8x2(make_float2(f[e] * inverse, f[e + 1] * inverse), __NV_SATFINITE, __NV_E4M3);
-          const unsigned hi = __nv_cvt_float2_to_fp8x2(make_float2(f[e + 2] * inverse, f[e + 3] * inverse), __NV_SATFINITE, __NV_E4M3);
-          packed[e / 4] = lo | hi << 16;
-        }
-        uint8_t* to = q + first + (size_t)i * COUNT;
-        if constexpr (COUNT == 8) *reinterpret_cast<uint2*>(to) = make_uint2(packed[0], packed[1]);
-        else *reinterpret_cast<unsigned*>(to) = packed[0];
-        const int per = group / COUNT;
-        if (i % per == 0) scale[(size_t)row * ((D + group - 1) / group) + i / per] = s;
-      }
-    }
+    norm_out<T, QUANT>(a, h[v], w[v], c, active && i < vectors, row, i);
   }
 }
 
-template <typename T, int V>
-static cudaError_t launch_norm(int rows, int D, int group, float eps, const void* x, const void* residual, const void* weight,
-                               void* sum, void* y, uint8_t* q, float* scale, float* rstd, cudaStream_t stream) {
-  const int vectors = D / Vec<T>::COUNT, warps = (vectors + 32 * V - 1) / (32 * V), teams = warps >= 8 ? 1 : 8 / warps;
-  const auto kern = q != nullptr ? norm_kernel<T, V, true> : norm_kernel<T, V, false>;
-  return launch(kern, (rows + teams - 1) / teams, 32 * warps * teams, 0, stream, rows, D, warps, group, eps, static_cast<const T*>(x),
-                static_cast<const T*>(residual), static_cast<const T*>(weight), static_cast<T*>(sum), static_cast<T*>(y), q, scale, rstd);
+// Few rows, a row a CTA of as many threads as there are vectors: nothing but latency
+template <typename T, bool ADDED, bool QUANT>
+__global__ void __launch_bounds__(1024) norm_few_kernel(NormArgs a) {
+  __shared__ float part[32];
+  const int vectors = a.D / Vec<T>::COUNT, i = threadIdx.x;
+  const size_t row = blockIdx.x, at = row * vectors + i;
+  const bool in = i < vectors;
+  const uint4 zero = make_uint4(0u, 0u, 0u, 0u), x = in ? load_once(static_cast<const uint4*>(a.x) + at) : zero,
+              r = in && ADDED ? load_once(static_cast<const uint4*>(a.residual) + at) : zero,
+              w = in ? __ldg(static_cast<const uint4*>(a.weight) + i) : zero;
+  float total = 0.0f;
+  const uint4 h = norm_in<T>(x, r, ADDED, total);
+  if (ADDED && in) static_cast<uint4*>(a.sum)[at] = h;
+  total = team_sum(total, part, blockDim.x >> 5, i >> 5, [] { __syncthreads(); });
+  const float c = rsqrtf(total / (float)a.D + a.eps);
+  if (a.rstd != nullptr && i == 0) a.rstd[row] = c;
+  norm_out<T, QUANT>(a, h, w, c, in, row, i);
+}
+
+// Rows that are longer than 512 threads hold: one a CTA, read twice, the second time from the L2
+template <typename T, bool QUANT>
+__global__ void __launch_bounds__(NORM_THREADS) norm_wide_kernel(NormArgs a) {
+  constexpr int COUNT = Vec<T>::COUNT;
+  __shared__ float part[32];
+  const int vectors = a.D / COUNT;
+  const size_t row = blockIdx.x;
+  const T *x = static_cast<const T*>(a.x) + row * a.D, *residual = static_cast<const T*>(a.residual) + row * a.D;
+  T* sum = static_cast<T*>(a.sum) + row * a.D;
+  const bool added = a.residual != nullptr;
+  const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+  float total = 0.0f;
+  for (int i = threadIdx.x; i < vectors; i += NORM_THREADS) {
+    const uint4 h = norm_in<T>(load_once(x + (size_t)i * COUNT), added ? load_once(residual + (size_t)i * COUNT) : zero, added, total);
+    if (added) *reinterpret_cast<uint4*>(sum + (size_t)i * COUNT) = h;
+  }
+  total = team_sum(total, part, NORM_THREADS / 32, threadIdx.x >> 5, [] { __syncthreads(); });
+  const float c = rsqrtf(total / (float)a.D + a.eps);
+  if (a.rstd != nullptr && threadIdx.x == 0) a.rstd[row] = c;
+  const T* h = added ? sum : x;                                 // (its own stores of before)
+  for (int base = 0; base < vectors; base += NORM_THREADS) {
+    const int i = base + threadIdx.x;
+    const bool in = i < vectors;
+    norm_out<T, QUANT>(a, in ? load_once(h + (size_t)i * COUNT) : zero, in ? __ldg(static_cast<const uint4*>(a.weight) + i) : zero, c, in, row, i);
+  }
+}
+
+template <typename T, int V, bool ADDED, bool QUANT>
+static cudaError_t launch_norm_rows(NormArgs a, cudaStream_t stream) {
+  const int vectors = a.D / Vec<T>::COUNT;
+  a.team_warps = (vectors + 32 * V - 1) / (32 * V);
+  const int teams = a.team_warps >= 8 ? 1 : 8 / a.team_warps;
+  return launch(norm_kernel<T, V, ADDED, QUANT>, dim3((unsigned)((a.rows + teams - 1) / teams)), dim3(32 * a.team_warps * teams), 0, false, stream, a);
+}
+
+template <typename T, bool ADDED, bool QUANT>
+static cudaError_t launch_norm(const NormArgs& a, cudaStream_t stream) {
+  const int vectors = a.D / Vec<T>::COUNT;
+  if (a.rows <= sm_count() && vectors <= 1024)
+    return launch(norm_few_kernel<T, ADDED, QUANT>, dim3(a.rows), dim3((vectors + 31) / 32 * 32), 0, false, stream, a);
+  if (vectors <= 32) return launch_norm_rows<T, 1, ADDED, QUANT>(a, stream);
+  if (vectors <= 64) return launch_norm_rows<T, 2, ADDED, QUANT>(a, stream);
+  if (vectors <= 4 * NORM_THREADS) return launch_norm_rows<T, 4, ADDED, QUANT>(a, stream);
+  return launch(norm_wide_kernel<T, QUANT>, dim3(a.rows), dim3(NORM_THREADS), 0, false, stream, a);
 }
 
 cudaError_t run_norm(int rows, int D, int dtype, float eps, int group, const void* x, const void* residual, const void* weight,
                      void* sum, void* y, uint8_t* q, float* scale, float* rstd, cudaStream_t stream) {
-  if (rows == 0) return cudaSuccess;
+  NormArgs a{rows, D, 0, 0, q != nullptr ? (D + group - 1) / group : 0, eps, x, residual, weight, sum, y, q, scale, rstd};
   return with_type(dtype, [&](auto type) {
     using T = decltype(type);
-    const int vectors = D / Vec<T>::COUNT;
-    if (vectors <= 4 * NORM_THREADS) return launch_norm<T, 4>(rows, D, group, eps, x, residual, weight, sum, y, q, scale, rstd, stream);
-    return launch_norm<T, 16>(rows, D, group, eps, x, residual, weight, sum, y, q, scale, rstd, stream);
+    while (Vec<T>::COUNT << a.group_shift < group) ++a.group_shift;
+    if (residual != nullptr) return q != nullptr ? launch_norm<T, true, true>(a, stream) : launch_norm<T, true, false>(a, stream);
+    return q != nullptr ? launch_norm<T, false, true>(a, stream) : launch_norm<T, false, false>(a, stream);
   });
 }
 
 // Gradients, from g = dy w:  dx = c (g - h c^2 sum(g h) / D) + what comes in for h,  dw = sum over the rows of dy h c.
-// A CTA takes every gridDim-th set of rows and keeps its threads' columns of dw in registers; a second kernel adds the CTAs' up, in
-// their order.
-template <typename T, int V>
-__global__ void __launch_bounds__(NORM_THREADS) norm_backward_kernel(int rows, int D, int team_warps, const T* dy, const T* h,
-                                                                     const T* __restrict__ weight, const float* __restrict__ rstd,
-                                                                     const T* dsum, T* dx, float* __restrict__ partial) {
-  constexpr int COUNT = Vec<T>::COUNT;
-  extern __shared__ __align__(16) float joined[];               // [D], where teams share the CTA
-  __shared__ float part[2][NORM_THREADS / 32];
-  const int vectors = D / COUNT, threads = 32 * team_warps, teams = blockDim.x / threads;
-  const int team = threadIdx.x / threads, at = threadIdx.x % threads;
-  float dw[V][COUNT];
-#pragma unroll
-  for (int v = 0; v < V; ++v)
-#pragma unroll
-    for (int e = 0; e < COUNT; ++e) dw[v][e] = 0.0f;
-  int set = 0;
-  for (long long base = (long long)blockIdx.x * teams; base < rows; base += (long long)gridDim.x * teams, set ^= 1) {
-    const long long row = base + team;
-    const bool active = row < rows;
-    const size_t first = (size_t)(active ? row : 0) * D;
-    const float c = active ? rstd[row] : 0.0f;
-    uint4 a[V], b[V];
-    float total = 0.0f;
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const int i = at + v * threads;
-      const bool in = active && i < vectors;
-      a[v] = in ? load_once(dy + first + (size_t)i * COUNT) : make_uint4(0u, 0u, 0u, 0u);
-      b[v] = in ? load_once(h + first + (size_t)i * COUNT) : make_uint4(0u, 0u, 0u, 0u);
-    }
+// A team takes every so many rows, each thread the same columns of all of them, whose dw it has in registers. A second kernel adds the dw of the CTAs up, in their order. Rows that are too long for one CTA's registers (SPLIT) have their sums made
+// by a kernel of its own, and a CTA has a block of columns.
+
+struct NormBackwardArgs {
+  int rows, D, team_warps;
+  const void *dy, *h, *weight;
+  const float* rstd;
+  const void* dsum;
+  void* dx;
+  float *partial, *dot;
+};
+
+template <typename T, int V, bool SPLIT>
+__global__ void __launch_bounds__(NORM_THREADS) norm_backward_kernel(NormBackwardArgs a) {
+  constexpr int COUNT = Vec<T>::COUNT, PAIRS = COUNT / 2;
+  constexpr int STAGES = norm_stages(V, 3);
+  constexpr bool KEEP = V * COUNT <= 16;                        // values of 32 bits stay in registers, or are made again of those of the type
+  extern __shared__ __align__(16) uint4 shared[];
+  float(*part)[NORM_THREADS / 32] = reinterpret_cast<float(*)[NORM_THREADS / 32]>(shared);      // [2]
+  uint4* ring = shared + NORM_PARTS_VECTORS;                    // [stage][dy, h, dsum][V][threads of the CTA]
+  const int vectors = a.D / COUNT, warps = a.team_warps, threads = 32 * warps, teams = blockDim.x / threads;
+  const int team = threadIdx.x / threads, at = threadIdx.x - team * threads, first = SPLIT ? blockIdx.y * V * threads : 0;
+  const int tensors = a.dsum != nullptr ? 3 : 2, stage_vectors = tensors * V * blockDim.x, step = gridDim.x * teams;
+  const uint4* const from[3] = {static_cast<const uint4*>(a.dy), static_cast<const uint4*>(a.h), static_cast<const uint4*>(a.dsum)};
+  const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+  const auto place = [&](int stage, int tensor, int v) { return ring + stage * stage_vectors + (tensor * V + v) * blockDim.x + threadIdx.x; };
+  const auto ask = [&](int row, int stage, int t) {
+    if (row >= a.rows) return;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const int i = at + v * threads;
-      float g[COUNT], x[COUNT], w[COUNT];
-      Vec<T>::unpack(a[v], g);
-      Vec<T>::unpack(b[v], x);
-      Vec<T>::unpack(i < vectors ? __ldg(reinterpret_cast<const uint4*>(weight) + i) : make_uint4(0u, 0u, 0u, 0u), w);
-#pragma unroll
-      for (int e = 0; e < COUNT; ++e) {
-        total = fmaf(g[e] * w[e], x[e], total);
-        dw[v][e] = fmaf(g[e] * c, x[e], dw[v][e]);
-      }
+      const int i = first + at + v * threads;
+      if (i < vectors) copy_behind(place(stage, t, v), from[t] + (size_t)row * vectors + i);
     }
-    total = team_sum(total, part[set], team, team_warps);        // (two sets: the next sum may begin while this one is read)
-    const float along = total / (float)D * c * c;
+  };
+  uint4 weight[V];
+  Two w[KEEP ? V : 1][PAIRS], dw[V][PAIRS];
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const int i = at + v * threads;
-      if (!active || i >= vectors) continue;
-      float g[COUNT], x[COUNT], w[COUNT], s[COUNT];
-      Vec<T>::unpack(a[v], g);
-      Vec<T>::unpack(b[v], x);
-      Vec<T>::unpack(__ldg(reinterpret_cast<const uint4*>(weight) + i), w);
-      if (dsum != nullptr) Vec<T>::unpack(load_once(dsum + first + (size_t)i * COUNT), s);
+  for (int v = 0; v < V; ++v) {
+    const int i = first + at + v * threads;
+    weight[v] = i < vectors ? __ldg(static_cast<const uint4*>(a.weight) + i) : zero;
+    if constexpr (KEEP) pairs_of<T>(weight[v], w[v]);
 #pragma unroll
-      for (int e = 0; e < COUNT; ++e) {
-        g[e] = c * fmaf(-along, x[e], g[e] * w[e]);
-        if (dsum != nullptr) g[e] += s[e];
-      }
-      *reinterpret_cast<uint4*>(dx + first + (size_t)i * COUNT) = Vec<T>::pack(g);
-    }
+    for (int e = 0; e < PAIRS; ++e) dw[v][e] = two(0.0f, 0.0f);
   }
-  // the teams' columns one after the other
+  int row = blockIdx.x * teams + team;
+#pragma unroll
+  for (int s = 0; s < STAGES; ++s) {
+    for (int t = 0; t < tensors; ++t) ask(row + s * step, s, t);
+    copies_asked();
+  }
+  float next_c = row < a.rows ? a.rstd[row] : 0.0f;
+  for (int stage = 0, turn = 0; row < a.rows; row += step, turn ^= 1, stage = stage + 1 == STAGES ? 0 : stage + 1) {
+    const float c = next_c;
+    if (row + step < a.rows) next_c = a.rstd[row + step];
+    copies_here<STAGES - 1>();
+    uint4 g4[V], h4[V];
+    Two gw[KEEP ? V : 1][PAIRS], x[KEEP ? V : 1][PAIRS], sum = two(0.0f, 0.0f);
+    const Two cc = two(c, c);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const int k = KEEP ? v : 0;
+      const bool in = first + at + v * threads < vectors;
+      g4[v] = in ? *place(stage, 0, v) : zero;
+      h4[v] = in ? *place(stage, 1, v) : zero;
+      if constexpr (!KEEP) pairs_of<T>(weight[v], w[k]);
+      Two g[PAIRS];
+      pairs_of<T>(g4[v], g);
+      pairs_of<T>(h4[v], x[k]);
+#pragma unroll
+      for (int e = 0; e < PAIRS; ++e) {
+        gw[k][e] = mul2(g[e], w[k][e]);
+        if constexpr (!SPLIT) sum = fma2(gw[k][e], x[k][e], sum);
+        dw[v][e] = fma2(mul2(g[e], cc), x[k][e], dw[v][e]);
+      }
+    }
+    ask(row + STAGES * step, stage, 0);
+    ask(row + STAGES * step, stage, 1);
+    // (two sets of parts in turn: a team that has met for one sum may begin the next while some of it still read)
+    float total;
+    if constexpr (SPLIT) {
+      total = a.dot[row];
+    } else {
+      const float2 halves = apart_of(sum);
+      total = team_sum(halves.x + halves.y, part[turn] + team * warps, warps, at >> 5,
+                       [&] { asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(threads) : "memory"); });
+    }
+    const float along = -total / (float)a.D * c * c;
+    const Two against = two(along, along);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const int k = KEEP ? v : 0, i = first + at + v * threads;
+      if (i >= vectors) continue;
+      if constexpr (!KEEP) {
+        Two g[PAIRS];
+        pairs_of<T>(g4[v], g);
+        pairs_of<T>(h4[v], x[k]);
+        pairs_of<T>(weight[v], w[k]);
+#pragma unroll
+        for (int e = 0; e < PAIRS; ++e) gw[k][e] = mul2(g[e], w[k][e]);
+      }
+      Two s[PAIRS];
+      pairs_of<T>(tensors == 3 ? *place(stage, 2, v) : zero, s);
+      float f[COUNT];
+#pragma unroll
+      for (int e = 0; e < PAIRS; ++e) {
+        const float2 d = apart_of(fma2(cc, fma2(against, x[k][e], gw[k][e]), s[e]));
+        f[2 * e] = d.x;
+        f[2 * e + 1] = d.y;
+      }
+      static_cast<uint4*>(a.dx)[(size_t)row * vectors + i] = Vec<T>::pack(f);
+    }
+    if (tensors == 3) ask(row + STAGES * step, stage, 2);
+    copies_asked();
+  }
+  copies_here<0>();
+  let_next_start();
+  // the teams' columns one after the other, in the ring's memory
+  float* joined = reinterpret_cast<float*>(ring);
   for (int t = 0; t < teams; ++t) {
-    if (team == t) {
+    __syncthreads();
+    if (team != t) continue;
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        const int i = at + v * threads;
-        if (i >= vectors) continue;
+    for (int v = 0; v < V; ++v) {
+      const int i = at + v * threads;
+      if (first + i >= vectors) continue;
+      float4* mine = reinterpret_cast<float4*>(joined + i * COUNT);
+      float4* out = reinterpret_cast<float4*>(a.partial + (size_t)blockIdx.x * a.D + (size_t)(first + i) * COUNT);
 #pragma unroll
-        for (int e = 0; e < COUNT; ++e) {
-          float* mine = joined + i * COUNT + e;
-          const float value = t == 0 ? dw[v][e] : *mine + dw[v][e];
-          if (t + 1 == teams) partial[(size_t)blockIdx.x * D + i * COUNT + e] = value;
-          else *mine = value;
+      for (int e = 0; e < COUNT / 4; ++e) {
+        const float2 lo = apart_of(dw[v][2 * e]), hi = apart_of(dw[v][2 * e + 1]);
+        float4 value = make_float4(lo.x, lo.y, hi.x, hi.y);
+        if (t > 0) {
+          const float4 before = mine[e];
+          value = make_float4(before.x + value.x, before.y + value.y, before.z + value.z, before.w + value.w);
         }
+        if (t + 1 == teams) out[e] = value;
+        else mine[e] = value;
       }
     }
-    if (teams > 1) __syncthreads();
   }
+}
+
+// sum(g h) of a row a CTA
+template <typename T>
+__global__ void __launch_bounds__(NORM_THREADS) norm_dot_kernel(int vectors, const uint4* dy, const uint4* h, const uint4* __restrict__ weight,
+                                                                float* __restrict__ dot) {
+  constexpr int COUNT = Vec<T>::COUNT;
+  __shared__ float part[NORM_THREADS / 32];
+  const size_t row = blockIdx.x;
+  float total = 0.0f;
+  for (int i = threadIdx.x; i < vectors; i += NORM_THREADS) {
+    float g[COUNT], x[COUNT], w[COUNT];
+    Vec<T>::unpack(load_once(dy + row * vectors + i), g);
+    Vec<T>::unpack(load_once(h + row * vectors + i), x);
+    Vec<T>::unpack(__ldg(weight + i), w);
+#pragma unroll
+    for (int e = 0; e < COUNT; ++e) total = fmaf(g[e] * w[e], x[e], total);
+  }
+  total = team_sum(total, part, NORM_THREADS / 32, threadIdx.x >> 5, [] { __syncthreads(); });
+  if (threadIdx.x == 0) dot[row] = total;
 }
 
 constexpr int COLUMN_ROWS = 16;
 
 // out[d] = sum of partial[.][d] in a fixed order: 32 columns and 16 stretches of the CTAs' sums a CTA
 template <typename T>
-__global__ void __launch_bounds__(32 * COLUMN_ROWS) column_sum_kernel(int parts, int D, const float* __restrict__ partial, T* out) {
+__global__ void __launch_bounds__(32 * COLUMN_ROWS) column_sum_kernel(int parts, int D, const float* partial, T* out) {
   __shared__ float sums[COLUMN_ROWS][32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, d = 32 * blockIdx.x + lane;
+  wait_for_previous();
   float total = 0.0f;
-  if (d < D)
+  if (d < D) {
+#pragma unroll 4
     for (int p = warp; p < parts; p += COLUMN_ROWS) total += partial[(size_t)p * D + d];
+  }
   sums[warp][lane] = total;
   __syncthreads();
   if (warp == 0 && d < D) {
@@ -227,32 +401,49 @@ __global__ void __launch_bounds__(32 * COLUMN_ROWS) column_sum_kernel(int parts,
   }
 }
 
-static int norm_parts(int rows) { return rows < 2 * 148 ? rows : 2 * 148; }   // CTAs that sum up dw, whatever the GPU has
-size_t norm_scratch_bytes(int rows, int D) { return (size_t)norm_parts(rows) * D * sizeof(float); }
+constexpr int NORM_PARTS = 148;                                 // CTAs that sum up dw, at most, whatever the GPU has
+static int norm_parts(int rows) { return rows < NORM_PARTS ? rows : NORM_PARTS; }
+size_t norm_scratch_bytes(int rows, int D) {
+  return ((size_t)norm_parts(rows) * D + (D > 16 * NORM_THREADS ? rows : 0)) * sizeof(float);
+}
 
-template <typename T, int V>
-static cudaError_t launch_norm_backward(int rows, int D, const void* dy, const void* h, const void* weight, const float* rstd,
-                                        const void* dsum, void* dx, float* partial, cudaStream_t stream) {
-  const int vectors = D / Vec<T>::COUNT, warps = (vectors + 32 * V - 1) / (32 * V), teams = warps >= 8 ? 1 : 8 / warps;
-  const auto kern = norm_backward_kernel<T, V>;
-  const size_t smem = teams > 1 ? (size_t)D * sizeof(float) : 0;
-  return launch(kern, norm_parts(rows), 32 * warps * teams, smem, stream, rows, D, warps, static_cast<const T*>(dy),
-                static_cast<const T*>(h), static_cast<const T*>(weight), rstd, static_cast<const T*>(dsum), static_cast<T*>(dx), partial);
+template <typename T, int V, bool SPLIT>
+static cudaError_t launch_norm_backward_rows(NormBackwardArgs a, int& parts, cudaStream_t stream) {
+  const int vectors = a.D / Vec<T>::COUNT, tensors = a.dsum != nullptr ? 3 : 2, blocks = SPLIT ? (vectors + V * NORM_THREADS - 1) / (V * NORM_THREADS) : 1;
+  a.team_warps = SPLIT ? NORM_THREADS / 32 : (vectors + 32 * V - 1) / (32 * V);
+  // as many rows at a time as 512 threads take, but not more than leave every SM one
+  int teams = NORM_THREADS / 32 / a.team_warps;
+  while (teams > 1 && (long long)(teams - 1) * NORM_PARTS >= a.rows) --teams;
+  parts = norm_parts((a.rows + teams - 1) / teams);
+  const size_t vectors_of_ring = (size_t)norm_stages(V, 3) * tensors * V * 32 * a.team_warps * teams;
+  return launch(norm_backward_kernel<T, V, SPLIT>, dim3(parts, blocks), dim3(32 * a.team_warps * teams), 16 * (NORM_PARTS_VECTORS + vectors_of_ring),
+                false, stream, a);
+}
+
+// 16 values of a row a thread where that is enough, twice as many where they are of 16 bits, half of them where the row is short
+template <typename T>
+static cudaError_t launch_norm_backward(const NormBackwardArgs& a, int& parts, cudaStream_t stream) {
+  constexpr int V = 16 / Vec<T>::COUNT;
+  const int vectors = a.D / Vec<T>::COUNT;
+  if (vectors <= 16 * V) return launch_norm_backward_rows<T, V / 2, false>(a, parts, stream);
+  if (vectors <= V * NORM_THREADS) return launch_norm_backward_rows<T, V, false>(a, parts, stream);
+  if (vectors <= 4 * NORM_THREADS) return launch_norm_backward_rows<T, 4, false>(a, parts, stream);
+  const cudaError_t e = launch(norm_dot_kernel<T>, dim3(a.rows), dim3(NORM_THREADS), 0, false, stream, vectors, static_cast<const uint4*>(a.dy),
+                               static_cast<const uint4*>(a.h), static_cast<const uint4*>(a.weight), a.dot);
+  return e != cudaSuccess ? e : launch_norm_backward_rows<T, V, true>(a, parts, stream);
 }
 
 cudaError_t run_norm_backward(int rows, int D, int dtype, const void* dy, const void* h, const void* weight, const float* rstd,
                               const void* dsum, void* dx, void* dweight, float* scratch, cudaStream_t stream) {
   return with_type(dtype, [&](auto type) {
     using T = decltype(type);
+    int parts = 0;
     if (rows > 0) {
-      const int vectors = D / Vec<T>::COUNT;
-      const cudaError_t e =
-          vectors <= 2 * NORM_THREADS ? launch_norm_backward<T, 2>(rows, D, dy, h, weight, rstd, dsum, dx, scratch, stream)
-                                      : launch_norm_backward<T, 16>(rows, D, dy, h, weight, rstd, dsum, dx, scratch, stream);
-      if (e != cudaSuccess) return e;
+      const NormBackwardArgs a{rows, D, 0, dy, h, weight, rstd, dsum, dx, scratch, scratch + (size_t)norm_parts(rows) * D};
+      if (cudaError_t e = launch_norm_backward<T>(a, parts, stream); e != cudaSuccess) return e;
     }
-    return launch(column_sum_kernel<T>, (D + 31) / 32, 32 * COLUMN_ROWS, 0, stream, norm_parts(rows), D, static_cast<const float*>(scratch),
-                  static_cast<T*>(dweight));
+    return launch(column_sum_kernel<T>, dim3((unsigned)((D + 31) / 32)), dim3(32 * COLUMN_ROWS), 0, true, stream, parts, D,
+                  static_cast<const float*>(scratch), static_cast<T*>(dweight));
   });
 }
 

@@ -49,7 +49,7 @@ def test_rms_norm_backward_checks_its_arguments(lib):
     for n in names:
         assert n == "dsum" or call(**{n: None}) == -1, n
         assert call(**{n: A[0] + (2 if n == "rstd" else 8)}) == -1, n
-    assert ms.norm_scratch_bytes(10, 64) == 10 * 64 * 4 and ms.norm_scratch_bytes(1 << 20, 4096) == 296 * 4096 * 4
+    assert ms.norm_scratch_bytes(10, 64) == 10 * 64 * 4 and ms.norm_scratch_bytes(1 << 20, 4096) == 148 * 4096 * 4 and ms.norm_scratch_bytes(1000, 16384) == (148 * 16384 + 1000) * 4
     assert ms.norm_scratch_bytes(-1, 64) == ms.norm_scratch_bytes(10, 60) == ms.norm_scratch_bytes((1 << 30) + 1, 64) == ms.norm_scratch_bytes((1 << 32) + 1, 64) == 0
 
 
