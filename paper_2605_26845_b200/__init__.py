@@ -99,9 +99,9 @@ def load_library():
 def use_library(path=None):
     """Route every call of this binding through another build of the library, e.g. the checked one
     (libmoesched_checked.so, see build.py); None goes back to the regular library. Returns the path."""
-    global _lib
+    global _lib, _bound
     path = LIB_PATH if path is None else path
-    _lib = _open(path)
+    _lib, _bound = _open(path), None
     return path
 
 
@@ -714,46 +714,27 @@ def expert_matvec4(x, weight, scale, offsets, weight_up=None, scale_up=None, act
     return out
 
 
-_TOKEN_TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
-_SCORES = {"softmax": 0, "sigmoid": 1}
 MAX_TOP_K = 32
 
+_bound = None                    # the compiled part of this binding, with the functions of the library that is loaded
 
-def _token_type(x, what="x"):
-    """Number of x's type, and its width; x [..., D] is checked."""
-    dtype = _TOKEN_TYPES.get(getattr(x, "dtype", None))
-    if dtype is None:
-        raise MoeschedError(f"{what} must be bfloat16, float16 or float32")
-    _dev(x, x.dtype, what)
-    if x.dim() < 2 or not 8 <= x.shape[-1] <= _MAX_WIDTH or x.shape[-1] % 8 != 0:
-        raise MoeschedError(f"{what} must be [..., D], D a multiple of 8 and {_MAX_WIDTH} at most")
-    return dtype, x.shape[-1]
+_BOUND = ("rms_norm", "rms_norm_backward", "route_choose", "route_choose_backward", "tokens_to_rows", "rows_to_tokens", "rows_to_tokens_backward",
+          "rows_widen", "norm_scratch_bytes", "strerror", "last_cuda_error")
 
 
-def _rows_of(x):
-    rows = x.numel() // x.shape[-1]
-    if rows > _MAX_ROWS:
-        raise MoeschedError("at most 2^30 rows")
-    return rows
-
-
-def _shaped(t, dtype, shape, device, what, make=True):
-    """`t`, checked, or a new tensor of that type and shape."""
-    if t is None and make:
-        if len(shape) == 2:
-            return _allocator(device)((shape[0], shape[1]), (shape[1], 1), dtype)
-        if len(shape) == 1:
-            return _allocator(device)((shape[0],), (1,), dtype)
-        return torch.empty(shape, dtype=dtype, device=device)
-    if _dev(t, dtype, what).shape != shape or t.device != device:
-        raise MoeschedError(f"{what} must have shape {tuple(shape)}, on the device of the others")
-    return t
-
-
-def _group(group):
-    if group not in (32, 64, 128):
-        raise MoeschedError("group must be 32, 64 or 128")
-    return int(group)
+def _bind():
+    """The calls on tokens take two or three microseconds on the GPU, and through ctypes 9 to 15 on the host: their arguments are checked and their outputs made
+    in csrc/binding.cpp, 5 to 8."""
+    global _bound
+    lib = load_library()
+    try:
+        from . import _binding
+    except ImportError as e:
+        raise MoeschedError(f"{os.path.join(_HERE, '_binding.so')} cannot be loaded ({e}): run `python -m paper_2605_26845_b200.build` "
+                            "(there is no CPU fallback)") from e
+    _binding.bind(MoeschedError, torch.OutOfMemoryError, {f"moesched_{n}": ctypes.cast(getattr(lib, f"moesched_{n}"), ctypes.c_void_p).value for n in _BOUND})
+    _bound = _binding
+    return _binding
 
 
 def rms_norm(x, weight, eps=1e-6, residual=None, group=None, want_y=True, save=False, out=None) -> dict:
@@ -762,40 +743,8 @@ def rms_norm(x, weight, eps=1e-6, residual=None, group=None, want_y=True, save=F
     with group (32, 64 or 128) 'q' [..., D] float8_e4m3fn and 'scale' [..., ceil(D / group)] float32, y = q * scale in 8 bits with a
     scale for every group of columns, rounded from y in 32 bits (y itself is left out with want_y=False); with save=True 'rstd' [...]
     float32 for rms_norm_backward. `out` may hand back the dict of an earlier call of the same shape for reuse; its 'sum' may be x or the
-    residual itself. Not recorded by autograd, like expert_ffn."""
-    _no_graph("rms_norm", x, weight, residual, backward="rms_norm_backward")
-    dtype, D = _token_type(x)
-    shape, kind, dev = x.shape, x.dtype, x.device
-    rows = _rows_of(x)
-    _shaped(weight, kind, (D,), dev, "weight", make=False)
-    if not 0.0 <= eps < 3e38:
-        raise MoeschedError("eps must be a number of at least 0")
-    if not want_y and group is None:
-        raise MoeschedError("y can only be left out where there is an output in 8 bits")
-    have = {} if out is None else out
-    res = {}
-    if want_y:
-        res["y"] = y = _shaped(have.get("y"), kind, shape, dev, "out['y']")
-    else:
-        y = None
-    if residual is not None:
-        _shaped(residual, kind, shape, dev, "residual", make=False)
-        res["sum"] = total = _shaped(have.get("sum"), kind, shape, dev, "out['sum']")
-    else:
-        total = None
-    if group is not None:
-        group = _group(group)
-        res["q"] = q = _shaped(have.get("q"), torch.float8_e4m3fn, shape, dev, "out['q']")
-        res["scale"] = scale = _shaped(have.get("scale"), torch.float32, shape[:-1] + (-(-D // group),), dev, "out['scale']")
-    else:
-        q = scale = None
-    if save:
-        res["rstd"] = rstd = _shaped(have.get("rstd"), torch.float32, shape[:-1], dev, "out['rstd']")
-    else:
-        rstd = None
-    _call("moesched_rms_norm", dev, rows, D, dtype, float(eps), group or 0, x.data_ptr(), _ptr(residual), weight.data_ptr(), _ptr(total),
-          _ptr(y), _ptr(q), _ptr(scale), _ptr(rstd))
-    return res
+    residual itself, its 'y' x. Not recorded by autograd, like expert_ffn."""
+    return (_bound or _bind()).rms_norm(x, weight, eps, residual, group, want_y, save, out)
 
 
 def norm_scratch_bytes(rows, width) -> int:
@@ -812,44 +761,7 @@ def rms_norm_backward(dy, h, weight, rstd, dsum=None, out=None, scratch=None) ->
     stream goes on. For an output in 8 bits, dy is the gradient of the values that it stands for. `out` may hand back the dict of an earlier
     call for reuse, its 'dx' may be dy or dsum itself; `scratch` is working memory of norm_scratch_bytes(rows, D), which calls that
     overlap do not share. Not recorded by autograd, like expert_ffn."""
-    _no_graph("rms_norm_backward", dy, h, weight, dsum, backward="rms_norm_backward")
-    dtype, D = _token_type(h, "h")
-    shape, kind, dev = h.shape, h.dtype, h.device
-    rows = _rows_of(h)
-    _shaped(dy, kind, shape, dev, "dy", make=False)
-    _shaped(weight, kind, (D,), dev, "weight", make=False)
-    _shaped(rstd, torch.float32, shape[:-1], dev, "rstd", make=False)
-    if dsum is not None:
-        _shaped(dsum, kind, shape, dev, "dsum", make=False)
-    have = {} if out is None else out
-    dx = _shaped(have.get("dx"), kind, shape, dev, "out['dx']")
-    dweight = _shaped(have.get("dweight"), kind, (D,), dev, "out['dweight']")
-    need = norm_scratch_bytes(rows, D)
-    if scratch is None:
-        scratch = _empty(torch.uint8, dev, max(1, need))
-    elif _dev(scratch, torch.uint8, "scratch").numel() < need or scratch.device != dev:
-        raise MoeschedError("scratch is smaller than norm_scratch_bytes, or on another device")
-    _call("moesched_rms_norm_backward", dev, rows, D, dtype, dy.data_ptr(), h.data_ptr(), weight.data_ptr(), rstd.data_ptr(), _ptr(dsum),
-          dx.data_ptr(), dweight.data_ptr(), scratch.data_ptr())
-    return {"dx": dx, "dweight": dweight}
-
-
-def _choice(logits, top_k, score, factor):
-    dtype = _TOKEN_TYPES.get(getattr(logits, "dtype", None))
-    if dtype is None:
-        raise MoeschedError("logits must be bfloat16, float16 or float32")
-    _dev(logits, logits.dtype, "logits")
-    if logits.dim() < 2 or not 1 <= logits.shape[-1] <= MAX_EXPERTS or not 1 <= top_k <= min(MAX_TOP_K, logits.shape[-1]):
-        raise MoeschedError(f"logits must be [..., T, E] with {MAX_EXPERTS} experts at most, top_k {MAX_TOP_K} and E at most")
-    if score not in _SCORES:
-        raise MoeschedError(f"score must be one of {sorted(_SCORES)}")
-    if not -3e38 < factor < 3e38:
-        raise MoeschedError("factor must be a number")
-    rows = _rows_of(logits)
-    shape = logits.shape[:-2] + (logits.shape[-2] * top_k,)
-    if shape[-1] > _INT_MAX:
-        raise MoeschedError("a source has less than 2^31 choices")
-    return dtype, rows, shape
+    return (_bound or _bind()).rms_norm_backward(dy, h, weight, rstd, dsum, out, scratch)
 
 
 def route_choose(logits, top_k, score="softmax", bias=None, normalise=False, factor=1.0, out=None) -> dict:
@@ -860,57 +772,13 @@ def route_choose(logits, top_k, score="softmax", bias=None, normalise=False, fac
     times factor. Experts whose logit (or score + bias) is -infinity or NaN are not chosen: a token without enough of them, padding for instance,
     has -1 and weight 0. A NaN among its logits makes a token's weights NaN. `out` may hand back the dict of an earlier call.
     Not recorded by autograd: the gradient comes from route_choose_backward."""
-    _no_graph("route_choose", logits, bias, backward="route_choose_backward")
-    top_k = int(top_k)
-    dtype, rows, shape = _choice(logits, top_k, score, factor)
-    E, dev = logits.shape[-1], logits.device
-    if bias is not None:
-        _shaped(bias, torch.float32, (E,), dev, "bias", make=False)
-    have = {} if out is None else out
-    experts = _shaped(have.get("experts"), torch.int32, shape, dev, "out['experts']")
-    weights = _shaped(have.get("weights"), torch.float32, shape, dev, "out['weights']")
-    _call("moesched_route_choose", dev, rows, E, top_k, dtype, _SCORES[score], int(bool(normalise)), float(factor), logits.data_ptr(),
-          _ptr(bias), experts.data_ptr(), weights.data_ptr())
-    return {"experts": experts, "weights": weights}
+    return (_bound or _bind()).route_choose(logits, top_k, score, bias, normalise, factor, out)
 
 
 def route_choose_backward(dweights, logits, experts, score="softmax", normalise=False, factor=1.0, out=None):
     """Gradient [..., T, E] of route_choose's logits, in their type, from that of its weights [..., T * top_k] float32 and the experts that it chose (the
     choice itself has no gradient, nor has the bias). Not recorded by autograd."""
-    _no_graph("route_choose_backward", dweights, logits, backward="route_choose_backward")
-    if not isinstance(logits, torch.Tensor) or not isinstance(experts, torch.Tensor) or logits.dim() < 2 or experts.dim() < 1:
-        raise MoeschedError("logits must be [..., T, E] and experts [..., T * top_k]")
-    T = logits.shape[-2]
-    top_k = experts.shape[-1] // T if T else 1
-    dtype, rows, shape = _choice(logits, top_k, score, factor)
-    dev = logits.device
-    _shaped(experts, torch.int32, shape, dev, "experts", make=False)
-    _shaped(dweights, torch.float32, shape, dev, "dweights", make=False)
-    out = _shaped(out, logits.dtype, logits.shape, dev, "out")
-    _call("moesched_route_choose_backward", dev, rows, logits.shape[-1], top_k, dtype, _SCORES[score], int(bool(normalise)), float(factor),
-          dweights.data_ptr(), logits.data_ptr(), experts.data_ptr(), out.data_ptr())
-    return out
-
-
-_ROW_TYPES = {torch.bfloat16: 2, torch.float16: 2, torch.float32: 4, torch.float8_e4m3fn: 1, torch.uint8: 1}
-
-
-def _sources(shape, tokens, slot, top_k):
-    """Number of sources and choices a token, for tensors of the leading dimensions `shape`, [..., T]; slot [..., T * top_k] is checked."""
-    slot = _dev(slot, torch.int32, "slot")
-    if slot.dim() != len(shape) or slot.shape[:-1] != shape[:-1]:
-        raise MoeschedError("slot must be [..., T * top_k], with the leading dimensions of the tokens or rows")
-    S = slot.shape[-1]
-    if top_k is None:
-        top_k = S // tokens if tokens else 1
-    if not 1 <= top_k <= MAX_TOP_K or S != tokens * top_k or S > _INT_MAX:
-        raise MoeschedError(f"slot must have top_k entries for every token, top_k {MAX_TOP_K} at most")
-    G = 1
-    for n in shape[:-1]:
-        G *= n
-    if G * tokens > _MAX_ROWS or G > _INT_MAX:
-        raise MoeschedError("at most 2^30 tokens")
-    return G, top_k
+    return (_bound or _bind()).route_choose_backward(dweights, logits, experts, score, normalise, factor, out)
 
 
 def tokens_to_rows(x, slot, scale=None, out=None, out_scale=None):
@@ -919,30 +787,7 @@ def tokens_to_rows(x, slot, scale=None, out=None, out_scale=None):
     or 8 bits (float8_e4m3fn, uint8) with scale [..., T, P] float32, which goes the same way. Returns rows [..., T * top_k, D], or
     (rows, scales). A slot outside 0 .. T * top_k - 1 is not sent; rows that no slot names are left as they were (undefined in a tensor
     made here). The slots of a source are distinct. The gradient of x is rows_to_tokens(drows, slot, top_k). Not recorded by autograd."""
-    _no_graph("tokens_to_rows", x, scale, out, backward="rows_to_tokens")
-    size = _ROW_TYPES.get(getattr(x, "dtype", None))
-    if size is None:
-        raise MoeschedError("x must be bfloat16, float16, float32, float8_e4m3fn or uint8")
-    _dev(x, x.dtype, "x")
-    if x.dim() < 2 or not 8 <= x.shape[-1] <= _MAX_WIDTH or x.shape[-1] % 8 != 0:
-        raise MoeschedError(f"x must be [..., T, D], D a multiple of 8 and {_MAX_WIDTH} at most")
-    lead, T, D, dev = x.shape[:-2], x.shape[-2], x.shape[-1], x.device
-    G, top_k = _sources(x.shape[:-1], T, slot, None)
-    if slot.device != dev:
-        raise MoeschedError("all tensors must be on one device")
-    P = 0
-    if scale is not None:
-        P = scale.shape[-1] if isinstance(scale, torch.Tensor) and scale.dim() else 0
-        _shaped(scale, torch.float32, x.shape[:-1] + (P,), dev, "scale", make=False)
-        if not 1 <= P <= D:
-            raise MoeschedError("scale must be [..., T, P], P between 1 and D")
-    elif out_scale is not None:
-        raise MoeschedError("out_scale goes with scale")
-    out = _shaped(out, x.dtype, lead + (T * top_k, D), dev, "out")
-    if P:
-        out_scale = _shaped(out_scale, torch.float32, lead + (T * top_k, P), dev, "out_scale")
-    _call("moesched_tokens_to_rows", dev, G, T, top_k, D * size, P, x.data_ptr(), _ptr(scale), slot.data_ptr(), out.data_ptr(), _ptr(out_scale))
-    return (out, out_scale) if P else out
+    return (_bound or _bind()).tokens_to_rows(x, slot, scale, out, out_scale)
 
 
 def rows_to_tokens(rows, slot, top_k, weights=None, add=None, out=None):
@@ -951,59 +796,20 @@ def rows_to_tokens(rows, slot, top_k, weights=None, add=None, out=None):
     tokens_to_rows, weights like slot in float32 (None: all 1), add [..., T, D] (a residual, a shared expert's output) or None.
     A choice that was not sent adds nothing; a token without any is add, or 0. `out` may be add itself. Not recorded by autograd: the gradients
     come from rows_to_tokens_backward, add's is dy; without weights the gradient of rows is tokens_to_rows(dy, slot)."""
-    _no_graph("rows_to_tokens", rows, weights, add, out, backward="rows_to_tokens_backward")
-    dtype, D = _token_type(rows, "rows")
-    top_k, dev = int(top_k), rows.device
-    if not 1 <= top_k <= MAX_TOP_K:
-        raise MoeschedError(f"top_k must be {MAX_TOP_K} at most")
-    T = rows.shape[-2] // top_k
-    G, _ = _sources(rows.shape[:-1], T, slot, top_k)
-    if slot.shape != rows.shape[:-1] or slot.device != dev:
-        raise MoeschedError("slot must be [..., T * top_k], on the device of rows")
-    shape = rows.shape[:-2] + (T, D)
-    if weights is not None:
-        _shaped(weights, torch.float32, slot.shape, dev, "weights", make=False)
-    if add is not None:
-        _shaped(add, rows.dtype, shape, dev, "add", make=False)
-    out = _shaped(out, rows.dtype, shape, dev, "out")
-    _call("moesched_rows_to_tokens", dev, G, T, top_k, D, dtype, rows.data_ptr(), slot.data_ptr(), _ptr(weights), _ptr(add), out.data_ptr())
-    return out
+    return (_bound or _bind()).rows_to_tokens(rows, slot, top_k, weights, add, out)
 
 
 def rows_to_tokens_backward(dy, rows, slot, weights, out=None) -> dict:
     """Gradients of rows_to_tokens: 'drows' [..., T * top_k, D], drows[slot] = weight * dy, rows that no slot names left as they were
     (undefined in a tensor made here), and 'dweights' [..., T * top_k] float32, 0 for a choice that was not sent. `out` may hand back the dict of
     an earlier call, or have one of the two; its 'drows' may be rows itself. Not recorded by autograd."""
-    _no_graph("rows_to_tokens_backward", dy, rows, weights, backward="rows_to_tokens_backward")
-    dtype, D = _token_type(dy, "dy")
-    T, dev = dy.shape[-2], dy.device
-    G, top_k = _sources(dy.shape[:-1], T, slot, None)
-    if slot.device != dev:
-        raise MoeschedError("all tensors must be on one device")
-    shape = dy.shape[:-2] + (T * top_k, D)
-    _shaped(rows, dy.dtype, shape, dev, "rows", make=False)
-    _shaped(weights, torch.float32, slot.shape, dev, "weights", make=False)
-    have = {} if out is None else out
-    drows = _shaped(have.get("drows"), dy.dtype, shape, dev, "out['drows']")
-    dweights = _shaped(have.get("dweights"), torch.float32, slot.shape, dev, "out['dweights']")
-    _call("moesched_rows_to_tokens_backward", dev, G, T, top_k, D, dtype, dy.data_ptr(), rows.data_ptr(), slot.data_ptr(),
-          weights.data_ptr(), drows.data_ptr(), dweights.data_ptr())
-    return {"drows": drows, "dweights": dweights}
+    return (_bound or _bind()).rows_to_tokens_backward(dy, rows, slot, weights, out)
 
 
 def rows_widen(rows, scale, group, dtype=torch.bfloat16, out=None):
     """Rows in 8 bits, as they arrive, in a type that expert_ffn takes: rows [..., D] float8_e4m3fn times scale [..., ceil(D / group)] float32,
     one for every `group` columns (32, 64 or 128), rounded once to dtype (bfloat16, float16 or float32)."""
-    if dtype not in _TOKEN_TYPES:
-        raise MoeschedError("dtype must be bfloat16, float16 or float32")
-    rows, group = _dev(rows, torch.float8_e4m3fn, "rows"), _group(group)
-    if rows.dim() < 2 or not 8 <= rows.shape[-1] <= _MAX_WIDTH or rows.shape[-1] % 8 != 0:
-        raise MoeschedError(f"rows must be [..., D], D a multiple of 8 and {_MAX_WIDTH} at most")
-    D, dev = rows.shape[-1], rows.device
-    _shaped(scale, torch.float32, rows.shape[:-1] + (-(-D // group),), dev, "scale", make=False)
-    out = _shaped(out, dtype, rows.shape, dev, "out")
-    _call("moesched_rows_widen", dev, _rows_of(rows), D, group, _TOKEN_TYPES[dtype], rows.data_ptr(), scale.data_ptr(), out.data_ptr())
-    return out
+    return (_bound or _bind()).rows_widen(rows, scale, group, dtype, out)
 
 
 def _expert_curve(tokens, times):

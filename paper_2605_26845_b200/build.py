@@ -12,6 +12,7 @@ SOURCES = ["api.cu", "mw_kernel.cu", "bvn_kernel.cu", "bvn_small.cu", "bvn_real_
 HEADERS = [os.path.join(CSRC, "common.cuh"), os.path.join(CSRC, "peel.cuh"), os.path.join(CSRC, "small.cuh"), os.path.join(CSRC, "expert.cuh"), os.path.join(CSRC, "token.cuh"), os.path.join(CSRC, "schedule_read.h"), os.path.join(HERE, "..", "include", "moesched.h")]
 LIB = os.path.join(HERE, "libmoesched.so")
 LIB_CHECKED = os.path.join(HERE, "libmoesched_checked.so")   # the same sources with -DMOESCHED_CHECKED
+BINDING = os.path.join(HERE, "_binding.so")                  # the compiled part of the Python binding (csrc/binding.cpp)
 
 
 def _stale(lib) -> bool:
@@ -22,10 +23,31 @@ def _stale(lib) -> bool:
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def build_binding(force: bool = False) -> str:
+    """Compile the Python extension that calls the library (g++, against the installed torch; no GPU code)."""
+    source = os.path.join(CSRC, "binding.cpp")
+    newest = max(os.path.getmtime(p) for p in (source, os.path.join(HERE, "..", "include", "moesched.h")))
+    if not force and os.path.exists(BINDING) and os.path.getmtime(BINDING) >= newest:
+        return BINDING
+    import sysconfig
+
+    import torch
+    root = os.path.dirname(torch.__file__)
+    cuda = os.environ.get("CUDA_HOME", "/usr/local/cuda")
+    includes = [sysconfig.get_paths()["include"], os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"),
+                os.path.join(cuda, "include")]
+    libs = os.path.join(root, "lib")
+    subprocess.run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
+                    *(f"-I{p}" for p in includes), source, "-o", BINDING, f"-L{libs}", f"-Wl,-rpath,{libs}", "-lc10", "-lc10_cuda", "-ltorch_cpu",
+                    "-ltorch_cuda", "-ltorch_python"], check=True)
+    return BINDING
+
+
 def build(force: bool = False, verbose: bool = False, checked: bool = False) -> str:
     """Compile every source to an object file (in parallel, one nvcc per file) and link the library.
     checked=True builds the variant whose kernels range-check their data-dependent indices."""
     lib = LIB_CHECKED if checked else LIB
+    build_binding(force)
     if not (force or _stale(lib)):
         return lib
     from concurrent.futures import ThreadPoolExecutor

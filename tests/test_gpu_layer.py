@@ -4,6 +4,7 @@ import pytest
 import torch
 
 import paper_2605_26845_b200 as ms
+from test_token_host import refused
 
 pytestmark = pytest.mark.gpu
 
@@ -131,3 +132,29 @@ def test_padding_is_not_sent():
     assert (rows[0, 1, 10:] == 7).all()
     y = ms.rows_to_tokens(rows, d["slot"], 2, weights=c["weights"], add=x)
     assert torch.equal(y[0, 1, 5:], x[0, 1, 5:])
+
+
+def test_what_is_refused_on_the_gpu():
+    wrong, missing, right = refused(lambda shape, dtype: torch.zeros(shape, dtype=dtype, device="cuda"))
+    for call in right:
+        call()
+    for n, call in enumerate(wrong + missing):
+        with pytest.raises(ms.MoeschedError):
+            call()
+            print("not refused:", n)
+    bf, f32, i32 = torch.bfloat16, torch.float32, torch.int32
+    x, w = torch.zeros((6, 64), dtype=bf, device="cuda"), torch.zeros(64, dtype=bf, device="cuda")
+    l, slot, ex = torch.zeros((6, 10), device="cuda"), torch.zeros(12, dtype=i32, device="cuda"), torch.zeros(12, dtype=i32, device="cuda")
+    rows, weights, rstd = torch.zeros((12, 64), dtype=bf, device="cuda"), torch.zeros(12, device="cuda"), torch.zeros(6, device="cuda")
+    other = torch.zeros((5, 64), dtype=bf, device="cuda")
+    host = dict(x=x.cpu(), w=w.cpu(), slot=slot.cpu(), weights=weights.cpu())
+    for call in (lambda: ms.rms_norm(x, w, out={"y": other}), lambda: ms.rms_norm(x, w, group=32, out={"q": x}), lambda: ms.rms_norm(x, w, save=True, out={"rstd": weights}),
+                 lambda: ms.rms_norm(x, w, out=[x]), lambda: ms.rms_norm(x, w, out={"y": x.t().contiguous().t()}), lambda: ms.rms_norm_backward(x, x, w, rstd, out={"dweight": rstd}),
+                 lambda: ms.route_choose(l, 2, out={"experts": ex.view(6, 2)}), lambda: ms.route_choose_backward(weights, l, ex, out=x), lambda: ms.tokens_to_rows(x, slot, out=x),
+                 lambda: ms.tokens_to_rows(x, slot, scale=l, out_scale=l), lambda: ms.rows_to_tokens(rows, slot, 2, out=rows), lambda: ms.rows_to_tokens_backward(x, rows, slot, weights, out={"drows": x}),
+                 lambda: ms.rows_to_tokens(rows, slot, 2, out=x.float()), lambda: ms.rms_norm(x, host["w"]), lambda: ms.rms_norm(host["x"], w), lambda: ms.tokens_to_rows(x, host["slot"]),
+                 lambda: ms.rows_to_tokens(rows, slot, 2, weights=host["weights"]), lambda: ms.rms_norm(x, w, out={"y": host["x"]}),
+                 lambda: ms.rms_norm(torch.zeros(6 * 64 + 1, dtype=bf, device="cuda")[1:].view(6, 64), w)):       # (the last one is not on 16 bytes)
+        with pytest.raises(ms.MoeschedError):
+            call()
+    assert torch.equal(ms.rms_norm(x, w, out={})["y"], x)

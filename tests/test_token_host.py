@@ -113,72 +113,89 @@ def test_rows_widen_checks_its_arguments(lib):
     assert call(R=0, q=None) == 0
 
 
-class Rows(torch.Tensor):
-    """Says that it is on a GPU, so that the checks behind that one are reached; nothing is read."""
-    @property
-    def is_cuda(self):
-        return True
-
-
-def on_gpu(*shape, dtype=torch.bfloat16):
-    return torch.zeros(shape, dtype=dtype).as_subclass(Rows)
-
-
-def test_the_binding_refuses_wrong_tensors(monkeypatch):
-    made = []
-    monkeypatch.setattr(ms, "_call", lambda name, device, *args: made.append(name))
-    monkeypatch.setattr(ms, "_allocator", lambda device: lambda shape, strides, dtype: torch.empty(shape, dtype=dtype))
+def refused(on):
+    """Calls with something wrong, on tensors made by on(shape, dtype); and with something missing."""
     i32, f32, f8 = torch.int32, torch.float32, torch.float8_e4m3fn
-    x, w, slot, wide = on_gpu(6, 64), on_gpu(64), on_gpu(12, dtype=i32), on_gpu(6, 64, dtype=f32)
-    rows, weights = on_gpu(12, 64), on_gpu(12, dtype=f32)
-    l, ex = on_gpu(6, 10, dtype=f32), on_gpu(12, dtype=i32)
-    rstd, q, s = on_gpu(6, dtype=f32), on_gpu(6, 64, dtype=f8), on_gpu(6, 2, dtype=f32)
+
+    def t(*shape, dtype=torch.bfloat16):
+        return on(shape, dtype)
+
+    x, w, slot, wide = t(6, 64), t(64), t(12, dtype=i32), t(6, 64, dtype=f32)
+    rows, weights = t(12, 64), t(12, dtype=f32)
+    l, ex = t(6, 10, dtype=f32), t(12, dtype=i32)
+    rstd, q, s = t(6, dtype=f32), t(6, 64, dtype=f8), t(6, 2, dtype=f32)
     wrong = (
-        lambda: ms.rms_norm(torch.zeros(6, 64), torch.zeros(64)), lambda: ms.rms_norm(None, w), lambda: ms.rms_norm(x, None),
-        lambda: ms.rms_norm(x, on_gpu(64, dtype=f32)), lambda: ms.rms_norm(x, on_gpu(32)), lambda: ms.rms_norm(w, w),
-        lambda: ms.rms_norm(on_gpu(6, 60), on_gpu(60)), lambda: ms.rms_norm(x.double(), w.double()), lambda: ms.rms_norm(x.t(), on_gpu(6)),
-        lambda: ms.rms_norm(x, w, eps=-1.0), lambda: ms.rms_norm(x, w, eps=float("nan")), lambda: ms.rms_norm(x, w, group=16),
-        lambda: ms.rms_norm(x, w, want_y=False), lambda: ms.rms_norm(x, w, residual=on_gpu(5, 64)), lambda: ms.rms_norm(x, w, residual=wide),
-        lambda: ms.rms_norm(x, w, out={"y": on_gpu(5, 64)}), lambda: ms.rms_norm(x, w, group=32, out={"q": x}),
-        lambda: ms.rms_norm(x, w, save=True, out={"rstd": on_gpu(5, dtype=f32)}),
-        lambda: ms.rms_norm_backward(x, x, w, on_gpu(5, dtype=f32)), lambda: ms.rms_norm_backward(None, x, w, rstd),
-        lambda: ms.rms_norm_backward(x, x, w, rstd, dsum=wide), lambda: ms.rms_norm_backward(x, x, w, rstd, out={"dweight": on_gpu(32)}),
-        lambda: ms.rms_norm_backward(x, x, w, rstd, scratch=on_gpu(8, dtype=torch.uint8)),
-        lambda: ms.route_choose(l, 0), lambda: ms.route_choose(l, 11), lambda: ms.route_choose(l, 2, score="tanh"), lambda: ms.route_choose(l.double(), 2),
-        lambda: ms.route_choose(on_gpu(6, 1025, dtype=f32), 2), lambda: ms.route_choose(on_gpu(6, 64, dtype=f32), 33), lambda: ms.route_choose(on_gpu(10, dtype=f32), 2),
-        lambda: ms.route_choose(l, 2, bias=on_gpu(9, dtype=f32)), lambda: ms.route_choose(l, 2, factor=float("inf")), lambda: ms.route_choose(torch.zeros(6, 10), 2),
-        lambda: ms.route_choose(l, 2, out={"experts": on_gpu(6, 2, dtype=i32)}),
-        lambda: ms.route_choose_backward(on_gpu(11, dtype=f32), l, ex), lambda: ms.route_choose_backward(weights, l, on_gpu(11, dtype=i32)),
-        lambda: ms.route_choose_backward(weights, l, on_gpu(0, dtype=i32)), lambda: ms.route_choose_backward(weights, None, ex),
-        lambda: ms.route_choose_backward(weights, l, ex, out=on_gpu(6, 10)),
-        lambda: ms.tokens_to_rows(x, on_gpu(13, dtype=i32)), lambda: ms.tokens_to_rows(x, on_gpu(0, dtype=i32)), lambda: ms.tokens_to_rows(x, slot.long()),
-        lambda: ms.tokens_to_rows(x, on_gpu(6 * 33, dtype=i32)), lambda: ms.tokens_to_rows(x, on_gpu(1, 12, dtype=i32)), lambda: ms.tokens_to_rows(on_gpu(6, 12), slot),
-        lambda: ms.tokens_to_rows(x.double(), slot), lambda: ms.tokens_to_rows(x, slot, out=x), lambda: ms.tokens_to_rows(x, slot, scale=on_gpu(5, 2, dtype=f32)),
-        lambda: ms.tokens_to_rows(x, slot, scale=on_gpu(6, 0, dtype=f32)), lambda: ms.tokens_to_rows(x, slot, out_scale=s), lambda: ms.tokens_to_rows(torch.zeros(6, 64), slot),
-        lambda: ms.rows_to_tokens(rows, slot, 5), lambda: ms.rows_to_tokens(rows, slot, 0), lambda: ms.rows_to_tokens(rows, on_gpu(10, dtype=i32), 2),
-        lambda: ms.rows_to_tokens(rows, slot, 2, weights=on_gpu(12)), lambda: ms.rows_to_tokens(rows, slot, 2, add=rows), lambda: ms.rows_to_tokens(on_gpu(12, 64, dtype=f8), slot, 2),
-        lambda: ms.rows_to_tokens(rows, slot, 2, out=wide),
-        lambda: ms.rows_to_tokens_backward(x, x, slot, weights), lambda: ms.rows_to_tokens_backward(x, rows, slot, None),
-        lambda: ms.rows_to_tokens_backward(wide, rows, slot, weights), lambda: ms.rows_to_tokens_backward(x, rows, slot, weights, out={"drows": x}),
-        lambda: ms.rows_widen(x, s, 32), lambda: ms.rows_widen(q, s, 64), lambda: ms.rows_widen(q, s, 32, torch.float64), lambda: ms.rows_widen(q, s, 48),
-        lambda: ms.rows_widen(q, s, 32, out=wide),
+        lambda: ms.rms_norm(x, t(64, dtype=f32)), lambda: ms.rms_norm(x, t(32)), lambda: ms.rms_norm(w, x), lambda: ms.rms_norm(t(), w),
+        lambda: ms.rms_norm(t(6, 60), t(60)), lambda: ms.rms_norm(t(6, 65544), t(65544)), lambda: ms.rms_norm(x.double(), w.double()), lambda: ms.rms_norm(x.t(), t(6)),
+        lambda: ms.rms_norm(t(64, 8).t(), w), lambda: ms.rms_norm(x, t(128)[::2]),
+        lambda: ms.rms_norm(x, w, eps=-1.0), lambda: ms.rms_norm(x, w, eps=float("nan")), lambda: ms.rms_norm(x, w, eps=float("inf")), lambda: ms.rms_norm(x, w, group=16),
+        lambda: ms.rms_norm(x, w, want_y=False), lambda: ms.rms_norm(x, w, residual=t(5, 64)), lambda: ms.rms_norm(x, w, residual=wide),
+        lambda: ms.rms_norm_backward(x, x, w, t(5, dtype=f32)), lambda: ms.rms_norm_backward(x, x, w, t(6)), lambda: ms.rms_norm_backward(wide, x, w, rstd),
+        lambda: ms.rms_norm_backward(x, x, w, rstd, dsum=wide), lambda: ms.rms_norm_backward(x, x, w, rstd, scratch=t(8, dtype=torch.uint8)),
+        lambda: ms.rms_norm_backward(x, x, w, rstd, scratch=t(1 << 16, dtype=f32)),
+        lambda: ms.route_choose(l, 0), lambda: ms.route_choose(l, 11), lambda: ms.route_choose(l, 1 << 40), lambda: ms.route_choose(l, -1), lambda: ms.route_choose(l, 2, score="tanh"),
+        lambda: ms.route_choose(l, 2, score=None), lambda: ms.route_choose(l.double(), 2), lambda: ms.route_choose(t(6, 0, dtype=f32), 1),
+        lambda: ms.route_choose(t(6, 1025, dtype=f32), 2), lambda: ms.route_choose(t(6, 64, dtype=f32), 33), lambda: ms.route_choose(t(10, dtype=f32), 2),
+        lambda: ms.route_choose(l, 2, bias=t(9, dtype=f32)), lambda: ms.route_choose(l, 2, bias=t(10)), lambda: ms.route_choose(l, 2, factor=float("inf")), lambda: ms.route_choose(l.t(), 2),
+        lambda: ms.route_choose_backward(t(11, dtype=f32), l, ex), lambda: ms.route_choose_backward(weights, l, t(11, dtype=i32)), lambda: ms.route_choose_backward(weights, l, t(6, 2, dtype=i32)),
+        lambda: ms.route_choose_backward(weights, l, t(0, dtype=i32)), lambda: ms.route_choose_backward(t(12), l, ex), lambda: ms.route_choose_backward(weights, l[0], ex),
+        lambda: ms.tokens_to_rows(x, t(13, dtype=i32)), lambda: ms.tokens_to_rows(x, t(0, dtype=i32)), lambda: ms.tokens_to_rows(x, slot.long()), lambda: ms.tokens_to_rows(w, slot),
+        lambda: ms.tokens_to_rows(x, t(6 * 33, dtype=i32)), lambda: ms.tokens_to_rows(x, t(1, 12, dtype=i32)), lambda: ms.tokens_to_rows(t(6, 12), slot),
+        lambda: ms.tokens_to_rows(x.double(), slot), lambda: ms.tokens_to_rows(x, slot, scale=t(5, 2, dtype=f32)), lambda: ms.tokens_to_rows(x, slot, scale=t(6, 2)),
+        lambda: ms.tokens_to_rows(x, slot, scale=t(6, 0, dtype=f32)), lambda: ms.tokens_to_rows(x, slot, scale=t(6, 65, dtype=f32)), lambda: ms.tokens_to_rows(x, slot, out_scale=s),
+        lambda: ms.rows_to_tokens(rows, slot, 5), lambda: ms.rows_to_tokens(rows, slot, 0), lambda: ms.rows_to_tokens(rows, slot, 36), lambda: ms.rows_to_tokens(rows, t(10, dtype=i32), 2),
+        lambda: ms.rows_to_tokens(rows, slot, 2, weights=t(12)), lambda: ms.rows_to_tokens(rows, slot, 2, add=rows), lambda: ms.rows_to_tokens(t(12, 64, dtype=f8), slot, 2),
+        lambda: ms.rows_to_tokens(rows, t(12), 2),
+        lambda: ms.rows_to_tokens_backward(x, x, slot, weights), lambda: ms.rows_to_tokens_backward(wide, rows, slot, weights), lambda: ms.rows_to_tokens_backward(x, rows, slot, t(12)),
+        lambda: ms.rows_widen(x, s, 32), lambda: ms.rows_widen(q, s, 64), lambda: ms.rows_widen(q, s, 32, torch.float64), lambda: ms.rows_widen(q, s, 48), lambda: ms.rows_widen(q, s, 32, None),
     )
+    missing = (
+        lambda: ms.rms_norm(None, w), lambda: ms.rms_norm(x, None), lambda: ms.rms_norm_backward(None, x, w, rstd), lambda: ms.rms_norm_backward(x, x, w, None),
+        lambda: ms.route_choose(None, 2), lambda: ms.route_choose_backward(weights, None, ex), lambda: ms.route_choose_backward(weights, l, None), lambda: ms.route_choose_backward(None, l, ex),
+        lambda: ms.tokens_to_rows(None, slot), lambda: ms.tokens_to_rows(x, None), lambda: ms.rows_to_tokens(None, slot, 2), lambda: ms.rows_to_tokens(rows, None, 2),
+        lambda: ms.rows_to_tokens_backward(x, rows, slot, None), lambda: ms.rows_widen(None, s, 32), lambda: ms.rows_widen(q, None, 32), lambda: ms.rms_norm([1.0], w),
+    )
+    right = (
+        lambda: ms.rms_norm(x, w, residual=x, group=32), lambda: ms.rms_norm_backward(x, x, w, rstd), lambda: ms.route_choose(l, 2), lambda: ms.route_choose_backward(weights, l, ex),
+        lambda: ms.tokens_to_rows(x, slot), lambda: ms.rows_to_tokens(rows, slot, 2), lambda: ms.rows_to_tokens_backward(x, rows, slot, weights), lambda: ms.rows_widen(q, s, 32),
+    )
+    return wrong, missing, right
+
+
+def test_the_binding_refuses_wrong_tensors(lib):
+    wrong, missing, right = refused(lambda shape, dtype: torch.zeros(shape, dtype=dtype))
     for n, call in enumerate(wrong):
-        with pytest.raises(ms.MoeschedError):
+        with pytest.raises(ms.MoeschedError, match="^(?!.*CUDA tensor)"):        # (something else than where the tensors are)
             call()
             print("not refused:", n)
-    assert made == []
+    for call in missing + right:
+        with pytest.raises(ms.MoeschedError, match="must be a CUDA tensor"):
+            call()
+    for call in (lambda: ms.route_choose(torch.zeros(4, 4), "two"), lambda: ms.rms_norm(torch.zeros(4, 8), torch.zeros(8), eps="no"),
+                 lambda: ms._bound.rms_norm(1), lambda: ms._bound.bind(1)):
+        with pytest.raises((TypeError, ValueError)):
+            call()
 
 
-def test_tensors_that_want_a_gradient_are_refused_where_autograd_records():
+def test_a_missing_part_of_the_binding_is_said(monkeypatch, lib):
+    import sys
+    monkeypatch.setattr(ms, "_bound", None)
+    monkeypatch.delattr(ms, "_binding", raising=False)
+    monkeypatch.setitem(sys.modules, ms.__name__ + "._binding", None)
+    with pytest.raises(ms.MoeschedError, match="build"):
+        ms.rms_norm(torch.zeros(4, 8), torch.zeros(8))
+
+
+def test_tensors_that_want_a_gradient_are_refused_where_autograd_records(lib):
     x, w, slot = torch.zeros((4, 8)), torch.zeros(8), torch.zeros(8, dtype=torch.int32)
     want = x.clone().requires_grad_()
-    f = torch.zeros(8)
-    calls = (lambda t: ms.rms_norm(t, w), lambda t: ms.rms_norm(x, w, residual=t), lambda t: ms.rms_norm_backward(t, x, w, f),
+    f, r4 = torch.zeros(8), torch.zeros(4)
+    calls = (lambda t: ms.rms_norm(t, w), lambda t: ms.rms_norm(x, w, residual=t), lambda t: ms.rms_norm_backward(t, x, w, r4),
              lambda t: ms.route_choose(t, 2), lambda t: ms.route_choose_backward(f, t, slot), lambda t: ms.tokens_to_rows(t, slot),
-             lambda t: ms.rows_to_tokens(t, slot, 2), lambda t: ms.rows_to_tokens(x, slot, 2, add=t), lambda t: ms.rows_to_tokens_backward(t, x, slot, f))
+             lambda t: ms.rows_to_tokens(t, slot[:4], 2), lambda t: ms.rows_to_tokens(x, slot[:4], 2, add=t), lambda t: ms.rows_to_tokens_backward(t, torch.zeros((8, 8)), slot, f))
     for n, call in enumerate(calls):
         with pytest.raises(ms.MoeschedError, match="no_grad"):
             call(want)
-        with torch.no_grad(), pytest.raises(ms.MoeschedError, match="CUDA tensor"):       # (the next check)
-            call(want)
+        if n != 7:
+            with torch.no_grad(), pytest.raises(ms.MoeschedError, match="CUDA tensor"):       # (the last check)
+                call(want)
