@@ -33,8 +33,12 @@ __device__ __forceinline__ unsigned long long warp_most(unsigned long long v) {
   const unsigned lo = __reduce_max_sync(FULL, (unsigned)(v >> 32) == hi ? (unsigned)v : 0u);
   return (unsigned long long)hi << 32 | lo;
 }
-__device__ __forceinline__ float warp_most(float v) {
+__device__ __forceinline__ float warp_most(float v) {            // NaN is none
   asm volatile("redux.sync.max.f32 %0, %0, 0xffffffff;" : "+f"(v));
+  return v;
+}
+__device__ __forceinline__ float warp_most_or_nan(float v) {
+  asm volatile("redux.sync.max.NaN.f32 %0, %0, 0xffffffff;" : "+f"(v));
   return v;
 }
 
@@ -63,13 +67,11 @@ __device__ __forceinline__ int greatest(Key (&key)[J], int count) {
 
 // The keys that may be among the `count` greatest, in falling order, the lowest expert first among equal ones: lane i gets the i-th. The count-th greatest of
 // the lanes' own greatest keys has `count` keys at or above it, so that nothing below it is wanted; spare(key) is the lowest key that has to be looked at
-// all the same. Returns how many there are: with more than 32, nothing else holds. -infinity and NaN are no keys. list: [64], of the warp.
+// all the same. Returns how many there are: with more than 32, nothing else holds. -infinity and NaN are no keys. best: the lane's greatest; list: [64], of the
+// warp.
 template <int J, typename Spare>
-__device__ __forceinline__ int candidates(const float (&key)[J], int count, uint2* list, Spare spare, float& own, int& expert) {
+__device__ __forceinline__ int candidates(const float (&key)[J], float best, int count, uint2* list, Spare spare, float& own, int& expert) {
   const int lane = threadIdx.x & 31;
-  float best = fmaxf(key[0], -INFINITY);
-#pragma unroll
-  for (int j = 1; j < J; ++j) best = fmaxf(best, key[j]);
   float bound = -INFINITY;
   for (int r = 0; r < count; ++r) {                             // (equal ones go together: the bound is only lower for it)
     bound = warp_most(best);
@@ -102,14 +104,18 @@ __device__ __forceinline__ int candidates(const float (&key)[J], int count, uint
   for (int j = 0; j < J; ++j)
     if (key[j] >= bound) list[at++] = make_uint2(__float_as_uint(key[j]), lane * J + j);
   __syncwarp();
-  const uint2 entry = lane < found ? list[lane] : make_uint2(0xff800000u, 0u);
+  // up to 16 keys: two lanes for each, which count among one half of them
+  const bool two_each = found <= 16;
+  const int which = two_each ? lane & 15 : lane, half = (found + 1) / 2, from = two_each && lane >= 16 ? half : 0, steps = two_each ? half : found;
+  const uint2 entry = which < found ? list[which] : make_uint2(0xff800000u, 0u);
   const unsigned mine = ordered(__uint_as_float(entry.x));
   int place = 0;
-#pragma unroll 4
-  for (int i = 0; i < found; ++i) {
-    const unsigned other = __shfl_sync(FULL, mine, i);
-    place += other + (i < lane) > mine;                         // (no key is the greatest number)
+#pragma unroll 2
+  for (int i = 0; i < steps; ++i) {
+    const unsigned other = __shfl_sync(FULL, mine, from + i);
+    place += other + (from + i < which) > mine;                 // (no key is the greatest number)
   }
+  if (two_each) place += __shfl_xor_sync(FULL, place, 16);
   if (lane < found) list[32 + place] = entry;
   __syncwarp();
   const uint2 sorted = lane < found ? list[32 + lane] : make_uint2(0xff800000u, 0xffffffffu);
@@ -123,21 +129,22 @@ __device__ __forceinline__ int candidates(const float (&key)[J], int count, uint
 // steps; the quotient by 2 steps), the sum with the bias by half a step of its own.
 __device__ __forceinline__ float apart(float u, float v) { return 0x1p-17f + 0x1p-23f * (fabsf(u) + fabsf(v)); }
 
-// The lane's logits, -infinity where there is no expert. WIDE: as many as 16 bytes hold at a time
-template <typename T, int J, bool WIDE>
-__device__ __forceinline__ void load_logits(const T* logits, int E, float (&l)[J]) {
+// The lane's logits (or biases), -infinity where there is no expert. wide: as many as 16 bytes hold at a time
+template <typename T, int J>
+__device__ __forceinline__ void load_logits(const T* logits, int E, bool wide, float (&l)[J]) {
   constexpr int COUNT = Vec<T>::COUNT;
+  constexpr unsigned NONE = sizeof(T) == 4 ? 0xff800000u : std::is_same_v<T, __half> ? 0xfc00fc00u : 0xff80ff80u;
   const int first = (threadIdx.x & 31) * J;
-  if constexpr (WIDE && J % COUNT == 0) {
+  if (J % COUNT == 0 && wide) {
 #pragma unroll
     for (int j = 0; j < J; j += COUNT) {
       float f[COUNT];
-      uint4 v = make_uint4(0u, 0u, 0u, 0u);
-      const bool in = first + j < E;
-      if (in) v = __ldg(reinterpret_cast<const uint4*>(logits + first + j));
+      uint4 v = make_uint4(NONE, NONE, NONE, NONE);
+      if (first + j < E) v = __ldg(reinterpret_cast<const uint4*>(logits + first + j));
       Vec<T>::unpack(v, f);
 #pragma unroll
-      for (int q = 0; q < COUNT; ++q) l[j + q] = in ? f[q] : -INFINITY;
+      for (int q = 0; q < COUNT; ++q)
+        if (j + q < J) l[j + q] = f[q];
     }
   } else {
 #pragma unroll
@@ -149,13 +156,18 @@ __device__ __forceinline__ void load_logits(const T* logits, int E, float (&l)[J
 __device__ __forceinline__ float exponential(float v) { return __expf(v); }
 __device__ __forceinline__ float logistic(float v) { return __fdividef(1.0f, 1.0f + exponential(-v)); }
 
+template <int J>
+__device__ __forceinline__ float most_of(const float (&v)[J]) {
+  float m = fmaxf(v[0], -INFINITY);
+#pragma unroll
+  for (int j = 1; j < J; ++j) m = fmaxf(m, v[j]);
+  return m;
+}
+
 // greatest logit of the row, and the sum of e^(l - m); the sum of a row without a logit is 0
 template <int J>
 __device__ __forceinline__ void softmax_of(const float (&l)[J], float& m, float& sum) {
-  m = l[0];
-#pragma unroll
-  for (int j = 1; j < J; ++j) m = fmaxf(m, l[j]);
-  m = warp_most(m);
+  m = warp_most(most_of(l));
   sum = 0.0f;
   if (m == -INFINITY) return;
 #pragma unroll
@@ -196,8 +208,8 @@ __device__ __noinline__ int choose64(const float (&l)[J], const float* bias, int
   return greatest(key, k);
 }
 
-template <typename T, int J, int SCORE, bool WIDE>
-__global__ void __launch_bounds__(32 * CHOOSE_WARPS) choose_kernel(int rows, int E, int k, int normalise, float factor,
+template <typename T, int J, int SCORE, bool BIAS>
+__global__ void __launch_bounds__(32 * CHOOSE_WARPS, J <= 8 ? 5 : 1) choose_kernel(int rows, int E, int k, int normalise, int wide, float factor,
                                                                    const T* __restrict__ logits, const float* __restrict__ bias,
                                                                    int32_t* __restrict__ experts, float* __restrict__ weights) {
   constexpr bool SOFTMAX = SCORE == MOESCHED_SCORE_SOFTMAX;
@@ -207,17 +219,25 @@ __global__ void __launch_bounds__(32 * CHOOSE_WARPS) choose_kernel(int rows, int
   const long long row = (long long)blockIdx.x * CHOOSE_WARPS + (threadIdx.x >> 5);
   if (row >= rows) return;
   const T* own = logits + row * E;
-  float l[J], top = 0.0f, sum = 0.0f;
-  load_logits<T, J, WIDE>(own, E, l);
-  float most = l[0];                                             // NaN if one of them is
+  float l[J], top = 0.0f, sum = 0.0f, best = 0.0f;
+  load_logits(own, E, wide != 0, l);
+  best = l[0];
 #pragma unroll
-  for (int j = 1; j < J; ++j) asm("max.NaN.f32 %0, %0, %1;" : "+f"(most) : "f"(l[j]));
-  const bool lost = __any_sync(FULL, isnan(most));
-  if (SOFTMAX && (bias != nullptr || !normalise)) softmax_of(l, top, sum);
+  for (int j = 1; j < J; ++j) asm("max.NaN.f32 %0, %0, %1;" : "+f"(best) : "f"(l[j]));
+  const bool lost = isnan(warp_most_or_nan(best));
+  if (lost) best = most_of(l);
+  if (SOFTMAX && (BIAS || !normalise)) {
+    top = warp_most(best);
+    if (top > -INFINITY) {
+#pragma unroll
+      for (int j = 0; j < J; ++j) sum += exponential(l[j] - top);
+      sum = warp_sum(sum);
+    }
+  }
   float mine;
   int expert, found;
-  if (bias == nullptr) {
-    found = candidates(l, k, list, [](float b) { return b; }, mine, expert);
+  if constexpr (!BIAS) {
+    found = candidates(l, best, k, list, [](float b) { return b; }, mine, expert);
     if (found > 32) {
       unsigned key[J];
 #pragma unroll
@@ -227,14 +247,14 @@ __global__ void __launch_bounds__(32 * CHOOSE_WARPS) choose_kernel(int rows, int
     }
   } else {
     float key[J];
+    load_logits(bias, E, J % 4 == 0 && E % 4 == 0 && (reinterpret_cast<uintptr_t>(bias) & 15) == 0, key);
     const float share = SOFTMAX ? __fdividef(1.0f, sum) : 0.0f;
 #pragma unroll
     for (int j = 0; j < J; ++j) {
-      const int e = lane * J + j;
       const float s = SOFTMAX ? exponential(l[j] - top) * share : logistic(l[j]);
-      key[j] = e < E && l[j] > -INFINITY ? s + __ldg(bias + e) : -INFINITY;
+      key[j] = l[j] > -INFINITY ? s + key[j] : -INFINITY;
     }
-    found = candidates(key, k, list, [](float b) { return b - 2.0f * apart(b, b); }, mine, expert);
+    found = candidates(key, most_of(key), k, list, [](float b) { return b - 2.0f * apart(b, b); }, mine, expert);
     const float next = __shfl_down_sync(FULL, mine, 1);
     const bool near = lane < k && lane + 1 < found && !(mine - next > apart(mine, next));
     if (found > 32 || __any_sync(FULL, near)) expert = choose64<J, SCORE>(l, bias, E, k, top);
@@ -253,8 +273,8 @@ __global__ void __launch_bounds__(32 * CHOOSE_WARPS) choose_kernel(int rows, int
 //   softmax             p (a [chosen] - sum a p)      over all experts
 //   softmax, normalised q (a - sum a q)               over the chosen, 0 for the others
 //   logistic            a s (1 - s);  normalised  q (a - sum a q) (1 - s)
-template <typename T, int J, int SCORE, bool WIDE>
-__global__ void __launch_bounds__(32 * CHOOSE_WARPS) choose_backward_kernel(int rows, int E, int k, int normalise, float factor,
+template <typename T, int J, int SCORE>
+__global__ void __launch_bounds__(32 * CHOOSE_WARPS) choose_backward_kernel(int rows, int E, int k, int normalise, int wide, float factor,
                                                                             const float* __restrict__ dweights,
                                                                             const T* __restrict__ logits,
                                                                             const int32_t* __restrict__ experts, T* dlogits) {
@@ -269,7 +289,7 @@ __global__ void __launch_bounds__(32 * CHOOSE_WARPS) choose_backward_kernel(int 
   float a = lane < k ? dweights[row * k + lane] * factor : 0.0f;
   const bool all = SOFTMAX && !normalise;
   if (!all) {                                                    // zeros, while the choices are on their way
-    if (WIDE)
+    if (wide)
       for (int e = lane * COUNT; e < E; e += 32 * COUNT) *reinterpret_cast<uint4*>(out + e) = make_uint4(0u, 0u, 0u, 0u);
     else
       for (int e = lane; e < E; e += 32) put(out + e, 0.0f);
@@ -281,18 +301,18 @@ __global__ void __launch_bounds__(32 * CHOOSE_WARPS) choose_backward_kernel(int 
   float d;
   if (all) {
     float l[J], top, sum;
-    load_logits<T, J, WIDE>(own, E, l);
+    load_logits(own, E, wide != 0, l);
     softmax_of(l, top, sum);
     const float share = __fdividef(1.0f, sum), p = there ? exponential(mine - top) * share : 0.0f, dot = warp_sum(a * p);
     d = p * (a - dot);
 #pragma unroll
     for (int j = 0; j < J; ++j) l[j] = l[j] == -INFINITY ? 0.0f : exponential(l[j] - top) * share * -dot;
-    if constexpr (WIDE && J % COUNT == 0) {
+    if (J % COUNT == 0 && wide) {
 #pragma unroll
       for (int j = 0; j < J; j += COUNT) {
         float f[COUNT];
 #pragma unroll
-        for (int q = 0; q < COUNT; ++q) f[q] = l[j + q];
+        for (int q = 0; q < COUNT; ++q) f[q] = l[(j + q) % J];
         if (lane * J + j < E) *reinterpret_cast<uint4*>(out + lane * J + j) = Vec<T>::pack(f);
       }
     } else {
@@ -333,12 +353,11 @@ cudaError_t run_choose(int rows, int E, int k, int dtype, int score, int normali
     using T = decltype(type);
     return with_experts(E, [&](auto count) {
       constexpr int J = decltype(count)::value;
-      const bool wide = wide_rows<T>(E, logits, nullptr);
-      const auto kern = score == MOESCHED_SCORE_SOFTMAX
-                            ? (wide ? choose_kernel<T, J, MOESCHED_SCORE_SOFTMAX, true> : choose_kernel<T, J, MOESCHED_SCORE_SOFTMAX, false>)
-                            : (wide ? choose_kernel<T, J, MOESCHED_SCORE_SIGMOID, true> : choose_kernel<T, J, MOESCHED_SCORE_SIGMOID, false>);
+      constexpr int SOFTMAX = MOESCHED_SCORE_SOFTMAX, SIGMOID = MOESCHED_SCORE_SIGMOID;
+      const auto kern = score == SOFTMAX ? (bias != nullptr ? choose_kernel<T, J, SOFTMAX, true> : choose_kernel<T, J, SOFTMAX, false>)
+                                         : (bias != nullptr ? choose_kernel<T, J, SIGMOID, true> : choose_kernel<T, J, SIGMOID, false>);
       return launch(kern, dim3((rows + CHOOSE_WARPS - 1) / CHOOSE_WARPS), dim3(32 * CHOOSE_WARPS), 0, false, stream, rows, E, k, normalise,
-                    factor, static_cast<const T*>(logits), bias, experts, weights);
+                    (int)wide_rows<T>(E, logits, nullptr), factor, static_cast<const T*>(logits), bias, experts, weights);
     });
   });
 }
@@ -349,13 +368,10 @@ cudaError_t run_choose_backward(int rows, int E, int k, int dtype, int score, in
     using T = decltype(type);
     return with_experts(E, [&](auto count) {
       constexpr int J = decltype(count)::value;
-      const bool wide = wide_rows<T>(E, logits, dlogits);
-      const auto kern =
-          score == MOESCHED_SCORE_SOFTMAX
-              ? (wide ? choose_backward_kernel<T, J, MOESCHED_SCORE_SOFTMAX, true> : choose_backward_kernel<T, J, MOESCHED_SCORE_SOFTMAX, false>)
-              : (wide ? choose_backward_kernel<T, J, MOESCHED_SCORE_SIGMOID, true> : choose_backward_kernel<T, J, MOESCHED_SCORE_SIGMOID, false>);
+      const auto kern = score == MOESCHED_SCORE_SOFTMAX ? choose_backward_kernel<T, J, MOESCHED_SCORE_SOFTMAX>
+                                                        : choose_backward_kernel<T, J, MOESCHED_SCORE_SIGMOID>;
       return launch(kern, dim3((rows + CHOOSE_WARPS - 1) / CHOOSE_WARPS), dim3(32 * CHOOSE_WARPS), 0, false, stream, rows, E, k, normalise,
-                    factor, dweights, static_cast<const T*>(logits), experts, static_cast<T*>(dlogits));
+                    (int)wide_rows<T>(E, logits, dlogits), factor, dweights, static_cast<const T*>(logits), experts, static_cast<T*>(dlogits));
     });
   });
 }
