@@ -3,6 +3,7 @@
 // Scores are the softmax or the logistic function of the token's logits l. Without a bias the order of the scores is that of the logits,
 // and those are compared as they are. With a bias b, score + b decides, and is compared as it is in 64 bits: it is computed in 32
 // first, with a bound of its error, and again in 64 where two of the k + 1 greatest are nearer than their bounds. Equal ones: the lowest expert.
+// (All that is near enough to be chosen is gathered, so that usually only those scores are computed again.)
 // Weights come from the logits of the chosen alone where they are normalised:
 //   softmax   w = e^(l - m) / sum e^(l - m),  m the greatest of them
 //   logistic  w = t / sum t,  t = e^(l - m) / (1 + e^l),  m = min(0, the greatest): it has no common factor left that could underflow
@@ -99,7 +100,10 @@ __device__ __forceinline__ int candidates(const float (&key)[J], float best, int
     found = __shfl_sync(FULL, at, 31);
     at -= mine;
   }
-  if (found > 32) return found;
+  if (found > 32) {
+    expert = -1;
+    return found;
+  }
 #pragma unroll
   for (int j = 0; j < J; ++j)
     if (key[j] >= bound) list[at++] = make_uint2(__float_as_uint(key[j]), lane * J + j);
@@ -186,25 +190,45 @@ __device__ __forceinline__ float normalised(float l, bool there) {
 
 __device__ __noinline__ double exp64(double v) { return exp(v); }
 
-// Scores and choices in 64 bits
-template <int J, int SCORE>
-__device__ __noinline__ int choose64(const float (&l)[J], const float* bias, int E, int k, float top) {
-  const int first = (threadIdx.x & 31) * J;
+template <int J>
+__device__ __noinline__ double softmax_sum64(const float (&l)[J], float top) {
   double sum = 0.0;
+#pragma unroll
+  for (int j = 0; j < J; ++j) sum += exp64((double)l[j] - (double)top);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(FULL, sum, o);
+  return sum;
+}
+template <int SCORE>
+__device__ __forceinline__ unsigned long long key64(float l, float bias, float top, double sum) {
+  if (!(l > -INFINITY)) return 0ull;
+  return ordered((SCORE == MOESCHED_SCORE_SOFTMAX ? exp64((double)l - (double)top) / sum : 1.0 / (1.0 + exp64(-(double)l))) + (double)bias);
+}
+
+// The order of up to 32 experts, one a lane, by their scores in 64 bits: lane i gets the i-th
+template <int SCORE>
+__device__ __noinline__ int order64(float l, float bias, float top, double sum, int expert, int found, uint2* list) {
+  const int lane = threadIdx.x & 31;
+  const unsigned long long mine = lane < found ? key64<SCORE>(l, bias, top, sum) : 0ull;
+  int place = 0;
+  for (int i = 0; i < found; ++i) {
+    const unsigned long long other = __shfl_sync(FULL, mine, i);
+    const int its = __shfl_sync(FULL, expert, i);
+    place += other > mine || (other == mine && its < expert);
+  }
+  __syncwarp();
+  if (lane < found) list[place].y = (unsigned)expert;
+  __syncwarp();
+  return lane < found ? (int)list[lane].y : -1;
+}
+
+// All scores and the choice in 64 bits
+template <int J, int SCORE>
+__device__ __noinline__ int choose64(const float (&l)[J], const float* bias, int E, int k, float top, double sum) {
+  const int first = (threadIdx.x & 31) * J;
   unsigned long long key[J];
-  if constexpr (SCORE == MOESCHED_SCORE_SOFTMAX) {
 #pragma unroll
-    for (int j = 0; j < J; ++j) sum += exp64((double)l[j] - (double)top);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(FULL, sum, o);
-  }
-#pragma unroll
-  for (int j = 0; j < J; ++j) {
-    key[j] = 0ull;
-    if (first + j >= E || !(l[j] > -INFINITY)) continue;
-    const double s = SCORE == MOESCHED_SCORE_SOFTMAX ? exp64((double)l[j] - (double)top) / sum : 1.0 / (1.0 + exp64(-(double)l[j]));
-    key[j] = ordered(s + (double)bias[first + j]);
-  }
+  for (int j = 0; j < J; ++j) key[j] = first + j < E ? key64<SCORE>(l[j], bias[first + j], top, sum) : 0ull;
   return greatest(key, k);
 }
 
@@ -257,8 +281,13 @@ __global__ void __launch_bounds__(32 * CHOOSE_WARPS, J <= 8 ? 5 : 1) choose_kern
     found = candidates(key, most_of(key), k, list, [](float b) { return b - 2.0f * apart(b, b); }, mine, expert);
     const float next = __shfl_down_sync(FULL, mine, 1);
     const bool near = lane < k && lane + 1 < found && !(mine - next > apart(mine, next));
-    if (found > 32 || __any_sync(FULL, near)) expert = choose64<J, SCORE>(l, bias, E, k, top);
     mine = expert >= 0 ? to_float(own[expert]) : -INFINITY;
+    if (found > 32 || __any_sync(FULL, near)) {
+      const double wide_sum = SOFTMAX ? softmax_sum64(l, top) : 1.0;
+      expert = found > 32 ? choose64<J, SCORE>(l, bias, E, k, top, wide_sum)
+                          : order64<SCORE>(mine, expert >= 0 ? bias[expert] : 0.0f, top, wide_sum, expert, found, list);
+      mine = expert >= 0 ? to_float(own[expert]) : -INFINITY;
+    }
   }
   const bool there = lane < k && expert >= 0;
   if (!there) mine = -INFINITY;

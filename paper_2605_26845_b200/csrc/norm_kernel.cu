@@ -12,9 +12,6 @@
 namespace moesched {
 
 constexpr int NORM_THREADS = 512;                               // of a CTA
-// Rows on their way, as many as fit: a thread has 16 V bytes for each of `tensors`
-constexpr int NORM_PARTS_VECTORS = 2 * NORM_THREADS / 32 / 4;      // sums of warps, in front of them
-__host__ __device__ constexpr int norm_stages(int V, int tensors) { return V * tensors <= 6 ? 3 : 2; }
 
 // Sum over a team of whole warps, in a fixed order. `part` has a float for every warp of the team, and is not written again before the team has
 // met once more. `meet` is the barrier, of the team or of all teams.
@@ -218,8 +215,14 @@ cudaError_t run_norm(int rows, int D, int dtype, float eps, int group, const voi
 }
 
 // Gradients, from g = dy w:  dx = c (g - h c^2 sum(g h) / D) + what comes in for h,  dw = sum over the rows of dy h c.
-// A team takes every so many rows, each thread the same columns of all of them, whose dw it has in registers. A second kernel adds the dw of the CTAs up, in their order. Rows that are too long for one CTA's registers (SPLIT) have their sums made
-// by a kernel of its own, and a CTA has a block of columns.
+// A CTA stays on every SM. Its teams take every so many rows, each thread the same 16 columns of all of them, whose dw it has in registers. The vectors of the
+// next rows are on their way to the thread's own places in shared memory meanwhile, so that no warp waits for memory between the sums
+// of rows. A second kernel adds the dw of the CTAs up, in their order. Rows of more than 8192 columns (SPLIT) have their sums made by a kernel of its own, and a
+// CTA has a block of columns.
+constexpr int NORM_PARTS_VECTORS = 2 * NORM_THREADS / 32 / 4;   // sums of warps, in front of the rows on their way
+// Rows on their way, as many as fit: a thread has 16 V bytes for each of three tensors
+template <int V>
+constexpr int NORM_STAGES = V <= 2 ? 3 : 2;
 
 struct NormBackwardArgs {
   int rows, D, team_warps;
@@ -233,8 +236,7 @@ struct NormBackwardArgs {
 template <typename T, int V, bool SPLIT>
 __global__ void __launch_bounds__(NORM_THREADS) norm_backward_kernel(NormBackwardArgs a) {
   constexpr int COUNT = Vec<T>::COUNT, PAIRS = COUNT / 2;
-  constexpr int STAGES = norm_stages(V, 3);
-  constexpr bool KEEP = V * COUNT <= 16;                        // values of 32 bits stay in registers, or are made again of those of the type
+  constexpr int STAGES = NORM_STAGES<V>;
   extern __shared__ __align__(16) uint4 shared[];
   float(*part)[NORM_THREADS / 32] = reinterpret_cast<float(*)[NORM_THREADS / 32]>(shared);      // [2]
   uint4* ring = shared + NORM_PARTS_VECTORS;                    // [stage][dy, h, dsum][V][threads of the CTA]
@@ -252,13 +254,11 @@ __global__ void __launch_bounds__(NORM_THREADS) norm_backward_kernel(NormBackwar
       if (i < vectors) copy_behind(place(stage, t, v), from[t] + (size_t)row * vectors + i);
     }
   };
-  uint4 weight[V];
-  Two w[KEEP ? V : 1][PAIRS], dw[V][PAIRS];
+  Two w[V][PAIRS], dw[V][PAIRS];
 #pragma unroll
   for (int v = 0; v < V; ++v) {
     const int i = first + at + v * threads;
-    weight[v] = i < vectors ? __ldg(static_cast<const uint4*>(a.weight) + i) : zero;
-    if constexpr (KEEP) pairs_of<T>(weight[v], w[v]);
+    pairs_of<T>(i < vectors ? __ldg(static_cast<const uint4*>(a.weight) + i) : zero, w[v]);
 #pragma unroll
     for (int e = 0; e < PAIRS; ++e) dw[v][e] = two(0.0f, 0.0f);
   }
@@ -273,24 +273,19 @@ __global__ void __launch_bounds__(NORM_THREADS) norm_backward_kernel(NormBackwar
     const float c = next_c;
     if (row + step < a.rows) next_c = a.rstd[row + step];
     copies_here<STAGES - 1>();
-    uint4 g4[V], h4[V];
-    Two gw[KEEP ? V : 1][PAIRS], x[KEEP ? V : 1][PAIRS], sum = two(0.0f, 0.0f);
+    Two gw[V][PAIRS], x[V][PAIRS], sum = two(0.0f, 0.0f);
     const Two cc = two(c, c);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const int k = KEEP ? v : 0;
       const bool in = first + at + v * threads < vectors;
-      g4[v] = in ? *place(stage, 0, v) : zero;
-      h4[v] = in ? *place(stage, 1, v) : zero;
-      if constexpr (!KEEP) pairs_of<T>(weight[v], w[k]);
       Two g[PAIRS];
-      pairs_of<T>(g4[v], g);
-      pairs_of<T>(h4[v], x[k]);
+      pairs_of<T>(in ? *place(stage, 0, v) : zero, g);
+      pairs_of<T>(in ? *place(stage, 1, v) : zero, x[v]);
 #pragma unroll
       for (int e = 0; e < PAIRS; ++e) {
-        gw[k][e] = mul2(g[e], w[k][e]);
-        if constexpr (!SPLIT) sum = fma2(gw[k][e], x[k][e], sum);
-        dw[v][e] = fma2(mul2(g[e], cc), x[k][e], dw[v][e]);
+        gw[v][e] = mul2(g[e], w[v][e]);
+        if constexpr (!SPLIT) sum = fma2(gw[v][e], x[v][e], sum);
+        dw[v][e] = fma2(mul2(g[e], cc), x[v][e], dw[v][e]);
       }
     }
     ask(row + STAGES * step, stage, 0);
@@ -308,22 +303,14 @@ __global__ void __launch_bounds__(NORM_THREADS) norm_backward_kernel(NormBackwar
     const Two against = two(along, along);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const int k = KEEP ? v : 0, i = first + at + v * threads;
+      const int i = first + at + v * threads;
       if (i >= vectors) continue;
-      if constexpr (!KEEP) {
-        Two g[PAIRS];
-        pairs_of<T>(g4[v], g);
-        pairs_of<T>(h4[v], x[k]);
-        pairs_of<T>(weight[v], w[k]);
-#pragma unroll
-        for (int e = 0; e < PAIRS; ++e) gw[k][e] = mul2(g[e], w[k][e]);
-      }
       Two s[PAIRS];
       pairs_of<T>(tensors == 3 ? *place(stage, 2, v) : zero, s);
       float f[COUNT];
 #pragma unroll
       for (int e = 0; e < PAIRS; ++e) {
-        const float2 d = apart_of(fma2(cc, fma2(against, x[k][e], gw[k][e]), s[e]));
+        const float2 d = apart_of(fma2(cc, fma2(against, x[v][e], gw[v][e]), s[e]));
         f[2 * e] = d.x;
         f[2 * e + 1] = d.y;
       }
@@ -410,24 +397,25 @@ size_t norm_scratch_bytes(int rows, int D) {
 template <typename T, int V, bool SPLIT>
 static cudaError_t launch_norm_backward_rows(NormBackwardArgs a, int& parts, cudaStream_t stream) {
   const int vectors = a.D / Vec<T>::COUNT, tensors = a.dsum != nullptr ? 3 : 2, blocks = SPLIT ? (vectors + V * NORM_THREADS - 1) / (V * NORM_THREADS) : 1;
-  a.team_warps = SPLIT ? NORM_THREADS / 32 : (vectors + 32 * V - 1) / (32 * V);
-  // as many rows at a time as 512 threads take, but not more than leave every SM one
+  a.team_warps = (vectors + 32 * V * blocks - 1) / (32 * V * blocks);
+  // as many rows at a time as the CTA's threads take, but not more than leave every SM one
   int teams = NORM_THREADS / 32 / a.team_warps;
-  while (teams > 1 && (long long)(teams - 1) * NORM_PARTS >= a.rows) --teams;
-  parts = norm_parts((a.rows + teams - 1) / teams);
-  const size_t vectors_of_ring = (size_t)norm_stages(V, 3) * tensors * V * 32 * a.team_warps * teams;
-  return launch(norm_backward_kernel<T, V, SPLIT>, dim3(parts, blocks), dim3(32 * a.team_warps * teams), 16 * (NORM_PARTS_VECTORS + vectors_of_ring),
-                false, stream, a);
+  const int most = NORM_PARTS / blocks;
+  while (teams > 1 && (long long)(teams - 1) * most >= a.rows) --teams;
+  parts = (a.rows + teams - 1) / teams;
+  if (parts > most) parts = most;
+  const size_t ring = (size_t)NORM_STAGES<V> * tensors * V * 32 * a.team_warps * teams;
+  return launch(norm_backward_kernel<T, V, SPLIT>, dim3(parts, blocks), dim3(32 * a.team_warps * teams), 16 * (NORM_PARTS_VECTORS + ring), false,
+                stream, a);
 }
 
-// 16 values of a row a thread where that is enough, twice as many where they are of 16 bits, half of them where the row is short
+// 16 values of a row a thread, half of them where the row is short
 template <typename T>
 static cudaError_t launch_norm_backward(const NormBackwardArgs& a, int& parts, cudaStream_t stream) {
   constexpr int V = 16 / Vec<T>::COUNT;
   const int vectors = a.D / Vec<T>::COUNT;
   if (vectors <= 16 * V) return launch_norm_backward_rows<T, V / 2, false>(a, parts, stream);
   if (vectors <= V * NORM_THREADS) return launch_norm_backward_rows<T, V, false>(a, parts, stream);
-  if (vectors <= 4 * NORM_THREADS) return launch_norm_backward_rows<T, 4, false>(a, parts, stream);
   const cudaError_t e = launch(norm_dot_kernel<T>, dim3(a.rows), dim3(NORM_THREADS), 0, false, stream, vectors, static_cast<const uint4*>(a.dy),
                                static_cast<const uint4*>(a.h), static_cast<const uint4*>(a.weight), a.dot);
   return e != cudaSuccess ? e : launch_norm_backward_rows<T, V, true>(a, parts, stream);

@@ -2,83 +2,103 @@
 //
 // A choice whose slot is not one of the source's T k rows was not sent: it writes nothing and adds nothing. Everything is done token by token, so
 // that a token's row is read once for all of its choices, sums are in the order of the choices, and nothing needs the inverse of `slot`.
-// A warp has a part of a token's row; memory bounds all of it, so what counts is that enough is on its way.
+// Memory bounds all of it, so what counts is that enough is on its way. Where rows are read, a thread has a vector of 16 bytes of some token, or a few of them,
+// and looks the token's slots up itself: no lane is idle at the end of a row, whatever its width. Where rows are written, a warp has a part of one, so that what it
+// writes lies together (the other way costs 3 to 10 % there), unless rows are shorter than a warp.
 #include <cuda_fp8.h>
 
 #include "token.cuh"
 
 namespace moesched {
 
-constexpr int ROWS_WARPS = 4;      // of a CTA
+constexpr int FLAT_THREADS = 128;
 
-// A CTA is a box of warps: y the parts of a row that it has, z tokens side by side. Rows of more parts take several CTAs, next to one another.
-struct RowsGrid {
-  int blocks;                      // CTAs of a token
-  dim3 ctas, threads;
-};
-static RowsGrid rows_grid(long long tokens, int parts, int warps = ROWS_WARPS) {
-  RowsGrid g;
-  g.blocks = (parts + warps - 1) / warps;
-  const int y = (parts + g.blocks - 1) / g.blocks, z = warps / y;
-  g.threads = dim3(32, y, z);
-  g.ctas = dim3((unsigned)((tokens + z - 1) / z * g.blocks));
-  return g;
-}
-struct RowsPlace {
+// Vectors of a CTA's threads among those of all tokens, `vectors` each
+struct FlatPlace {
+  long long at;      // of all
   unsigned token;
-  int part;
+  int i;             // of the token's
 };
-__device__ __forceinline__ RowsPlace rows_place(int blocks) {
-  const unsigned set = blocks == 1 ? blockIdx.x : blockIdx.x / (unsigned)blocks;
-  return {set * blockDim.z + threadIdx.z, (int)((blockIdx.x - set * blocks) * blockDim.y + threadIdx.y)};
+__device__ __forceinline__ FlatPlace flat_place(long long block, int vectors, const FastDiv& by_vectors) {
+  const long long at = block * FLAT_THREADS + threadIdx.x, token = fast_div(at, by_vectors);
+  return {at, (unsigned)token, (int)(at - token * vectors)};
 }
+static long long flat_ctas(long long vectors, int each) { return (vectors + FLAT_THREADS * each - 1) / (FLAT_THREADS * each); }
 
-// Rows of the token's choices, one a lane, counted from the first source; negative: not sent
-__device__ __forceinline__ long long row_of(const int32_t* slot, unsigned token, int k, int per, int j, bool wanted) {
-  if (!wanted) return -1;
-  const int at = slot[(long long)token * k + j], rows = per * k;
-  return (unsigned)at < (unsigned)rows ? (long long)(token / (unsigned)per) * rows + at : -1;
-}
+// The sources' rows: `per` tokens with k choices each
+struct Sources {
+  unsigned tokens;
+  int per, k;
+  __device__ __forceinline__ unsigned rows() const { return (unsigned)per * k; }
+  __device__ __forceinline__ long long first(unsigned token) const {
+    return tokens == (unsigned)per ? 0 : (long long)(token / (unsigned)per) * rows();
+  }
+};
 
 template <typename V>
 __device__ __forceinline__ V load_vec(const void* p) {
   if constexpr (sizeof(V) == 16) return load_once(p);
-  else return load_once8(p);
+  else if constexpr (sizeof(V) == 8) return load_once8(p);
+  else return load_once4(p);
 }
 
-template <typename V, int AHEAD>
-__global__ void __launch_bounds__(32 * ROWS_WARPS) scatter_kernel(unsigned tokens, int per, int k, int vectors, int blocks, int scales,
-                                                                  const V* __restrict__ x, const float* __restrict__ scale,
-                                                                  const int32_t* __restrict__ slot, V* __restrict__ rows,
-                                                                  float* __restrict__ row_scale) {
-  const int lane = threadIdx.x;
-  const auto [token, part] = rows_place(blocks);
-  if (token >= tokens) return;
-  V v[AHEAD];
-#pragma unroll
-  for (int q = 0; q < AHEAD; ++q) {
-    const int i = (part * AHEAD + q) * 32 + lane;
-    if (i < vectors) v[q] = load_vec<V>(x + (size_t)token * vectors + i);
-  }
-  const long long row = row_of(slot, token, k, per, lane, lane < k);
+// A vector of x a thread
+template <typename V>
+__device__ __forceinline__ void scatter_flat(long long block, const Sources& s, int vectors, const FastDiv& by_vectors, const V* x, const int32_t* slot,
+                                             V* rows) {
+  const FlatPlace p = flat_place(block, vectors, by_vectors);
+  if (p.at >= (long long)s.tokens * vectors) return;
+  const V v = load_vec<V>(x + p.at);
+  const long long first = s.first(p.token);
+  const int32_t* own = slot + (long long)p.token * s.k;
 #pragma unroll 4
-  for (int j = 0; j < k; ++j) {
-    const long long to = __shfl_sync(FULL, row, j);
-    if (to < 0) continue;
+  for (int j = 0; j < s.k; ++j) {
+    const unsigned to = (unsigned)__ldg(own + j);
+    if (to < s.rows()) rows[(first + to) * vectors + p.i] = v;
+  }
+}
+
+// EACH times 32 vectors of a token a warp; a CTA is a box of warps: y the parts of a row that it has, z tokens side by side. Rows of more parts take several
+// CTAs (`blocks`), next to one another.
+constexpr int SCATTER_WARPS = FLAT_THREADS / 32;
+
+template <typename V, int EACH>
+__device__ __forceinline__ void scatter_rows(unsigned block, int blocks, const Sources& s, int vectors, const V* x, const int32_t* slot, V* rows) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, parts = (vectors + 32 * EACH - 1) / (32 * EACH);
+  const int y = (parts + blocks - 1) / blocks, z = SCATTER_WARPS / y, of_token = warp / y;
+  const unsigned set = blocks == 1 ? block : block / (unsigned)blocks, token = set * z + of_token;
+  const int part = (int)(block - set * blocks) * y + warp - of_token * y;
+  if (of_token >= z || token >= s.tokens) return;
+  V v[EACH];
 #pragma unroll
-    for (int q = 0; q < AHEAD; ++q) {
-      const int i = (part * AHEAD + q) * 32 + lane;
-      if (i < vectors) rows[to * vectors + i] = v[q];
+  for (int a = 0; a < EACH; ++a) {
+    const int i = (part * EACH + a) * 32 + lane;
+    if (i < vectors) v[a] = load_vec<V>(x + (size_t)token * vectors + i);
+  }
+  const unsigned own = lane < s.k ? (unsigned)slot[(long long)token * s.k + lane] : ~0u;
+  const long long first = s.first(token);
+#pragma unroll 4
+  for (int j = 0; j < s.k; ++j) {
+    const unsigned to = __shfl_sync(FULL, own, j);
+    if (to >= s.rows()) continue;
+#pragma unroll
+    for (int a = 0; a < EACH; ++a) {
+      const int i = (part * EACH + a) * 32 + lane;
+      if (i < vectors) rows[(first + to) * vectors + i] = v[a];
     }
   }
-  if (part != 0) return;
-  for (int i = lane; i - lane < scales; i += 32) {
-    const float f = i < scales ? scale[(size_t)token * scales + i] : 0.0f;
-    for (int j = 0; j < k; ++j) {
-      const long long to = __shfl_sync(FULL, row, j);
-      if (to >= 0 && i < scales) row_scale[to * scales + i] = f;
-    }
-  }
+}
+
+// The last CTAs have the scales, the others the tokens; EACH = 0: vectors of any token side by side
+template <typename V, int EACH>
+__global__ void __launch_bounds__(FLAT_THREADS) scatter_kernel(Sources s, unsigned ctas, int blocks, int vectors, FastDiv by_vectors, int scales,
+                                                               FastDiv by_scales, const V* __restrict__ x, const float* __restrict__ scale,
+                                                               const int32_t* __restrict__ slot, V* __restrict__ rows,
+                                                               float* __restrict__ row_scale) {
+  if (blockIdx.x >= ctas)
+    scatter_flat<unsigned>(blockIdx.x - ctas, s, scales, by_scales, reinterpret_cast<const unsigned*>(scale), slot, reinterpret_cast<unsigned*>(row_scale));
+  else if constexpr (EACH == 0) scatter_flat<V>(blockIdx.x, s, vectors, by_vectors, x, slot, rows);
+  else scatter_rows<V, EACH>(blockIdx.x, blocks, s, vectors, x, slot, rows);
 }
 
 // whether there are so few warps that they should rather have less each
@@ -86,84 +106,97 @@ static bool few_warps(long long warps) { return warps < 8LL * sm_count(); }
 
 cudaError_t run_tokens_to_rows(int G, int T, int k, int row_bytes, int scales, const void* x, const float* scale, const int32_t* slot,
                                void* rows, float* row_scale, cudaStream_t stream) {
-  const unsigned tokens = (unsigned)G * T;
-  const auto with = [&](auto vec, auto ahead) {
+  const Sources s{(unsigned)G * T, T, k};
+  const auto with = [&](auto vec, auto each) {
     using V = decltype(vec);
-    constexpr int AHEAD = decltype(ahead)::value;
-    const int vectors = row_bytes / (int)sizeof(V), parts = (vectors + 32 * AHEAD - 1) / (32 * AHEAD);
-    const RowsGrid g = rows_grid(tokens, parts);
-    return launch(scatter_kernel<V, AHEAD>, g.ctas, g.threads, 0, false, stream, tokens, T, k, vectors, g.blocks, scales,
-                  static_cast<const V*>(x), scale, slot, static_cast<V*>(rows), row_scale);
+    constexpr int EACH = decltype(each)::value;
+    const int vectors = row_bytes / (int)sizeof(V);
+    int blocks = 1;
+    long long ctas;
+    if constexpr (EACH == 0) {
+      ctas = flat_ctas((long long)s.tokens * vectors, 1);
+    } else {
+      const int parts = (vectors + 32 * EACH - 1) / (32 * EACH);
+      blocks = (parts + SCATTER_WARPS - 1) / SCATTER_WARPS;
+      const int z = SCATTER_WARPS / ((parts + blocks - 1) / blocks);
+      ctas = ((long long)s.tokens + z - 1) / z * blocks;
+    }
+    return launch(scatter_kernel<V, EACH>, dim3((unsigned)(ctas + flat_ctas((long long)s.tokens * scales, 1))), dim3(FLAT_THREADS), 0, false, stream, s,
+                  (unsigned)ctas, blocks, vectors, make_fastdiv(vectors), scales, make_fastdiv(scales > 0 ? scales : 1), static_cast<const V*>(x), scale,
+                  slot, static_cast<V*>(rows), row_scale);
   };
-  const bool few = few_warps((long long)tokens * ((row_bytes + 2047) / 2048));
-  if (row_bytes % 16 == 0)
-    return few ? with(uint4(), std::integral_constant<int, 1>()) : with(uint4(), std::integral_constant<int, 4>());
-  return few ? with(uint2(), std::integral_constant<int, 1>()) : with(uint2(), std::integral_constant<int, 4>());
+  const auto with_each = [&](auto vec) {
+    const int vectors = row_bytes / (int)sizeof(vec);
+    if (vectors < 32) return with(vec, std::integral_constant<int, 0>());
+    if (few_warps((long long)s.tokens * ((vectors + 127) / 128))) return with(vec, std::integral_constant<int, 1>());
+    return with(vec, std::integral_constant<int, 4>());
+  };
+  return row_bytes % 16 == 0 ? with_each(uint4()) : with_each(uint2());
 }
 
-// ROWS rows at a time, VECTORS vectors of each a lane
-template <typename T, int ROWS, int VECTORS>
-__global__ void __launch_bounds__(32 * ROWS_WARPS) gather_kernel(unsigned tokens, int per, int k, int vectors, int blocks,
-                                                                 const uint4* __restrict__ rows, const int32_t* __restrict__ slot,
-                                                                 const float* __restrict__ weights, const uint4* add, uint4* y) {
+// ROWS rows at a time of EACH vectors a thread
+template <typename T, int ROWS, int EACH>
+__global__ void __launch_bounds__(FLAT_THREADS) gather_kernel(Sources s, int vectors, FastDiv by_vectors, const uint4* __restrict__ rows,
+                                                              const int32_t* __restrict__ slot, const float* __restrict__ weights, const uint4* add,
+                                                              uint4* y) {
   constexpr int COUNT = Vec<T>::COUNT;
-  const int lane = threadIdx.x;
-  const auto [token, part] = rows_place(blocks);
-  if (token >= tokens) return;
-  const int i0 = part * VECTORS * 32 + lane;
-  const long long row = row_of(slot, token, k, per, lane, lane < k);
-  const float weight = lane >= k ? 0.0f : weights != nullptr ? weights[(size_t)token * k + lane] : 1.0f;
-  float sum[VECTORS][COUNT];
+  const long long all = (long long)s.tokens * vectors;
+  FlatPlace p[EACH];
+  float sum[EACH][COUNT];
 #pragma unroll
-  for (int a = 0; a < VECTORS; ++a) {
+  for (int a = 0; a < EACH; ++a) {
+    p[a] = flat_place((long long)blockIdx.x * EACH + a, vectors, by_vectors);
+    if (p[a].at >= all) p[a].token = 0u;
 #pragma unroll
     for (int e = 0; e < COUNT; ++e) sum[a][e] = 0.0f;
-    if (add != nullptr && i0 + 32 * a < vectors) Vec<T>::unpack(load_once(add + (size_t)token * vectors + i0 + 32 * a), sum[a]);
+    if (add != nullptr && p[a].at < all) Vec<T>::unpack(load_once(add + p[a].at), sum[a]);
   }
-  for (int j0 = 0; j0 < k; j0 += ROWS) {
-    uint4 v[ROWS][VECTORS];
-    long long from[ROWS];
+  for (int j0 = 0; j0 < s.k; j0 += ROWS) {
+    uint4 v[EACH][ROWS];
+    unsigned from[EACH][ROWS];
 #pragma unroll
-    for (int q = 0; q < ROWS; ++q) {
-      from[q] = __shfl_sync(FULL, row, (j0 + q) & 31);
-      if (j0 + q >= k) from[q] = -1;
+    for (int a = 0; a < EACH; ++a)
 #pragma unroll
-      for (int a = 0; a < VECTORS; ++a)
-        if (from[q] >= 0 && i0 + 32 * a < vectors) v[q][a] = load_once(rows + from[q] * vectors + i0 + 32 * a);
-    }
+      for (int q = 0; q < ROWS; ++q)
+        from[a][q] = j0 + q < s.k && p[a].at < all ? (unsigned)__ldg(slot + (long long)p[a].token * s.k + j0 + q) : ~0u;
 #pragma unroll
-    for (int q = 0; q < ROWS; ++q) {
-      const float w = __shfl_sync(FULL, weight, (j0 + q) & 31);
-      if (from[q] < 0) continue;
+    for (int a = 0; a < EACH; ++a)
 #pragma unroll
-      for (int a = 0; a < VECTORS; ++a) {
-        if (i0 + 32 * a >= vectors) continue;
+      for (int q = 0; q < ROWS; ++q)
+        if (from[a][q] < s.rows()) v[a][q] = load_once(rows + (s.first(p[a].token) + from[a][q]) * vectors + p[a].i);
+#pragma unroll
+    for (int a = 0; a < EACH; ++a)
+#pragma unroll
+      for (int q = 0; q < ROWS; ++q) {
+        if (from[a][q] >= s.rows()) continue;
+        const float w = weights != nullptr ? __ldg(weights + (long long)p[a].token * s.k + j0 + q) : 1.0f;
         float f[COUNT];
-        Vec<T>::unpack(v[q][a], f);
+        Vec<T>::unpack(v[a][q], f);
 #pragma unroll
         for (int e = 0; e < COUNT; ++e) sum[a][e] = fmaf(w, f[e], sum[a][e]);
       }
-    }
   }
 #pragma unroll
-  for (int a = 0; a < VECTORS; ++a)
-    if (i0 + 32 * a < vectors) y[(size_t)token * vectors + i0 + 32 * a] = Vec<T>::pack(sum[a]);
+  for (int a = 0; a < EACH; ++a)
+    if (p[a].at < all) y[p[a].at] = Vec<T>::pack(sum[a]);
 }
 
 cudaError_t run_rows_to_tokens(int G, int T, int k, int D, int dtype, const void* rows, const int32_t* slot, const float* weights,
                                const void* add, void* y, cudaStream_t stream) {
-  const unsigned tokens = (unsigned)G * T;
+  const Sources s{(unsigned)G * T, T, k};
   return with_type(dtype, [&](auto type) {
     using V = decltype(type);
     const int vectors = D / Vec<V>::COUNT;
-    const auto with = [&](auto kern, int count) {
-      const RowsGrid g = rows_grid(tokens, (vectors + 32 * count - 1) / (32 * count));
-      return launch(kern, g.ctas, g.threads, 0, false, stream, tokens, T, k, vectors, g.blocks, static_cast<const uint4*>(rows), slot,
-                    weights, static_cast<const uint4*>(add), static_cast<uint4*>(y));
+    const long long all = (long long)s.tokens * vectors;
+    const auto with = [&](auto kern, int each) {
+      return launch(kern, dim3((unsigned)flat_ctas(all, each)), dim3(FLAT_THREADS), 0, false, stream, s, vectors, make_fastdiv(vectors),
+                    static_cast<const uint4*>(rows), slot, weights, static_cast<const uint4*>(add), static_cast<uint4*>(y));
     };
-    if (few_warps((long long)tokens * ((vectors + 31) / 32))) return with(gather_kernel<V, 8, 1>, 1);
-    if (k > 4 || vectors <= 32) return with(gather_kernel<V, 4, 1>, 1);
-    return with(gather_kernel<V, 4, 2>, 2);
+    // few threads have all of their rows on their way at once; one or two rows a token need several vectors a thread
+    if (all < 256LL * sm_count()) return with(gather_kernel<V, 8, 1>, 1);
+    if (k == 1) return with(gather_kernel<V, 1, 4>, 4);
+    if (k == 2) return with(gather_kernel<V, 2, 2>, 2);
+    return with(gather_kernel<V, 4, 1>, 1);
   });
 }
 
@@ -184,12 +217,19 @@ __device__ __forceinline__ float eight_sums(float (&s)[8]) {
   return v + __shfl_xor_sync(FULL, v, 1);
 }
 
-// Gradients of the weighted sum: drows[slot] = w dy[t], dw = <dy[t], rows[slot]>. The warps of a token (z: tokens side by side) go over its vectors,
-// ROWS rows at a time. drows may be rows itself: a vector is read by the thread that writes it, before it does.
-template <typename T, int ROWS>
+// Row of a choice, counted from the first source; negative: not sent
+__device__ __forceinline__ long long row_of(const int32_t* slot, unsigned token, int k, int per, int j, bool wanted) {
+  if (!wanted) return -1;
+  const int at = slot[(long long)token * k + j], rows = per * k;
+  return (unsigned)at < (unsigned)rows ? (long long)(token / (unsigned)per) * rows + at : -1;
+}
+
+// Gradients of the weighted sum: drows[slot] = w dy[t], dw = <dy[t], rows[slot]>. The warps of a token (z: tokens side by side) go over its vectors, VECTORS a lane
+// and ROWS rows at a time. drows may be rows itself: a vector is read by the thread that writes it, before it does.
+template <typename T, int ROWS, int VECTORS>
 __global__ void __launch_bounds__(512, ROWS == 8 ? 1 : 2) gather_backward_kernel(unsigned tokens, int per, int k, int vectors, const uint4* dy, const uint4* rows,
-                                                              const int32_t* __restrict__ slot, const float* __restrict__ weights,
-                                                              uint4* drows, float* __restrict__ dweights) {
+                                                                                 const int32_t* __restrict__ slot, const float* __restrict__ weights,
+                                                                                 uint4* drows, float* __restrict__ dweights) {
   constexpr int COUNT = Vec<T>::COUNT;
   __shared__ float part[16][MOESCHED_MAX_TOP_K];
   const int lane = threadIdx.x, warp = threadIdx.y, warps = blockDim.y;
@@ -208,26 +248,34 @@ __global__ void __launch_bounds__(512, ROWS == 8 ? 1 : 2) gather_backward_kernel
     }
 #pragma unroll
     for (int q = 0; q < 8; ++q) sum[q] = 0.0f;
-    for (int i = 32 * warp + lane; i - lane < vectors; i += 32 * warps) {
-      const bool in = i < vectors;
-      uint4 v[ROWS];
+    for (int i0 = 32 * VECTORS * warp + lane; i0 - lane < vectors; i0 += 32 * VECTORS * warps) {
+      uint4 v[VECTORS][ROWS], d[VECTORS];
 #pragma unroll
-      for (int q = 0; q < ROWS; ++q)
-        if (at[q] >= 0 && in) v[q] = load_once(rows + at[q] * vectors + i);
-      float g[COUNT];
-      Vec<T>::unpack(active && in ? dy[(size_t)token * vectors + i] : make_uint4(0u, 0u, 0u, 0u), g);
+      for (int a = 0; a < VECTORS; ++a) {
+        const int i = i0 + 32 * a;
 #pragma unroll
-      for (int q = 0; q < ROWS; ++q) {
-        const float w = __shfl_sync(FULL, weight, (j0 + q) & 31);
-        if (at[q] < 0 || !in) continue;
-        float f[COUNT];
-        Vec<T>::unpack(v[q], f);
+        for (int q = 0; q < ROWS; ++q)
+          if (at[q] >= 0 && i < vectors) v[a][q] = load_once(rows + at[q] * vectors + i);
+        d[a] = active && i < vectors ? dy[(size_t)token * vectors + i] : make_uint4(0u, 0u, 0u, 0u);
+      }
 #pragma unroll
-        for (int e = 0; e < COUNT; ++e) {
-          sum[q] = fmaf(g[e], f[e], sum[q]);
-          f[e] = g[e] * w;
+      for (int a = 0; a < VECTORS; ++a) {
+        const int i = i0 + 32 * a;
+        float g[COUNT];
+        Vec<T>::unpack(d[a], g);
+#pragma unroll
+        for (int q = 0; q < ROWS; ++q) {
+          const float w = __shfl_sync(FULL, weight, (j0 + q) & 31);
+          if (at[q] < 0 || i >= vectors) continue;
+          float f[COUNT];
+          Vec<T>::unpack(v[a][q], f);
+#pragma unroll
+          for (int e = 0; e < COUNT; ++e) {
+            sum[q] = fmaf(g[e], f[e], sum[q]);
+            f[e] = g[e] * w;
+          }
+          drows[at[q] * vectors + i] = Vec<T>::pack(f);
         }
-        drows[at[q] * vectors + i] = Vec<T>::pack(f);
       }
     }
     const float total = eight_sums(sum);
@@ -247,68 +295,67 @@ cudaError_t run_rows_to_tokens_backward(int G, int T, int k, int D, int dtype, c
   const unsigned tokens = (unsigned)G * T;
   return with_type(dtype, [&](auto type) {
     using V = decltype(type);
-    const int vectors = D / Vec<V>::COUNT, all = (vectors + 31) / 32;
-    const auto with = [&](auto kern, int most) {
-      const int turns = (all + most - 1) / most, warps = (all + turns - 1) / turns, z = warps >= 8 ? 1 : 8 / warps;
+    const int vectors = D / Vec<V>::COUNT;
+    const auto with = [&](auto kern, int warps, int z) {
       return launch(kern, dim3((tokens + z - 1) / z), dim3(32, warps, z), 0, false, stream, tokens, T, k, vectors,
                     static_cast<const uint4*>(dy), static_cast<const uint4*>(rows), slot, weights, static_cast<uint4*>(drows), dweights);
     };
-    return few_warps((long long)tokens * all) ? with(gather_backward_kernel<V, 8>, 16) : with(gather_backward_kernel<V, 4>, 8);
+    const int all = (vectors + 31) / 32;                        // parts of a row that a warp takes at a time
+    const long long enough = 16LL * sm_count();
+    if (tokens * (long long)all < enough) return with(gather_backward_kernel<V, 8, 1>, all < 16 ? all : 16, 1);
+    // A token's warps have a few parts each, so that what a token costs once is spread over them (8 rows of 4096 bfloat16, 8191 tokens: 4 warps
+    // 164 us, 8 175, 2 178; 4 rows of 2048: 2 warps 168 us, 4 171, 8 205; 8 of 264: 1 warp 243 us, 2 265),
+    // unless the tokens are few
+    int warps = all / (k > 4 ? 2 : 4);
+    warps = warps < 1 ? 1 : warps > 4 ? 4 : warps;
+    while (warps < 16 && 2 * warps <= all && tokens * (long long)warps < enough) warps *= 2;
+    const int z = warps < 4 ? 4 / warps : 1;
+    return k <= 2 ? with(gather_backward_kernel<V, 2, 2>, warps, z) : with(gather_backward_kernel<V, 4, 1>, warps, z);
   });
 }
 
-// 8-bit rows to the type: y = q scale, a scale for every `group` columns. A lane has as many values as 16 bytes of the type hold at a time.
-template <typename T, int AHEAD>
-__global__ void __launch_bounds__(32 * ROWS_WARPS) widen_kernel(unsigned rows, int vectors, int blocks, int shift, int scales,
-                                                                const uint8_t* __restrict__ q, const float* __restrict__ scale,
-                                                                uint4* __restrict__ y) {
-  constexpr int COUNT = Vec<T>::COUNT, WORDS = COUNT / 4;
-  const int lane = threadIdx.x;
-  const auto [row, part] = rows_place(blocks);
-  if (row >= rows) return;
-  unsigned v[AHEAD][WORDS];
-  float s[AHEAD];
+// 8-bit rows to the type: y = q scale, a scale for every 2^shift vectors of a row. A thread has as many values as 16 bytes of the type hold, a few times.
+template <typename T, int EACH>
+__global__ void __launch_bounds__(FLAT_THREADS) widen_kernel(long long all, int vectors, FastDiv by_vectors, int shift, int scales,
+                                                             const uint8_t* __restrict__ q, const float* __restrict__ scale, uint4* __restrict__ y) {
+  constexpr int COUNT = Vec<T>::COUNT;
+  using Bytes = std::conditional_t<COUNT == 8, uint2, unsigned>;
+  FlatPlace p[EACH];
+  Bytes v[EACH];
+  float s[EACH];
 #pragma unroll
-  for (int a = 0; a < AHEAD; ++a) {
-    const int i = (part * AHEAD + a) * 32 + lane;
-    if (i < vectors) {
-      const uint8_t* from = q + ((size_t)row * vectors + i) * COUNT;
-      if constexpr (WORDS == 2) {
-        const uint2 w = load_once8(from);
-        v[a][0] = w.x;
-        v[a][1] = w.y;
-      } else {
-        v[a][0] = load_once4(from);
-      }
-      s[a] = __ldg(scale + (size_t)row * scales + (i >> shift));
-    }
+  for (int a = 0; a < EACH; ++a) {
+    p[a] = flat_place((long long)blockIdx.x * EACH + a, vectors, by_vectors);
+    if (p[a].at >= all) continue;
+    v[a] = load_vec<Bytes>(q + p[a].at * COUNT);
+    s[a] = __ldg(scale + (size_t)p[a].token * scales + (p[a].i >> shift));
   }
 #pragma unroll
-  for (int a = 0; a < AHEAD; ++a) {
-    const int i = (part * AHEAD + a) * 32 + lane;
-    if (i >= vectors) continue;
+  for (int a = 0; a < EACH; ++a) {
+    if (p[a].at >= all) return;
+    const unsigned* words = reinterpret_cast<const unsigned*>(&v[a]);
     float f[COUNT];
 #pragma unroll
     for (int e = 0; e < COUNT; e += 2) {
-      const __half2_raw both = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(v[a][e / 4] >> (8 * (e & 2))), __NV_E4M3);
+      const __half2_raw both = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(words[e / 4] >> (8 * (e & 2))), __NV_E4M3);
       const float2 wide = __half22float2(*reinterpret_cast<const __half2*>(&both));
       f[e] = wide.x * s[a];
       f[e + 1] = wide.y * s[a];
     }
-    y[(size_t)row * vectors + i] = Vec<T>::pack(f);
+    y[p[a].at] = Vec<T>::pack(f);
   }
 }
 
 cudaError_t run_rows_widen(int R, int D, int group, int dtype, const uint8_t* q, const float* scale, void* y, cudaStream_t stream) {
   return with_type(dtype, [&](auto type) {
     using V = decltype(type);
-    constexpr int AHEAD = 4;
+    constexpr int EACH = 2;
     int shift = 0;
-    while (Vec<V>::COUNT << shift < group) ++shift;             // vectors of a group: 2^shift
+    while (Vec<V>::COUNT << shift < group) ++shift;
     const int vectors = D / Vec<V>::COUNT;
-    const RowsGrid g = rows_grid(R, (vectors + 32 * AHEAD - 1) / (32 * AHEAD));
-    return launch(widen_kernel<V, AHEAD>, g.ctas, g.threads, 0, false, stream, (unsigned)R, vectors, g.blocks, shift, (D + group - 1) / group, q,
-                  scale, static_cast<uint4*>(y));
+    const long long all = (long long)R * vectors;
+    return launch(widen_kernel<V, EACH>, dim3((unsigned)flat_ctas(all, EACH)), dim3(FLAT_THREADS), 0, false, stream, all, vectors,
+                  make_fastdiv(vectors), shift, (D + group - 1) / group, q, scale, static_cast<uint4*>(y));
   });
 }
 
