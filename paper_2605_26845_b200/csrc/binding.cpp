@@ -91,12 +91,14 @@ const Tensor& leading(PyObject* o, const char* what, size_t least) {
   return t;
 }
 
-// A tensor that has to be like that, on the GPU of `first`
-const Tensor& held(PyObject* o, ScalarType dtype, at::IntArrayRef shape, const Tensor& first, const char* what) {
-  const Tensor& t = tensor(o, what);
-  if (t.scalar_type() != dtype || !t.is_contiguous()) refuse(std::string(what) + " must be contiguous " + text(dtype));
+// A tensor that has to be like that, on the GPU of `first`; in_out: an entry of the caller's dict of outputs
+const Tensor& held(PyObject* o, ScalarType dtype, at::IntArrayRef shape, const Tensor& first, const char* what, bool in_out = false) {
+  const auto name = [&] { return in_out ? std::string("out['") + what + "']" : std::string(what); };
+  if (!THPVariable_Check(o)) refuse(name() + " must be a CUDA tensor (the library has no CPU path)");
+  const Tensor& t = THPVariable_Unpack(o);
+  if (t.scalar_type() != dtype || !t.is_contiguous()) refuse(name() + " must be contiguous " + text(dtype));
   if (t.sizes() != shape || t.device() != first.device())
-    refuse(std::string(what) + " must have shape " + text(shape) + ", on the device of the others");
+    refuse(name() + " must have shape " + text(shape) + ", on the device of the others");
   return t;
 }
 const Tensor* held_or_none(PyObject* o, ScalarType dtype, at::IntArrayRef shape, const Tensor& first, const char* what) {
@@ -120,8 +122,7 @@ struct Outputs {
   Tensor take(PyObject* name, at::IntArrayRef shape, ScalarType dtype, const Tensor& first) const {
     PyObject* o = have == nullptr ? nullptr : PyDict_GetItemWithError(have, name);
     if (o == nullptr || o == Py_None) return fresh(shape, dtype, first);
-    const std::string what = std::string("out['") + PyUnicode_AsUTF8(name) + "']";
-    return held(o, dtype, shape, first, what.c_str());
+    return held(o, dtype, shape, first, PyUnicode_AsUTF8(name), true);
   }
 };
 Tensor taken(PyObject* o, at::IntArrayRef shape, ScalarType dtype, const Tensor& first, const char* what) {

@@ -101,6 +101,7 @@ __device__ __forceinline__ int candidates(const float (&key)[J], float best, int
     at -= mine;
   }
   if (found > 32) {
+    own = -INFINITY;
     expert = -1;
     return found;
   }

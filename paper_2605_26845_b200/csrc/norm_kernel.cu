@@ -208,7 +208,7 @@ cudaError_t run_norm(int rows, int D, int dtype, float eps, int group, const voi
   NormArgs a{rows, D, 0, 0, q != nullptr ? (D + group - 1) / group : 0, eps, x, residual, weight, sum, y, q, scale, rstd};
   return with_type(dtype, [&](auto type) {
     using T = decltype(type);
-    while (Vec<T>::COUNT << a.group_shift < group) ++a.group_shift;
+    while (q != nullptr && Vec<T>::COUNT << a.group_shift < group) ++a.group_shift;
     if (residual != nullptr) return q != nullptr ? launch_norm<T, true, true>(a, stream) : launch_norm<T, true, false>(a, stream);
     return q != nullptr ? launch_norm<T, false, true>(a, stream) : launch_norm<T, false, false>(a, stream);
   });

@@ -155,6 +155,16 @@ def test_outputs_in_place_of_inputs_and_of_an_earlier_call():
             assert all(torch.equal(got[k], want[k]) for k in want)
 
 
+def test_the_group_is_not_looked_at_without_an_output_in_8_bits():
+    x, _, w, _, _ = inputs(5, 72, torch.bfloat16, 3)
+    want, y = ms.rms_norm(x, w)["y"], torch.empty_like(x)
+    for group in (2 ** 31 - 1, -5, 0):
+        y.zero_()
+        rc = ms.load_library().moesched_rms_norm(5, 72, 0, 1e-6, group, x.data_ptr(), None, w.data_ptr(), None, y.data_ptr(), None, None, None,
+                                                 torch.cuda.current_stream().cuda_stream)
+        assert rc == 0 and torch.equal(y, want)
+
+
 def test_no_rows_and_leading_dimensions():
     x, r, w, dy, dsum = inputs(24, 64, torch.bfloat16, 4)
     none = ms.rms_norm(x[:0], w, residual=r[:0], group=32, save=True)
