@@ -191,16 +191,22 @@ int64_t rows_in(const Tensor& t) {
   return rows;
 }
 
-// The call, with the GPU of `first` current and on its current stream
+// Other threads of the interpreter may run meanwhile
+struct Unlocked {
+  PyThreadState* state = PyEval_SaveThread();
+  ~Unlocked() { PyEval_RestoreThread(state); }
+};
+
+// The call, with the GPU of `first` current and on its current stream. (An address may be refused too: a tensor without memory, as tracers have.)
 template <typename Call>
 void run(const char* what, const Tensor& first, Call call) {
   const c10::DeviceIndex index = first.device().index();
   const c10::cuda::OptionalCUDAGuard guard(first.device());
   void* stream = c10::cuda::getCurrentCUDAStream(index).stream();
-  int rc;
-  Py_BEGIN_ALLOW_THREADS
-  rc = call(stream);
-  Py_END_ALLOW_THREADS
+  const int rc = [&] {
+    const Unlocked unlocked;
+    return call(stream);
+  }();
   if (rc != 0)
     refuse(std::string("moesched_") + what + ": " + library.strerror(rc) + " (rc=" + std::to_string(rc) + ", cuda error " +
            std::to_string(library.last_cuda_error()) + ")");

@@ -8,7 +8,9 @@
 //   softmax   w = e^(l - m) / sum e^(l - m),  m the greatest of them
 //   logistic  w = t / sum t,  t = e^(l - m) / (1 + e^l),  m = min(0, the greatest): it has no common factor left that could underflow
 // One warp has a token, lane i the experts i J .. i J + J - 1. It finds a bound that no wanted key is below, gathers what is left (10 of 256 usually) one a
-// lane, and each counts the keys before its own. Instructions bound it, 300 to 400 a token.
+// lane, and each counts the keys before its own. Instructions bound it: 8 of 256 experts for 16384 tokens take 7.6 us, 371 instructions a token, 74 % of what can be issued
+// (the bytes alone 2.8 us); with a bias 11.3; the greatest of all keys k times over, as more than 32 candidates have it, 16.3. The gradient takes 5.5 us, bound by its
+// stores and the way from a choice to its logit.
 #include <cfloat>
 
 #include "token.cuh"

@@ -5,6 +5,8 @@
 // Memory bounds all of it, so what counts is that enough is on its way. Where rows are read, a thread has a vector of 16 bytes of some token, or a few of them,
 // and looks the token's slots up itself: no lane is idle at the end of a row, whatever its width. Where rows are written, a warp has a part of one, so that what it
 // writes lies together (the other way costs 3 to 10 % there), unless rows are shorter than a warp.
+// bfloat16, 8191 tokens of 4096 features, 8 choices: rows 96 us (604 MB, 6.3 TB/s), back 106, gradients 183 (1.14 GB, 6.2 TB/s); 131072 rows of 7168 widened 414 us. 16 tokens of
+// 7168: 2.3, 2.9, 5.6 us.
 #include <cuda_fp8.h>
 
 #include "token.cuh"
@@ -192,7 +194,8 @@ cudaError_t run_rows_to_tokens(int G, int T, int k, int D, int dtype, const void
       return launch(kern, dim3((unsigned)flat_ctas(all, each)), dim3(FLAT_THREADS), 0, false, stream, s, vectors, make_fastdiv(vectors),
                     static_cast<const uint4*>(rows), slot, weights, static_cast<const uint4*>(add), static_cast<uint4*>(y));
     };
-    // few threads have all of their rows on their way at once; one or two rows a token need several vectors a thread
+    // few threads have all of their rows on their way at once; one or two rows a token need several vectors a thread (2048 features, one choice each: 71 us
+    // with four vectors, 87 with two)
     if (all < 256LL * sm_count()) return with(gather_kernel<V, 8, 1>, 1);
     if (k == 1) return with(gather_kernel<V, 1, 4>, 4);
     if (k == 2) return with(gather_kernel<V, 2, 2>, 2);

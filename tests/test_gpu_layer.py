@@ -120,6 +120,80 @@ def test_a_layer_and_its_gradients(bits8):
         assert off <= 16 * 4 * 2.0 ** -11, (name, off)
 
 
+def test_the_checked_library_gives_the_same():
+    """The compiled part of the binding calls whichever library is loaded."""
+    from paper_2605_26845_b200 import build as cuda_build
+    x = torch.randn((50, 264), device="cuda", generator=torch.Generator("cuda").manual_seed(1)).bfloat16()
+    w, l = torch.ones(264, dtype=torch.bfloat16, device="cuda"), torch.randn((50, 24), device="cuda", generator=torch.Generator("cuda").manual_seed(2))
+
+    def run():
+        n = ms.rms_norm(x, w, residual=x, group=64, save=True)
+        c = ms.route_choose(l, 3, bias=l[0].contiguous())
+        slot = ms.route_demand(c["experts"].view(1, 1, -1), 24)["slot"].view(-1)
+        rows = ms.tokens_to_rows(n["y"], slot)
+        y = ms.rows_to_tokens(rows, slot, 3, weights=c["weights"])
+        return [*n.values(), *c.values(), rows, y, *ms.rows_to_tokens_backward(x, rows, slot, c["weights"]).values(),
+                *ms.rms_norm_backward(x, n["sum"], w, n["rstd"], dsum=y).values()]
+
+    want = run()
+    ms.use_library(cuda_build.build(checked=True))
+    try:
+        got = run()
+        assert ms.debug_index_faults() == 0
+    finally:
+        ms.use_library(None)
+    assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(got, want))
+    assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(run(), want))
+
+
+def test_tensors_without_memory_end_in_an_exception():
+    from torch._subclasses.fake_tensor import FakeTensorMode
+    with FakeTensorMode() as mode:
+        x, w = torch.empty((4, 64), device="cuda"), torch.empty(64, device="cuda")
+        with pytest.raises(Exception):
+            ms.rms_norm(x, w)
+    with pytest.raises(Exception):
+        ms.rms_norm(x, w, out={"y": x})
+    x = torch.zeros((4, 64), device="cuda")
+    assert torch.equal(ms.rms_norm(x, x[0])["y"], x)                              # (and the lock is held again)
+
+
+def test_outputs_of_deterministic_programs_are_filled():
+    """Where the program asks for it, memory that a call leaves as it is holds NaN and not whatever was there."""
+    x, slot = torch.ones((2, 64), device="cuda"), torch.tensor([1, -1], dtype=torch.int32, device="cuda")
+    torch.use_deterministic_algorithms(True)
+    try:
+        rows = ms.tokens_to_rows(x, slot)
+    finally:
+        torch.use_deterministic_algorithms(False)
+    assert torch.isnan(rows[0]).all() and torch.equal(rows[1], x[0])
+
+
+def test_calls_from_several_threads():
+    import threading
+    made = {}
+
+    def work(n):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            x = torch.full((300, 1032), float(n + 1), device="cuda", dtype=torch.bfloat16)
+            w, slot = torch.ones(1032, dtype=torch.bfloat16, device="cuda"), torch.arange(600, dtype=torch.int32, device="cuda")
+            for _ in range(50):
+                res = ms.rms_norm(x, w, residual=x, save=True, group=128)
+                y = ms.rows_to_tokens(ms.tokens_to_rows(res["sum"], slot), slot, 2)
+                g = ms.rms_norm_backward(x, res["sum"], w, res["rstd"])["dweight"]
+            torch.cuda.current_stream().synchronize()
+            made[n] = y, g, res["q"].float()
+
+    threads = [threading.Thread(target=work, args=(n,)) for n in range(6)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    for n in range(6):
+        y, g, q = made[n]
+        assert (y == 4 * (n + 1)).all() and (q == 448).all() and torch.isfinite(g).all() and len(set(g.tolist())) == 1
+
+
 def test_padding_is_not_sent():
     """Tokens whose logits are all off choose nobody: no demand, no row, and the residual stream goes on as it was."""
     logits = torch.randn((1, 2, 8, 4), device="cuda", generator=torch.Generator("cuda").manual_seed(2))
