@@ -550,14 +550,14 @@ def _act(act):
     return _ACTS[act]
 
 
-def _no_graph(what, *tensors, backward="expert_ffn_backward"):
-    """Refuses tensors that want a gradient where autograd records: the calls are not recorded, and the gradient would be lost
+def _no_graph(what, *tensors):
+    """Refuses tensors that want a gradient where autograd records: the experts' calls are not recorded, and the gradient would be lost
     without a sign."""
     if torch.is_grad_enabled():
         for t in tensors:
             if isinstance(t, torch.Tensor) and t.requires_grad:
                 raise MoeschedError(f"{what} is not recorded by autograd, but an argument requires a gradient: call it under torch.no_grad() "
-                                    f"(gradients come from {backward}), or detach the argument")
+                                    "(gradients come from expert_ffn_backward), or detach the argument")
 
 
 def _expert_rows(x, offsets, num_experts):
@@ -724,7 +724,7 @@ _BOUND = ("rms_norm", "rms_norm_backward", "route_choose", "route_choose_backwar
 
 def _bind():
     """The calls on tokens take two or three microseconds on the GPU, and through ctypes 9 to 15 on the host: their arguments are checked and their outputs made
-    in csrc/binding.cpp, 5 to 8."""
+    in csrc/binding.cpp, 3 to 6."""
     global _bound
     lib = load_library()
     try:

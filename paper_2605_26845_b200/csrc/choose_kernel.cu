@@ -188,7 +188,8 @@ __device__ __forceinline__ float normalised(float l, bool there) {
   const float most = warp_most(l), m = SOFTMAX ? most : fminf(most, 0.0f);
   float w = SOFTMAX ? exponential(l - m) : l > 0.0f ? logistic(l) : __fdividef(exponential(l - m), 1.0f + exponential(l));
   w = there ? w : 0.0f;
-  return __fdividef(w, warp_sum(w));
+  const float sum = warp_sum(w);
+  return w == sum ? (there ? 1.0f : 0.0f) : __fdividef(w, sum);  // (of one alone it is 1 exactly, which the fast quotient need not give)
 }
 
 __device__ __noinline__ double exp64(double v) { return exp(v); }

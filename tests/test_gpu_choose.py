@@ -136,6 +136,15 @@ def test_experts_that_are_switched_off(score, normalise):
         assert (got["experts"].view(60, 2)[:, 1] == -1).all() and set(got["experts"].view(60, 2)[:, 0].tolist()) == {-1, 0}
 
 
+def test_one_normalised_choice_has_the_factor_for_its_weight_and_no_gradient():
+    for scale in (0.1, 3.0, 40.0):
+        l = logits_of(300, 60, torch.float32, 5, scale)
+        for score in ("softmax", "sigmoid"):
+            got = ms.route_choose(l, 1, score=score, normalise=True, factor=2.5)
+            assert (got["weights"] == 2.5).all()
+            assert (ms.route_choose_backward(torch.randn(300, device="cuda"), l, got["experts"], score=score, normalise=True, factor=2.5) == 0).all()
+
+
 def test_logits_that_are_no_numbers():
     l = logits_of(8, 40, torch.float32, 2)
     l[1, 7], l[2] = math.nan, math.nan
