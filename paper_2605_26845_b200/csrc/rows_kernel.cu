@@ -311,7 +311,7 @@ cudaError_t run_rows_to_tokens_backward(int G, int T, int k, int D, int dtype, c
     // unless the tokens are few
     int warps = all / (k > 4 ? 2 : 4);
     warps = warps < 1 ? 1 : warps > 4 ? 4 : warps;
-    while (warps < 16 && 2 * warps <= all && tokens * (long long)warps < enough) warps *= 2;
+    while (2 * warps <= 16 && 2 * warps <= all && tokens * (long long)warps < enough) warps *= 2;
     const int z = warps < 4 ? 4 / warps : 1;
     return k <= 2 ? with(gather_backward_kernel<V, 2, 2>, warps, z) : with(gather_backward_kernel<V, 4, 1>, warps, z);
   });
