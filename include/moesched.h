@@ -565,11 +565,11 @@ int moesched_expert_matvec4(int R, int K, int N, int E, int groups, int group, i
 /*
  * Root-mean-square norm of every token, with the residual's addition before it and an output in 8 bits behind it:
  *   h = x + r rounded to the type (without d_residual h = x),  c = 1 / sqrt(sum h^2 / D + eps),  y = h c w,
- *   q = y / scale in e4m3 (rounded to nearest, at most 448),  scale = the greatest |y| of a group of columns / 448, 2^-126 at least.
- * y is the norm of h as it is kept, in the type. q is rounded from y in 32 bits. (With 8 bits and a scale for every 128 columns a token is
- * D + 4 ceil(D / 128) bytes on a link in place of 2 D: bytes_per_token of the model.) The sum of squares is one of 32 bits: above
- * 3e38 (or with an infinity) c is 0, below 1e-38 it loses digits, and where it is 0 with an eps of 0 c is infinite. A NaN in a row
- * makes its y, its scales and what they stand for NaN.
+ *   q = y / scale in e4m3 (rounded to nearest, at most 448),  scale = the greatest |y| of a group of columns times 1/448, 2^-126 at least.
+ * y is the norm of h as it is kept, in the type. q is made of y in 32 bits: scale and quotient are those of 32 bits, and the quotient is
+ * rounded to 8. (With 8 bits and a scale for every 128 columns a token is D + 4 ceil(D / 128) bytes on a link in place of 2 D:
+ * bytes_per_token of the model.) The sum of squares is one of 32 bits: above 3e38 (or with an infinity) c is 0, below 1e-38 it loses
+ * digits, and where it is 0 with an eps of 0 c is infinite. A NaN in a row makes its y, its scales and what they stand for NaN.
  *
  *   rows       in   0 .. MOESCHED_MAX_ROWS;  eps >= 0, finite
  *   d_x        in   [rows][D];  d_residual  in  [rows][D] or NULL;  d_weight  in  [D]

@@ -5,7 +5,7 @@
 //   q = y / scale in e4m3, scale = max |y| of a group of columns / 448, from y in 32 bits
 // A team of warps has a row in registers, from one read to the outputs: V vectors of 16 bytes a thread. The greatest of a group is
 // found among the neighbouring lanes that hold it. Memory bounds all of it: 16384 x 7168 bfloat16 with residual and 8 bits 163 us (1.06 GB, 6.5 TB/s), 8191 x 4096
-// with residual 43 us (6.3 TB/s), one row of 7168 2.6 us. What counts is how many warps an SM has whose rows are on their way: 64 registers leave it 28 (with 48,
+// with residual 43 us (6.3 TB/s), one row of 7168 2.8 us. What counts is how many warps an SM has whose rows are on their way: 64 registers leave it 28 (with 48,
 // some of them spilled, 211 us; two vectors a thread 224; rows ahead in shared memory, as the gradients have them, 233), and named barriers would leave it four CTAs.
 #include <cuda_fp8.h>
 
@@ -45,6 +45,14 @@ __device__ __forceinline__ float most_or_nan(float a, float b) {
   return v;
 }
 
+// -y / s as 32 bits have it, rounded to nearest, with minus = -1 / s: a product, and what its remainder, which one instruction gives exactly, adds to it (P. Markstein,
+// "Computation of elementary functions on the IBM RISC System/6000 processor", 1990). What is rounded to 8 bits then is the nearest to y over the scale; by the product alone
+// one value in 37000 was the neighbour. (Negative, so that zeros keep their sign.)
+__device__ __forceinline__ Two minus_quotient(Two y, Two s, Two minus) {
+  const Two q = mul2(y, minus);
+  return fma2(fma2(q, s, y), minus, q);
+}
+
 // Vector i of a row: h, of which y and q are made, and where they go. All lanes of a warp come here, those without a vector with zeros.
 template <typename T, bool QUANT>
 __device__ __forceinline__ void norm_out(const NormArgs& a, const uint4& h, const uint4& w, float c, bool in, size_t row, int i) {
@@ -55,7 +63,8 @@ __device__ __forceinline__ void norm_out(const NormArgs& a, const uint4& h, cons
   float f[COUNT];
 #pragma unroll
   for (int e = 0; e < COUNT / 2; ++e) {
-    const float2 y = apart_of(mul2(mul2(x[e], two(c, c)), u[e]));
+    x[e] = mul2(mul2(x[e], two(c, c)), u[e]);
+    const float2 y = apart_of(x[e]);
     f[2 * e] = y.x;
     f[2 * e + 1] = y.y;
   }
@@ -68,15 +77,32 @@ __device__ __forceinline__ void norm_out(const NormArgs& a, const uint4& h, cons
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1)
       if (o >> a.group_shift == 0) most = most_or_nan(most, __shfl_xor_sync(FULL, most, o));
-    // not below the smallest normal number, whose reciprocal is finite: groups of zeros, or of hardly more
-    const float s = most < 448.0f * 0x1p-126f ? 0x1p-126f : most * (1.0f / 448.0f), inverse = __fdividef(1.0f, s);
+    // The scale, 2^-126 at least. (A quotient would have one rounding less, which counts for nothing: the values are divided by the scale as it is.) Groups of next to nothing are
+    // divided with both sides made larger, so that the remainders are numbers of 32 bits; what is finite is 0 over infinity, and infinity itself NaN.
+    float s = most * (1.0f / 448.0f), over = s, by = s;
+    if (most < 0x1p-60f) {
+      s = fmaxf(s, 0x1p-126f);
+      over = by = s * 0x1p80f;
+#pragma unroll
+      for (int e = 0; e < COUNT / 2; ++e) x[e] = mul2(x[e], two(0x1p80f, 0x1p80f));
+    } else if (most == INFINITY) {
+      by = 0.0f;
+    }
+    float minus = -__fdividef(1.0f, over);
+    minus = fmaf(fmaf(minus, by, 1.0f), minus, minus);
+#pragma unroll
+    for (int e = 0; e < COUNT / 2; ++e) {
+      const float2 v = apart_of(minus_quotient(x[e], two(by, by), two(minus, minus)));
+      f[2 * e] = v.x;
+      f[2 * e + 1] = v.y;
+    }
     if (in) {
       unsigned packed[COUNT / 4];
 #pragma unroll
       for (int e = 0; e < COUNT; e += 4) {
-        const unsigned lo = __nv_cvt_float2_to_fp8x2(make_float2(f[e] * inverse, f[e + 1] * inverse), __NV_SATFINITE, __NV_E4M3);
-        const unsigned hi = __nv_cvt_float2_to_fp8x2(make_float2(f[e + 2] * inverse, f[e + 3] * inverse), __NV_SATFINITE, __NV_E4M3);
-        packed[e / 4] = lo | hi << 16;
+        const unsigned lo = __nv_cvt_float2_to_fp8x2(make_float2(f[e], f[e + 1]), __NV_SATFINITE, __NV_E4M3);
+        const unsigned hi = __nv_cvt_float2_to_fp8x2(make_float2(f[e + 2], f[e + 3]), __NV_SATFINITE, __NV_E4M3);
+        packed[e / 4] = (lo | hi << 16) ^ 0x80808080u;
       }
       if constexpr (COUNT == 8) *reinterpret_cast<uint2*>(a.q + at) = make_uint2(packed[0], packed[1]);
       else *reinterpret_cast<unsigned*>(a.q + at) = packed[0];
@@ -194,7 +220,7 @@ static cudaError_t launch_norm_rows(NormArgs a, cudaStream_t stream) {
   return launch(norm_kernel<T, V, ADDED, QUANT>, dim3((unsigned)((a.rows + teams - 1) / teams)), dim3(32 * a.team_warps * teams), 0, false, stream, a);
 }
 
-// Few rows leave SMs without one, and take the less time the more threads they have (one of 7168: 2.6 us with a vector a thread, 4.0 with four). Short rows
+// Few rows leave SMs without one, and take the less time the more threads they have (one of 7168: 2.8 us with a vector a thread, 4.0 with four). Short rows
 // would leave threads without a vector (300000 x 256 with one vector a thread 95 us, with four 149).
 template <typename T, bool ADDED, bool QUANT>
 static cudaError_t launch_norm(const NormArgs& a, cudaStream_t stream) {
