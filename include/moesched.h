@@ -600,7 +600,9 @@ int moesched_rms_norm_backward(int rows, int D, int dtype, const void* d_dy, con
  * logits over the experts, or their logistic function. Experts come in falling order, the lowest first among equal ones (compared
  * as in 64 bits; without a bias by the logits themselves). An expert whose logit (or score + bias) is -infinity or NaN is not chosen; a
  * token that runs out of experts has -1 and weight 0 for the rest: choices that are not sent. Weights are scores times `factor`, without
- * the bias; with `normalise`, scores over the sum of the chosen ones, times `factor`. A NaN among a token's logits makes its weights NaN.
+ * the bias; with `normalise`, scores over the sum of the chosen ones, times `factor`. A NaN among a token's logits makes its weights NaN,
+ * and with the softmax an infinity does too: no score is a number then, and the choice is by the logits, among the experts whose bias is
+ * above -infinity, so that what is wrong shows where the token's rows come back.
  *
  *   rows       in   tokens, 0 .. MOESCHED_MAX_ROWS;  1 <= E <= MOESCHED_MAX_EXPERTS;  1 <= k <= min(E, MOESCHED_MAX_TOP_K)
  *   factor     in   finite
@@ -614,7 +616,8 @@ int moesched_route_choose(int rows, int E, int k, int dtype, int score, int norm
 
 /*
  * Gradient of the logits from that of the weights (the choice itself has none, nor has the bias). d_experts as the forward call wrote them;
- * entries outside 0 .. E-1 were not chosen. A token's experts are different ones.
+ * entries outside 0 .. E-1 were not chosen. A token's experts are different ones. Only the softmax that is not normalised looks at
+ * the logits of the others, and its gradient is NaN throughout a token with a NaN or an infinity among them (0 for those of -infinity).
  *   d_dweights  in  [rows][k] float;  d_dlogits  out  [rows][E], written throughout
  */
 int moesched_route_choose_backward(int rows, int E, int k, int dtype, int score, int normalise, float factor,

@@ -770,7 +770,8 @@ def route_choose(logits, top_k, score="softmax", bias=None, normalise=False, fac
     counts for the choice alone. Returns 'experts' [..., T * top_k] int32, a token's side by side, as route_demand takes them, and 'weights'
     [..., T * top_k] float32: the scores times factor, or with normalise=True the scores over the sum of the token's chosen ones,
     times factor. Experts whose logit (or score + bias) is -infinity or NaN are not chosen: a token without enough of them, padding for instance,
-    has -1 and weight 0. A NaN among its logits makes a token's weights NaN. `out` may hand back the dict of an earlier call.
+    has -1 and weight 0. A NaN among its logits makes a token's weights NaN, and so does an infinity with the softmax; such a
+    token chooses by its logits alone, and its output is NaN in the end. `out` may hand back the dict of an earlier call.
     Not recorded by autograd: the gradient comes from route_choose_backward."""
     return (_bound or _bind()).route_choose(logits, top_k, score, bias, normalise, factor, out)
 

@@ -236,6 +236,16 @@ __device__ __noinline__ int choose64(const float (&l)[J], const float* bias, int
   return greatest(key, k);
 }
 
+// The choice of a token whose softmax is NaN: by its logits, as without a bias, of the experts that the bias leaves
+template <int J>
+__device__ __noinline__ int choose_lost(const float (&l)[J], const float* bias, int E, int k) {
+  const int first = (threadIdx.x & 31) * J;
+  unsigned key[J];
+#pragma unroll
+  for (int j = 0; j < J; ++j) key[j] = first + j < E && bias[first + j] > -INFINITY ? ordered(l[j]) : 0u;
+  return greatest(key, k);
+}
+
 template <typename T, int J, int SCORE, bool BIAS>
 __global__ void __launch_bounds__(32 * CHOOSE_WARPS, J <= 8 ? 5 : 1) choose_kernel(int rows, int E, int k, int normalise, int wide, float factor,
                                                                    const T* __restrict__ logits, const float* __restrict__ bias,
@@ -252,7 +262,8 @@ __global__ void __launch_bounds__(32 * CHOOSE_WARPS, J <= 8 ? 5 : 1) choose_kern
   best = l[0];
 #pragma unroll
   for (int j = 1; j < J; ++j) asm("max.NaN.f32 %0, %0, %1;" : "+f"(best) : "f"(l[j]));
-  const bool lost = isnan(warp_most_or_nan(best));
+  const float most = warp_most_or_nan(best);
+  const bool lost = SOFTMAX ? !(most < INFINITY) : isnan(most); // (the softmax of infinity is NaN)
   if (lost) best = most_of(l);
   if (SOFTMAX && (BIAS || !normalise)) {
     top = warp_most(best);
@@ -286,7 +297,10 @@ __global__ void __launch_bounds__(32 * CHOOSE_WARPS, J <= 8 ? 5 : 1) choose_kern
     const float next = __shfl_down_sync(FULL, mine, 1);
     const bool near = lane < k && lane + 1 < found && !(mine - next > apart(mine, next));
     mine = expert >= 0 ? to_float(own[expert]) : -INFINITY;
-    if (found > 32 || __any_sync(FULL, near)) {
+    if (SOFTMAX && lost) {                                      // (no key is a number)
+      expert = choose_lost(l, bias, E, k);
+      mine = expert >= 0 ? to_float(own[expert]) : -INFINITY;
+    } else if (found > 32 || __any_sync(FULL, near)) {
       const double wide_sum = SOFTMAX ? softmax_sum64(l, top) : 1.0;
       expert = found > 32 ? choose64<J, SCORE>(l, bias, E, k, top, wide_sum)
                           : order64<SCORE>(mine, expert >= 0 ? bias[expert] : 0.0f, top, wide_sum, expert, found, list);
