@@ -603,6 +603,7 @@ int moesched_rms_norm_backward(int rows, int D, int dtype, const void* d_dy, con
  * the bias; with `normalise`, scores over the sum of the chosen ones, times `factor`. A NaN among a token's logits makes its weights NaN,
  * and with the softmax an infinity does too: no score is a number then, and the choice is by the logits, among the experts whose bias is
  * above -infinity, so that what is wrong shows where the token's rows come back.
+ * Weights and gradients are as near as arithmetic in 32 bits makes them, exponentials and quotients included.
  *
  *   rows       in   tokens, 0 .. MOESCHED_MAX_ROWS;  1 <= E <= MOESCHED_MAX_EXPERTS;  1 <= k <= min(E, MOESCHED_MAX_TOP_K)
  *   factor     in   finite
