@@ -726,11 +726,14 @@ def _bind():
     """The calls on tokens take two or three microseconds on the GPU, and through ctypes 9 to 15 on the host: their arguments are checked and their outputs made
     in csrc/binding.cpp, 3 to 6."""
     global _bound
+    from . import build
     lib = load_library()
     try:
+        if not build.holds(build.BINDING, build.made_for()):
+            raise ImportError("it was compiled for another torch or Python")
         from . import _binding
-    except ImportError as e:
-        raise MoeschedError(f"{os.path.join(_HERE, '_binding.so')} cannot be loaded ({e}): run `python -m paper_2605_26845_b200.build` "
+    except (ImportError, OSError) as e:
+        raise MoeschedError(f"{build.BINDING} cannot be loaded ({e}): run `python -m paper_2605_26845_b200.build` "
                             "(there is no CPU fallback)") from e
     _binding.bind(MoeschedError, torch.OutOfMemoryError, {f"moesched_{n}": ctypes.cast(getattr(lib, f"moesched_{n}"), ctypes.c_void_p).value for n in _BOUND})
     _bound = _binding

@@ -23,23 +23,39 @@ def _stale(lib) -> bool:
     return any(os.path.getmtime(d) > t for d in deps)
 
 
-def build_binding(force: bool = False) -> str:
-    """Compile the Python extension that calls the library (g++, against the installed torch; no GPU code)."""
-    source = os.path.join(CSRC, "binding.cpp")
-    newest = max(os.path.getmtime(p) for p in (source, os.path.join(HERE, "..", "include", "moesched.h")))
-    if not force and os.path.exists(BINDING) and os.path.getmtime(BINDING) >= newest:
-        return BINDING
+def made_for() -> str:
+    """What the compiled part of the binding goes with: it reads torch's C++ classes and Python's, of one version each."""
     import sysconfig
 
     import torch
+    return f"moesched binding for torch {torch.__version__} {torch.version.git_version}, Python {sysconfig.get_config_var('SOABI')};"
+
+
+def holds(path, text) -> bool:
+    """Whether a compiled file has that text in it."""
+    with open(path, "rb") as f:
+        return text.encode() in f.read()
+
+
+def build_binding(force: bool = False) -> str:
+    """Compile the Python extension that calls the library (g++, against the installed torch; no GPU code). The file says what it was made for and how: one that was made
+    for another torch or Python, or with other flags, is not up to date."""
+    import sysconfig
+
+    import torch
+    source = os.path.join(CSRC, "binding.cpp")
     root = os.path.dirname(torch.__file__)
     cuda = os.environ.get("CUDA_HOME", "/usr/local/cuda")
     includes = [sysconfig.get_paths()["include"], os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"),
                 os.path.join(cuda, "include")]
     libs = os.path.join(root, "lib")
-    subprocess.run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
-                    *(f"-I{p}" for p in includes), source, "-o", BINDING, f"-L{libs}", f"-Wl,-rpath,{libs}", "-lc10", "-lc10_cuda", "-ltorch_cpu",
-                    "-ltorch_cuda", "-ltorch_python"], check=True)
+    flags = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
+             *(f"-I{p}" for p in includes)]
+    link = [f"-L{libs}", f"-Wl,-rpath,{libs}", "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_cuda", "-ltorch_python"]
+    stamp = " ".join([made_for(), *flags, *link]).replace("\\", "/").replace('"', "'")
+    newest = max(os.path.getmtime(p) for p in (source, os.path.join(HERE, "..", "include", "moesched.h")))
+    if force or not os.path.exists(BINDING) or os.path.getmtime(BINDING) < newest or not holds(BINDING, stamp + "\0"):
+        subprocess.run([*flags, f'-DMOESCHED_STAMP="{stamp}"', source, "-o", BINDING, *link], check=True)
     return BINDING
 
 
@@ -47,9 +63,13 @@ def build(force: bool = False, verbose: bool = False, checked: bool = False) -> 
     """Compile every source to an object file (in parallel, one nvcc per file) and link the library.
     checked=True builds the variant whose kernels range-check their data-dependent indices."""
     lib = LIB_CHECKED if checked else LIB
-    build_binding(force)
-    if not (force or _stale(lib)):
-        return lib
+    if force or _stale(lib):
+        _build_library(lib, verbose, checked)
+    build_binding(force)             # (after the library, which does without it)
+    return lib
+
+
+def _build_library(lib, verbose, checked):
     from concurrent.futures import ThreadPoolExecutor
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     objdir = os.path.join(HERE, "_build_checked" if checked else "_build")
@@ -69,7 +89,6 @@ def build(force: bool = False, verbose: bool = False, checked: bool = False) -> 
         objects = list(pool.map(compile_one, SOURCES))
     subprocess.run([nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-shared", "-cudart", "static", "-o", lib,
                     *objects], check=True)
-    return lib
 
 
 if __name__ == "__main__":

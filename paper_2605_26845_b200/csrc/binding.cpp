@@ -546,6 +546,12 @@ PyMethodDef methods[] = {
     {"rows_widen", method<rows_widen, 5>(), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
+// What this file was compiled for and how, to be found in it before it is loaded
+#ifndef MOESCHED_STAMP
+#define MOESCHED_STAMP ""
+#endif
+const char stamp[] = MOESCHED_STAMP;
+
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
@@ -554,5 +560,7 @@ PyMODINIT_FUNC PyInit__binding() {
 #define X(name) names.name = PyUnicode_InternFromString(#name);
   NAMES(X)
 #undef X
-  return PyModule_Create(&module);
+  PyObject* m = PyModule_Create(&module);
+  if (m != nullptr && PyModule_AddStringConstant(m, "stamp", stamp) != 0) Py_CLEAR(m);
+  return m;
 }
