@@ -14,6 +14,7 @@ import os
 from dataclasses import dataclass
 
 import torch
+from torch.autograd import forward_ad
 
 from .workload import DEFAULT_MODEL, PROFILED_MODEL, bvn_capacity  # noqa: F401  (re-exported)
 
@@ -551,13 +552,19 @@ def _act(act):
 
 
 def _no_graph(what, *tensors):
-    """Refuses tensors that want a gradient where autograd records: the experts' calls are not recorded, and the gradient would be lost
-    without a sign."""
-    if torch.is_grad_enabled():
-        for t in tensors:
-            if isinstance(t, torch.Tensor) and t.requires_grad:
-                raise MoeschedError(f"{what} is not recorded by autograd, but an argument requires a gradient: call it under torch.no_grad() "
-                                    "(gradients come from expert_ffn_backward), or detach the argument")
+    """Refuses tensors that want a gradient where autograd records, and those with a tangent of its forward mode: the experts' calls are not recorded, and
+    both would be lost without a sign."""
+    records, tangents = torch.is_grad_enabled(), forward_ad._current_level >= 0 and torch._C._is_fwd_grad_enabled()
+    if not (records or tangents):
+        return
+    for t in tensors:
+        if not isinstance(t, torch.Tensor):
+            continue
+        if records and t.requires_grad:
+            raise MoeschedError(f"{what} is not recorded by autograd, but an argument requires a gradient: call it under torch.no_grad() "
+                                "(gradients come from expert_ffn_backward), or detach the argument")
+        if tangents and forward_ad.unpack_dual(t).tangent is not None:
+            raise MoeschedError(f"{what} has no forward mode of autograd, but an argument has a tangent: call it with its primal")
 
 
 def _expert_rows(x, offsets, num_experts):

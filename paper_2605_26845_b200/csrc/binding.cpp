@@ -9,6 +9,7 @@
 #include <ATen/core/Tensor.h>
 #include <ATen/cuda/EmptyTensor.h>
 #include <ATen/ops/empty.h>
+#include <c10/core/AutogradState.h>
 #include <c10/core/GradMode.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/cuda/CUDAGuard.h>
@@ -176,13 +177,19 @@ int group_of(PyObject* o) {
   return (int)g;
 }
 
-// Autograd does not record the calls: tensors that want a gradient are refused where it records, or the gradient would be lost without a sign
+// Autograd does not record the calls: tensors that want a gradient are refused where it records, and those with a tangent of forward mode, which no_grad() leaves on,
+// or gradient and tangent would be lost without a sign
 void unrecorded(const char* what, const char* backward, std::initializer_list<PyObject*> arguments) {
-  if (!c10::GradMode::is_enabled()) return;
-  for (PyObject* o : arguments)
-    if (THPVariable_Check(o) && THPVariable_Unpack(o).requires_grad())
+  const bool records = c10::GradMode::is_enabled(), tangents = c10::AutogradState::get_tls_state().get_fw_grad_mode();
+  for (PyObject* o : arguments) {
+    if (!THPVariable_Check(o)) continue;
+    const Tensor& t = THPVariable_Unpack(o);
+    if (records && t.requires_grad())
       refuse(std::string(what) + " is not recorded by autograd, but an argument requires a gradient: call it under torch.no_grad() "
              "(gradients come from " + backward + "), or detach the argument");
+    if (tangents && t._fw_grad(0).defined())
+      refuse(std::string(what) + " has no forward mode of autograd, but an argument has a tangent: call it with its primal");
+  }
 }
 
 int64_t rows_in(const Tensor& t) {
