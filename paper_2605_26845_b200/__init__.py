@@ -666,7 +666,7 @@ def expert_ffn_backward(dy, x, w_gate, w_up, w_down, offsets, saved, act="silu",
     in float16, fewer digits below 6e-5 and 0 below 3e-8.) Rows of dx outside the groups are left as they were (undefined in a
     tensor made here); NaN throughout, as in expert_ffn, if the offsets are out of order. `out` may hand back the dict of an earlier
     call for reuse; `scratch` is working memory of expert_scratch_bytes(R, I, groups, True). Not recorded by autograd, like expert_ffn."""
-    _no_graph("expert_ffn_backward", dy, x, w_gate, w_up, w_down)
+    _no_graph("expert_ffn_backward", dy, x, w_gate, w_up, w_down, *(out or {}).values())
     E, I, D = _expert_weights(x, w_gate, w_up, w_down)
     dtype, groups = _expert_rows(x, offsets, E)
     R, dev = x.shape[0], x.device
@@ -819,7 +819,7 @@ def rows_to_tokens_backward(dy, rows, slot, weights, out=None) -> dict:
 
 def rows_widen(rows, scale, group, dtype=torch.bfloat16, out=None):
     """Rows in 8 bits, as they arrive, in a type that expert_ffn takes: rows [..., D] float8_e4m3fn times scale [..., ceil(D / group)] float32,
-    one for every `group` columns (32, 64 or 128), rounded once to dtype (bfloat16, float16 or float32)."""
+    one for every `group` columns (32, 64 or 128), rounded once to dtype (bfloat16, float16 or float32). Not recorded by autograd."""
     return (_bound or _bind()).rows_widen(rows, scale, group, dtype, out)
 
 

@@ -179,16 +179,21 @@ int group_of(PyObject* o) {
 
 // Autograd does not record the calls: tensors that want a gradient are refused where it records, and those with a tangent of forward mode, which no_grad() leaves on,
 // or gradient and tangent would be lost without a sign
-void unrecorded(const char* what, const char* backward, std::initializer_list<PyObject*> arguments) {
+void unrecorded(const char* what, const char* backward, std::initializer_list<PyObject*> arguments, PyObject* out = nullptr) {
   const bool records = c10::GradMode::is_enabled(), tangents = c10::AutogradState::get_tls_state().get_fw_grad_mode();
-  for (PyObject* o : arguments) {
-    if (!THPVariable_Check(o)) continue;
+  const auto check = [&](PyObject* o) {
+    if (!THPVariable_Check(o)) return;
     const Tensor& t = THPVariable_Unpack(o);
     if (records && t.requires_grad())
       refuse(std::string(what) + " is not recorded by autograd, but an argument requires a gradient: call it under torch.no_grad() "
              "(gradients come from " + backward + "), or detach the argument");
     if (tangents && t._fw_grad(0).defined())
       refuse(std::string(what) + " has no forward mode of autograd, but an argument has a tangent: call it with its primal");
+  };
+  for (PyObject* o : arguments) check(o);
+  if (out != nullptr && PyDict_Check(out)) {                    // a caller's dict of outputs
+    PyObject *name, *o;
+    for (Py_ssize_t at = 0; PyDict_Next(out, &at, &name, &o);) check(o);
   }
 }
 
@@ -228,7 +233,7 @@ struct Names {
 
 // x, weight, eps, residual, group, want_y, save, out
 PyObject* rms_norm(PyObject* const* a) {
-  unrecorded("rms_norm", "rms_norm_backward", {a[0], a[1], a[3]});
+  unrecorded("rms_norm", "rms_norm_backward", {a[0], a[1], a[3]}, a[7]);
   const Tensor& x = leading(a[0], "x", 1);
   const ScalarType dtype = x.scalar_type();
   const int kind = type_of(dtype);
@@ -265,7 +270,7 @@ PyObject* rms_norm(PyObject* const* a) {
 
 // dy, h, weight, rstd, dsum, out, scratch
 PyObject* rms_norm_backward(PyObject* const* a) {
-  unrecorded("rms_norm_backward", "rms_norm_backward", {a[0], a[1], a[2], a[4]});
+  unrecorded("rms_norm_backward", "rms_norm_backward", {a[0], a[1], a[2], a[3], a[4]}, a[5]);
   const Tensor& h = leading(a[1], "h", 1);
   const ScalarType dtype = h.scalar_type();
   const int kind = type_of(dtype);
@@ -325,7 +330,7 @@ Choice choice(PyObject* logits, int64_t k, PyObject* score, PyObject* normalise,
 
 // logits, top_k, score, bias, normalise, factor, out
 PyObject* route_choose(PyObject* const* a) {
-  unrecorded("route_choose", "route_choose_backward", {a[0], a[3]});
+  unrecorded("route_choose", "route_choose_backward", {a[0], a[3]}, a[6]);
   const Choice c = choice(a[0], whole(a[1], "top_k"), a[2], a[4], a[5]);
   const Tensor* bias = held_or_none(a[3], ScalarType::Float, {c.E}, c.logits, "bias");
   on_gpu(c.logits, "logits");
@@ -387,7 +392,7 @@ Shape with(Shape s, int64_t last) {
 
 // x, slot, scale, out, out_scale
 PyObject* tokens_to_rows(PyObject* const* a) {
-  unrecorded("tokens_to_rows", "rows_to_tokens", {a[0], a[2], a[3]});
+  unrecorded("tokens_to_rows", "rows_to_tokens", {a[0], a[2], a[3], a[4]});
   const Tensor& x = leading(a[0], "x", 2);
   const ScalarType dtype = x.scalar_type();
   if (type_of(dtype) < 0 && dtype != ScalarType::Float8_e4m3fn && dtype != ScalarType::Byte)
@@ -449,7 +454,7 @@ PyObject* rows_to_tokens(PyObject* const* a) {
 
 // dy, rows, slot, weights, out
 PyObject* rows_to_tokens_backward(PyObject* const* a) {
-  unrecorded("rows_to_tokens_backward", "rows_to_tokens_backward", {a[0], a[1], a[3]});
+  unrecorded("rows_to_tokens_backward", "rows_to_tokens_backward", {a[0], a[1], a[3]}, a[4]);
   const Tensor& dy = leading(a[0], "dy", 2);
   const ScalarType dtype = dy.scalar_type();
   const int kind = type_of(dtype);
@@ -473,6 +478,7 @@ PyObject* rows_to_tokens_backward(PyObject* const* a) {
 
 // rows, scale, group, dtype, out
 PyObject* rows_widen(PyObject* const* a) {
+  unrecorded("rows_widen", "dy times scale, and for scale from dy times rows", {a[0], a[1], a[4]});
   const int kind = THPDtype_Check(a[3]) ? type_of(reinterpret_cast<THPDtype*>(a[3])->scalar_type) : -1;
   if (kind < 0) refuse("dtype must be bfloat16, float16 or float32");
   const Tensor& rows = leading(a[0], "rows", 1);
