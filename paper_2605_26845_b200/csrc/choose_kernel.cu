@@ -109,7 +109,7 @@ __device__ __forceinline__ int candidates(const float (&key)[J], float best, int
   }
 #pragma unroll
   for (int j = 0; j < J; ++j)
-    if (key[j] >= bound) list[at++] = make_uint2(__float_as_uint(key[j]), lane * J + j);
+    if (key[j] >= bound) list[MS_AT(at++, 32)] = make_uint2(__float_as_uint(key[j]), lane * J + j);
   __syncwarp();
   // up to 16 keys: two lanes for each, which count among one half of them
   const bool two_each = found <= 16;
@@ -123,7 +123,7 @@ __device__ __forceinline__ int candidates(const float (&key)[J], float best, int
     place += other + (from + i < which) > mine;                 // (no key is the greatest number)
   }
   if (two_each) place += __shfl_xor_sync(FULL, place, 16);
-  if (lane < found) list[32 + place] = entry;
+  if (lane < found) list[32 + MS_AT(place, 32)] = entry;
   __syncwarp();
   const uint2 sorted = lane < found ? list[32 + lane] : make_uint2(0xff800000u, 0xffffffffu);
   own = __uint_as_float(sorted.x);
@@ -238,7 +238,7 @@ __device__ __noinline__ int order64(float l, float bias, float top, double sum, 
     place += other > mine || (other == mine && its < expert);
   }
   __syncwarp();
-  if (lane < found) list[place].y = (unsigned)expert;
+  if (lane < found) list[MS_AT(place, 32)].y = (unsigned)expert;
   __syncwarp();
   return lane < found ? (int)list[lane].y : -1;
 }
@@ -299,7 +299,7 @@ __global__ void __launch_bounds__(32 * CHOOSE_WARPS, J <= 8 ? 5 : 1) choose_kern
 #pragma unroll
       for (int j = 0; j < J; ++j) key[j] = ordered(l[j]);
       expert = greatest(key, k);
-      mine = expert >= 0 ? to_float(own[expert]) : -INFINITY;
+      mine = expert >= 0 ? to_float(own[MS_AT(expert, E)]) : -INFINITY;
     }
   } else {
     float key[J];
@@ -313,15 +313,15 @@ __global__ void __launch_bounds__(32 * CHOOSE_WARPS, J <= 8 ? 5 : 1) choose_kern
     found = candidates(key, most_of(key), k, list, [](float b) { return b - 2.0f * apart(b, b); }, mine, expert);
     const float next = __shfl_down_sync(FULL, mine, 1);
     const bool near = lane < k && lane + 1 < found && !(mine - next > apart(mine, next));
-    mine = expert >= 0 ? to_float(own[expert]) : -INFINITY;
+    mine = expert >= 0 ? to_float(own[MS_AT(expert, E)]) : -INFINITY;
     if (SOFTMAX && lost) {                                      // (no key is a number)
       expert = choose_lost(l, bias, E, k);
-      mine = expert >= 0 ? to_float(own[expert]) : -INFINITY;
+      mine = expert >= 0 ? to_float(own[MS_AT(expert, E)]) : -INFINITY;
     } else if (found > 32 || __any_sync(FULL, near)) {
       const double wide_sum = SOFTMAX ? softmax_sum64(l, top) : 1.0;
       expert = found > 32 ? choose64<J, SCORE>(l, bias, E, k, top, wide_sum)
-                          : order64<SCORE>(mine, expert >= 0 ? bias[expert] : 0.0f, top, wide_sum, expert, found, list);
-      mine = expert >= 0 ? to_float(own[expert]) : -INFINITY;
+                          : order64<SCORE>(mine, expert >= 0 ? bias[MS_AT(expert, E)] : 0.0f, top, wide_sum, expert, found, list);
+      mine = expert >= 0 ? to_float(own[MS_AT(expert, E)]) : -INFINITY;
     }
   }
   const bool there = lane < k && expert >= 0;
@@ -360,7 +360,7 @@ __global__ void __launch_bounds__(32 * CHOOSE_WARPS) choose_backward_kernel(int 
   }
   if ((unsigned)expert >= (unsigned)E) expert = -1;
   const bool there = expert >= 0;
-  const float mine = there ? to_float(own[expert]) : -INFINITY;
+  const float mine = there ? to_float(own[MS_AT(expert, E)]) : -INFINITY;
   a = there ? a : 0.0f;
   float d;
   if (all) {
@@ -392,7 +392,7 @@ __global__ void __launch_bounds__(32 * CHOOSE_WARPS) choose_backward_kernel(int 
     d = a * logistic_slope(mine);
   }
   __syncwarp();                                                  // the chosen after all of them
-  if (there) put(out + expert, d);
+  if (there) put(out + MS_AT(expert, E), d);
 }
 
 template <typename Call>

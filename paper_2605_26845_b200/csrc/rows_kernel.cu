@@ -56,7 +56,7 @@ __device__ __forceinline__ void scatter_flat(long long block, const Sources& s, 
 #pragma unroll 4
   for (int j = 0; j < s.k; ++j) {
     const unsigned to = (unsigned)__ldg(own + j);
-    if (to < s.rows()) rows[(first + to) * vectors + p.i] = v;
+    if (to < s.rows()) rows[(first + MS_AT((int)to, (int)s.rows())) * vectors + p.i] = v;
   }
 }
 
@@ -86,7 +86,7 @@ __device__ __forceinline__ void scatter_rows(unsigned block, int blocks, const S
 #pragma unroll
     for (int a = 0; a < EACH; ++a) {
       const int i = (part * EACH + a) * 32 + lane;
-      if (i < vectors) rows[(first + to) * vectors + i] = v[a];
+      if (i < vectors) rows[(first + MS_AT((int)to, (int)s.rows())) * vectors + i] = v[a];
     }
   }
 }
@@ -165,7 +165,7 @@ __global__ void __launch_bounds__(FLAT_THREADS) gather_kernel(Sources s, int vec
     for (int a = 0; a < EACH; ++a)
 #pragma unroll
       for (int q = 0; q < ROWS; ++q)
-        if (from[a][q] < s.rows()) v[a][q] = load_once(rows + (s.first(p[a].token) + from[a][q]) * vectors + p[a].i);
+        if (from[a][q] < s.rows()) v[a][q] = load_once(rows + (s.first(p[a].token) + MS_AT((int)from[a][q], (int)s.rows())) * vectors + p[a].i);
 #pragma unroll
     for (int a = 0; a < EACH; ++a)
 #pragma unroll
@@ -224,7 +224,7 @@ __device__ __forceinline__ float eight_sums(float (&s)[8]) {
 __device__ __forceinline__ long long row_of(const int32_t* slot, unsigned token, int k, int per, int j, bool wanted) {
   if (!wanted) return -1;
   const int at = slot[(long long)token * k + j], rows = per * k;
-  return (unsigned)at < (unsigned)rows ? (long long)(token / (unsigned)per) * rows + at : -1;
+  return (unsigned)at < (unsigned)rows ? (long long)(token / (unsigned)per) * rows + MS_AT(at, rows) : -1;
 }
 
 // Gradients of the weighted sum: drows[slot] = w dy[t], dw = <dy[t], rows[slot]>. The warps of a token (z: tokens side by side) go over its vectors, VECTORS a lane
