@@ -3,13 +3,15 @@
 // Scores are the softmax or the logistic function of the token's logits l. Without a bias the order of the scores is that of the logits,
 // and those are compared as they are. With a bias b, score + b decides, and is compared as it is in 64 bits: it is computed in 32
 // first, with a bound of its error, and again in 64 where two of the k + 1 greatest are nearer than their bounds. Equal ones: the lowest expert.
-// (All that is near enough to be chosen is gathered, so that usually only those scores are computed again.)
+// (All that is near enough to be chosen is gathered, so that only those scores are computed again, unless they are more than 32. The bound of the error is one for all scores, and
+// those of a softmax that is nearly even lie within it: with a bias of 0 and logits of a spread of 1.5, 0.5, 0.1 and 0.02, 16384 x 256 take 14.7, 17.1, 24.3 and 27.0 us, and
+// 8192 x 1024 47.7, 70.1, 72.7 and 173.4, where at 0.02 nearly every token has more than 32. Logistic: 11.7 to 12.8 and 43 to 45.)
 // Weights come from the logits of the chosen alone where they are normalised:
 //   softmax   w = e^(l - m) / sum e^(l - m),  m the greatest of them
 //   logistic  w = t / sum t,  t = e^(l - m) / (1 + e^l),  m = min(0, the greatest): it has no common factor left that could underflow
 // One warp has a token, lane i the experts i J .. i J + J - 1. It finds a bound that no wanted key is below, gathers what is left (10 of 256 usually) one a
-// lane, and each counts the keys before its own. Instructions bound it: 8 of 256 experts for 16384 tokens take 7.6 us, 371 instructions a token, 74 % of what can be issued
-// (the bytes alone 2.8 us); with a bias 11.3; the greatest of all keys k times over, as more than 32 candidates have it, 16.3. The gradient takes 5.5 us, bound by its
+// lane, and each counts the keys before its own. Instructions bound it: 8 of 256 experts for 16384 tokens take 7.9 us, 387 instructions a token, 73 % of what can be issued
+// (the bytes alone 2.8 us); with a bias 11.5 (logistic) and 14.1 (softmax, which spills 20 bytes for its five CTAs an SM); 8 of 1024 for 8192 tokens 14.3, with a bias 43; the greatest of all keys k times over, as more than 32 candidates have it, 16.3. The gradient takes 5.5 us, bound by its
 // stores and the way from a choice to its logit.
 #include <cfloat>
 

@@ -5,8 +5,8 @@
 //   q = y / scale in e4m3, scale = max |y| of a group of columns / 448, from y in 32 bits
 // A team of warps has a row in registers, from one read to the outputs: V vectors of 16 bytes a thread. The greatest of a group is
 // found among the neighbouring lanes that hold it. Memory bounds all of it: 16384 x 7168 bfloat16 with residual and 8 bits 163 us (1.06 GB, 6.5 TB/s), 8191 x 4096
-// with residual 43 us (6.3 TB/s), one row of 7168 2.8 us. What counts is how many warps an SM has whose rows are on their way: 64 registers leave it 28 (with 48,
-// some of them spilled, 211 us; two vectors a thread 224; rows ahead in shared memory, as the gradients have them, 233), and named barriers would leave it four CTAs.
+// with residual 43 us (6.3 TB/s), one row of 7168 2.8 us. What counts is how many warps an SM has whose rows are on their way: 64 registers leave it 28 (bfloat16 with both outputs spills 20 bytes,
+// fp16 with a residual 52; with 48 registers 211 us; two vectors a thread 224; rows ahead in shared memory, as the gradients have them, 233), and named barriers would leave it four CTAs.
 #include <cuda_fp8.h>
 
 #include "token.cuh"
@@ -220,7 +220,8 @@ static cudaError_t launch_norm_rows(NormArgs a, cudaStream_t stream) {
   return launch(norm_kernel<T, V, ADDED, QUANT>, dim3((unsigned)((a.rows + teams - 1) / teams)), dim3(32 * a.team_warps * teams), 0, false, stream, a);
 }
 
-// Few rows leave SMs without one, and take the less time the more threads they have (one of 7168: 2.8 us with a vector a thread, 4.0 with four). Short rows
+// Few rows leave SMs without one, and take the less time the more threads they have: with a vector a thread and with four, 2.9 and 3.5 us for one row of 7168, 3.3 and 3.8 for 148,
+// 4.6 both for 222, 7.9 and 6.7 for 592; of 2048 columns (two vectors a thread) 2.0 and 3.3, 2.2 and 3.6, 2.4 and 3.6, 3.2 and 3.7. Short rows
 // would leave threads without a vector (300000 x 256 with one vector a thread 95 us, with four 149).
 template <typename T, bool ADDED, bool QUANT>
 static cudaError_t launch_norm(const NormArgs& a, cudaStream_t stream) {

@@ -103,7 +103,8 @@ __global__ void __launch_bounds__(FLAT_THREADS) scatter_kernel(Sources s, unsign
   else scatter_rows<V, EACH>(blockIdx.x, blocks, s, vectors, x, slot, rows);
 }
 
-// whether there are so few warps that they should rather have less each
+// whether there are so few warps that they should rather have less each (16 tokens of 4096 in bfloat16, 8 choices: 2.2 us with one vector a lane, 2.8 with four; the same
+// at 500 warps of four; 592 tokens 7.5 and 7.3, of 7168 10.9 and 12.4 with 8 choices, 5.1 and 4.7 with 2)
 static bool few_warps(long long warps) { return warps < 8LL * sm_count(); }
 
 cudaError_t run_tokens_to_rows(int G, int T, int k, int row_bytes, int scales, const void* x, const float* scale, const int32_t* slot,
@@ -194,8 +195,9 @@ cudaError_t run_rows_to_tokens(int G, int T, int k, int D, int dtype, const void
       return launch(kern, dim3((unsigned)flat_ctas(all, each)), dim3(FLAT_THREADS), 0, false, stream, s, vectors, make_fastdiv(vectors),
                     static_cast<const uint4*>(rows), slot, weights, static_cast<const uint4*>(add), static_cast<uint4*>(y));
     };
-    // few threads have all of their rows on their way at once; one or two rows a token need several vectors a thread (2048 features, one choice each: 71 us
-    // with four vectors, 87 with two)
+    // Few threads have all of their rows on their way at once (4096 in bfloat16, 8 choices: 16 tokens 2.8 us, 3.1 with four rows at a time; 296 tokens, four times the limit, 4.3
+    // and 4.6; 8191 tokens 111 and 106); one or two rows a token need several vectors a thread (65536 tokens of 2048: one choice 154 us with four vectors, 179 with one; two
+    // choices 180 with two, 213 with four, 209 with one).
     if (all < 256LL * sm_count()) return with(gather_kernel<V, 8, 1>, 1);
     if (k == 1) return with(gather_kernel<V, 1, 4>, 4);
     if (k == 2) return with(gather_kernel<V, 2, 2>, 2);
@@ -229,6 +231,7 @@ __device__ __forceinline__ long long row_of(const int32_t* slot, unsigned token,
 
 // Gradients of the weighted sum: drows[slot] = w dy[t], dw = <dy[t], rows[slot]>. The warps of a token (z: tokens side by side) go over its vectors, VECTORS a lane
 // and ROWS rows at a time. drows may be rows itself: a vector is read by the thread that writes it, before it does.
+// (64 registers, for two CTAs of 512: 36 bytes of them spilled in 16 bits with two rows of two vectors.)
 template <typename T, int ROWS, int VECTORS>
 __global__ void __launch_bounds__(512, ROWS == 8 ? 1 : 2) gather_backward_kernel(unsigned tokens, int per, int k, int vectors, const uint4* dy, const uint4* rows,
                                                                                  const int32_t* __restrict__ slot, const float* __restrict__ weights,
@@ -304,10 +307,12 @@ cudaError_t run_rows_to_tokens_backward(int G, int T, int k, int D, int dtype, c
                     static_cast<const uint4*>(dy), static_cast<const uint4*>(rows), slot, weights, static_cast<uint4*>(drows), dweights);
     };
     const int all = (vectors + 31) / 32;                        // parts of a row that a warp takes at a time
+    // Below 16 parts an SM all rows at once (4096, 8 choices: 16 tokens 4.1 us, 4.5 with four rows at a time; 148 tokens, the limit, 4.5 and 4.9; 222 tokens 7.5 and 6.4.
+    // With two choices 3.4, and 2.9 with two rows at a time.)
     const long long enough = 16LL * sm_count();
     if (tokens * (long long)all < enough) return with(gather_backward_kernel<V, 8, 1>, all < 16 ? all : 16, 1);
-    // A token's warps have a few parts each, so that what a token costs once is spread over them (8 rows of 4096 bfloat16, 8191 tokens: 4 warps
-    // 164 us, 8 175, 2 178; 4 rows of 2048: 2 warps 168 us, 4 171, 8 205; 8 of 264: 1 warp 243 us, 2 265),
+    // A token's warps have a few parts each, so that what a token costs once is spread over them (bfloat16. 8 rows of 4096, 8191 tokens: 1 warp 202 us, 2 190, 4 and 8 182;
+    // 4 rows of 2048, 16384 tokens: 1 warp 102 us, 2 97, 4 98, 8 116; 8 rows of 264, 60000 tokens: 1 warp 130 us, 2 142; 1 row of 2048, 32768 tokens: 1 warp 66, 2 72),
     // unless the tokens are few
     int warps = all / (k > 4 ? 2 : 4);
     warps = warps < 1 ? 1 : warps > 4 ? 4 : warps;
